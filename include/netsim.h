@@ -605,6 +605,154 @@ netsim_status netsim_solve_rates_noalloc(int32_t device, int32_t num_links,
                                          const int32_t* d_path_off, const int32_t* d_path_link,
                                          double* d_rates, int64_t* d_status, void* hip_stream);
 
+/*
+ * Operators of an expert-parallel layer.
+ *
+ * Section 6 names performance that depends on values -- the imbalance of
+ * experts -- as what a simulation needs from the outside: the bytes of an
+ * expert-parallel all-to-all follow from which experts the tokens choose and
+ * from how many bits a row has on the way.  These entry points compute, on
+ * arrays in device memory, the routing of tokens to experts, the slots and
+ * the byte matrix that follow from it (what netsim_add_all_to_all and
+ * netsim_stream_all_to_all take), rows saved in 8 bits (what travels, and
+ * what is kept for the backward pass) and the gradients.  Timed on one GPU
+ * they also give the computations of netsim_stream_compute (Section 3:
+ * operators are profiled on a single GPU).
+ *
+ * Every pointer named d_ is a device pointer of `device`; the caller owns
+ * all arrays, among them the workspaces (any content, free again once the
+ * stream has passed the call; calls that may overlap need one each).  A call
+ * checks its scalar arguments, enqueues kernels on hip_stream (NULL: the
+ * default stream), allocates nothing, never synchronises and may be captured
+ * in a graph.  Outputs must not overlap inputs.  Rows of `ld` elements
+ * (ld >= the row's length) may be parts of wider arrays.  Values read on the
+ * device that would lead out of an array (experts, rows, offsets out of
+ * range) are left out, as -1 is.  Sums are held in 32 bits or more; calls
+ * with the same inputs give the same bits.
+ */
+
+/* Element types. */
+enum { NETSIM_F32 = 0, NETSIM_BF16 = 1, NETSIM_F16 = 2 };
+/* netsim_router.scores */
+enum { NETSIM_SCORES_SOFTMAX = 0, NETSIM_SCORES_SIGMOID = 1 };
+
+typedef struct {
+  int32_t experts;           /* 1 .. 1024                                        */
+  int32_t top_k;             /* experts a token chooses: 1 .. 32, <= experts     */
+  int32_t scores;            /* NETSIM_SCORES_*                                  */
+  int32_t renormalise;       /* 1: a token's weights are divided by their sum    */
+  int32_t groups;            /* divides experts; groups of consecutive experts   */
+  int32_t groups_kept;       /* 1 .. groups: the groups a token chooses from     */
+  int32_t group_best;        /* 1 or 2: a group counts with the sum of so many of
+                                its largest choice values                         */
+  float scale;               /* factor of every weight (finite)                  */
+} netsim_router;
+
+/*
+ * Routing.  Of a row l of logits: scores s = softmax(l) or 1/(1 + exp(-l)),
+ * choice values c = s + d_bias[expert] (d_bias may be NULL: none; the bias
+ * balances the experts and has no part in the weights).  Of the groups_kept
+ * groups of the largest group values the top_k largest c are chosen, equal
+ * ones from the lowest expert on; weights w = s, divided by the sum of the
+ * chosen s if renormalise, times scale.  Without a bias, and where no scores
+ * are summed for a group, the logits themselves are compared: the same order
+ * without the rounding of the scores.
+ *   d_logits[tokens x ld_logits], d_bias[experts] (float32 or NULL),
+ *   d_experts[tokens x top_k]: the chosen experts, best first,
+ *   d_weights[tokens x top_k]: their weights (float32).
+ * A logit of minus infinity takes an expert out of the row (a c of minus
+ * infinity too); where fewer than top_k are left, the last experts are -1
+ * with weight 0, a row without any is all -1 and 0.  Chosen scores whose sum
+ * underflows to 0 have weights 0 when renormalised, and no gradient.  Finite logits, the
+ * type's lowest value too, are values as any other.  A row whose scores are
+ * not defined (a NaN; plus infinity under softmax) has experts -1 and NaN
+ * weights.
+ */
+netsim_status netsim_route(int32_t device, const netsim_router* router, int64_t tokens, int32_t type,
+                           const void* d_logits, int64_t ld_logits, const float* d_bias,
+                           int32_t* d_experts, float* d_weights, void* hip_stream);
+
+/*
+ * Routing's backward pass: d_dlogits[tokens x ld_dlogits] (the logits' type)
+ * = the gradient of sum_j d_dweights[j] w_j with the choice d_experts held
+ * (distinct experts in a row, -1 for none; the bias has no gradient).  All
+ * `experts` elements of a row are written, zero where nothing depends on
+ * the logit; a row without any expert is zero.
+ */
+netsim_status netsim_route_backward(int32_t device, const netsim_router* router, int64_t tokens,
+                                    int32_t type, const void* d_logits, int64_t ld_logits,
+                                    const int32_t* d_experts, const float* d_dweights, void* d_dlogits,
+                                    int64_t ld_dlogits, void* hip_stream);
+
+/*
+ * Dispatch of the routed tokens d_experts[tokens x top_k].  The choices are
+ * ordered by expert, within one by token and then by position in the row:
+ *   d_offsets[experts + 1]: expert e has the slots d_offsets[e] ..
+ *     d_offsets[e+1]-1;
+ *   d_token_of_slot[tokens x top_k]: the token of every slot, -1 beyond
+ *     d_offsets[experts];
+ *   d_slot_of_choice[tokens x top_k]: the slot of every choice, -1 for none;
+ *   d_traffic[ranks x ranks] (row-major, may be NULL): bytes from the rank
+ *     that holds a token (token / tokens_per_rank) to the rank that holds
+ *     its expert (expert / (experts / ranks)): row_bytes per choice, or with
+ *     once_per_rank = 1 per token and destination, however many of the
+ *     token's experts live there.  The diagonal holds what stays.
+ * ranks: 1 .. 1024, divides experts; tokens <= ranks * tokens_per_rank;
+ * at most 2^31-1 choices.  d_work: netsim_dispatch_work_bytes(...) bytes
+ * (-1 for sizes netsim_dispatch refuses), aligned to 4.
+ */
+int64_t netsim_dispatch_work_bytes(int32_t experts, int32_t top_k, int64_t tokens, int32_t ranks,
+                                   int64_t tokens_per_rank);
+netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_t top_k, int64_t tokens,
+                              const int32_t* d_experts, int32_t ranks, int64_t tokens_per_rank,
+                              double row_bytes, int32_t once_per_rank, int32_t* d_offsets,
+                              int32_t* d_token_of_slot, int32_t* d_slot_of_choice, double* d_traffic,
+                              void* d_work, int64_t work_bytes, void* hip_stream);
+
+/*
+ * Rows saved in 8 bits.  With blocks = (cols + 31) / 32 a saved row is
+ * 32*blocks signed whole numbers q (zeros beyond cols) and `blocks`
+ * exponents e, one per 32 columns: x is q 2^e with e = floor(log2 of the
+ * block's largest magnitude) - 6, at least -126, q = x 2^-e rounded to
+ * nearest even and held to +-127.  So |x - q 2^e| <= 2^e, 2^(e-1) where q
+ * was not held: at most 1/64 of the block's largest magnitude, and restoring
+ * never overflows.  A block with an infinity or a NaN has e = -128 and
+ * restores as NaN.
+ *   d_x[rows x ld_x], d_q[rows x 32*blocks] (aligned to 16),
+ *   d_exponents[rows x blocks]; cols: 1 .. 2^20.
+ */
+netsim_status netsim_act_save(int32_t device, int64_t rows, int32_t cols, int32_t type,
+                              const void* d_x, int64_t ld_x, int8_t* d_q, int8_t* d_exponents,
+                              void* hip_stream);
+netsim_status netsim_act_restore(int32_t device, int64_t rows, int32_t cols, const int8_t* d_q,
+                                 const int8_t* d_exponents, int32_t type, void* d_x, int64_t ld_x,
+                                 void* hip_stream);
+
+/*
+ * The experts' weight gradients from saved rows: with x the `rows` rows that
+ * d_q and d_exponents hold,
+ *   d_dw[e][i][c] = sum over e's slots s of d_dy[s][i] * x[row(s)][c],
+ * row(s) = d_row_of_slot[s] (NULL: s) -- the gradient of y_s = W_e x_row(s).
+ *   d_dy[slots x ld_dy] of `type` (n values a row), d_offsets[experts + 1]
+ *   as netsim_dispatch gives them (not decreasing, within 0 .. slots),
+ *   d_dw[experts x n x cols] of out_type, contiguous; zero for an expert
+ *   without slots.
+ * dy takes part with all its bits (float16 and float32 as two and three
+ * bfloat16 terms, magnitudes below 2^-126 not kept exactly), x as restored,
+ * the sums in 32 bits, rounded once to out_type.  A slot whose row is out of
+ * range counts as a row of zeros.  experts: 1 .. 1024; n, cols: 1 .. 2^20;
+ * slots <= 2^31-1.  d_work: netsim_act_weight_grad_work_bytes(...) bytes
+ * (-1 for refused sizes), aligned to 16.
+ */
+int64_t netsim_act_weight_grad_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                          int32_t type);
+netsim_status netsim_act_weight_grad(int32_t device, int32_t experts, int64_t slots, int32_t n,
+                                     int32_t cols, int32_t type, const void* d_dy, int64_t ld_dy,
+                                     int64_t rows, const int8_t* d_q, const int8_t* d_exponents,
+                                     const int32_t* d_row_of_slot, const int32_t* d_offsets,
+                                     int32_t out_type, void* d_dw, void* d_work, int64_t work_bytes,
+                                     void* hip_stream);
+
 /* Message of the last failure on h (or of the calling thread when h is NULL). */
 const char* netsim_last_error(const netsim_t* h);
 

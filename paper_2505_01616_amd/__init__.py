@@ -1,8 +1,9 @@
 """MI355X flow-level network simulator (max-min fair bandwidth sharing).
 
 The C ABI is ``include/netsim.h``; ``netsim`` is its ctypes binding and
-``program`` loads workload descriptions into a handle.  Build the library
+``program`` loads workload descriptions into a handle; ``moe`` has the
+operators of an expert-parallel layer on torch tensors.  Build the library
 with ``python -m paper_2505_01616_amd.build``.
 """
 
-__all__ = ["netsim", "program"]
+__all__ = ["netsim", "program", "moe"]

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnetsim.so")
 SOURCES = ["netsim.cpp", "fabric.cpp", "kernels.hip", "wave.hip", "xwave.hip", "exact.hip", "sweep.hip", "history.hip",
-           "results.hip"]
+           "results.hip", "moe.hip", "act.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

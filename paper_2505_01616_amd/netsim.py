@@ -28,6 +28,9 @@ RING_ALLREDUCE, RING_REDUCE_SCATTER, RING_ALL_GATHER = 0, 1, 2
 MODE_CHAINED, MODE_FLAT, MODE_AGGREGATED = 0, 1, 2
 EXEC_AUTO, EXEC_GRID, EXEC_BLOCK, EXEC_CLUSTER, EXEC_EXACT = 0, 1, 2, 3, 4
 
+F32, BF16, F16 = 0, 1, 2
+SCORES_SOFTMAX, SCORES_SIGMOID = 0, 1
+
 STATUS_NAMES = {OK: "NETSIM_OK", E_INVALID: "NETSIM_E_INVALID", E_NOMEM: "NETSIM_E_NOMEM",
                 E_DEVICE: "NETSIM_E_DEVICE", E_STATE: "NETSIM_E_STATE", E_LIMIT: "NETSIM_E_LIMIT"}
 
@@ -72,6 +75,13 @@ class netsim_stats(ctypes.Structure):
         d = {k: getattr(self, k) for k, _ in self._fields_ if k != "reserved"}
         d["phase_seconds"] = list(self.phase_seconds)
         return d
+
+
+class netsim_router(ctypes.Structure):
+    _fields_ = [("experts", ctypes.c_int32), ("top_k", ctypes.c_int32), ("scores", ctypes.c_int32),
+                ("renormalise", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("groups_kept", ctypes.c_int32), ("group_best", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class NetsimError(RuntimeError):
@@ -125,6 +135,17 @@ _SIGS = {
     "netsim_num_checkpoints": (_I32, [_H, ctypes.POINTER(_I64)]),
     "netsim_solve_rates_noalloc": (_I32, [_I32, _I32, _P, _I32, _P, _P, _P, _P, _P]),
     "netsim_bench_sweeps": (_I32, [_H, _I32, _I64, _P, _I32, _I64, _P, _P, _P, _P, _P]),
+    "netsim_route": (_I32, [_I32, ctypes.POINTER(netsim_router), _I64, _I32, _P, _I64, _P, _P, _P, _P]),
+    "netsim_route_backward": (_I32, [_I32, ctypes.POINTER(netsim_router), _I64, _I32, _P, _I64, _P, _P,
+                                     _P, _I64, _P]),
+    "netsim_dispatch_work_bytes": (_I64, [_I32, _I32, _I64, _I32, _I64]),
+    "netsim_dispatch": (_I32, [_I32, _I32, _I32, _I64, _P, _I32, _I64, _D, _I32, _P, _P, _P, _P, _P, _I64,
+                               _P]),
+    "netsim_act_save": (_I32, [_I32, _I64, _I32, _I32, _P, _I64, _P, _P, _P]),
+    "netsim_act_restore": (_I32, [_I32, _I64, _I32, _P, _P, _I32, _P, _I64, _P]),
+    "netsim_act_weight_grad_work_bytes": (_I64, [_I32, _I64, _I32, _I32, _I32]),
+    "netsim_act_weight_grad": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _P, _I64, _I64, _P, _P, _P, _P,
+                                      _I32, _P, _P, _I64, _P]),
     "netsim_last_error": (ctypes.c_char_p, [_H]),
     "netsim_destroy": (None, [_H]),
 }
@@ -464,6 +485,51 @@ def netsim_solve_rates_noalloc(device, num_links, d_cap, num_flows, d_path_off, 
     _check(None, load_library().netsim_solve_rates_noalloc(
         int(device), int(num_links), _P(d_cap), int(num_flows), _P(d_path_off), _P(d_path_link),
         _P(d_rates), _P(d_status), _stream(stream)))
+
+
+# The operators on device arrays: arguments are device addresses (ints, None
+# for NULL), in the order of include/netsim.h; moe.py calls them on tensors.
+def netsim_route(device, router, tokens, type, d_logits, ld_logits, d_bias, d_experts, d_weights, stream=None):
+    _check(None, load_library().netsim_route(device, ctypes.byref(router), tokens, type, d_logits, ld_logits, d_bias,
+                                             d_experts, d_weights, _stream(stream)))
+
+
+def netsim_route_backward(device, router, tokens, type, d_logits, ld_logits, d_experts, d_dweights, d_dlogits,
+                          ld_dlogits, stream=None):
+    _check(None, load_library().netsim_route_backward(device, ctypes.byref(router), tokens, type, d_logits, ld_logits,
+                                                      d_experts, d_dweights, d_dlogits, ld_dlogits, _stream(stream)))
+
+
+def netsim_dispatch_work_bytes(experts, top_k, tokens, ranks, tokens_per_rank) -> int:
+    return load_library().netsim_dispatch_work_bytes(experts, top_k, tokens, ranks, tokens_per_rank)
+
+
+def netsim_dispatch(device, experts, top_k, tokens, d_experts, ranks, tokens_per_rank, row_bytes, once_per_rank,
+                    d_offsets, d_token_of_slot, d_slot_of_choice, d_traffic, d_work, work_bytes, stream=None):
+    _check(None, load_library().netsim_dispatch(device, experts, top_k, tokens, d_experts, ranks, tokens_per_rank,
+                                                row_bytes, once_per_rank, d_offsets, d_token_of_slot,
+                                                d_slot_of_choice, d_traffic, d_work, work_bytes, _stream(stream)))
+
+
+def netsim_act_save(device, rows, cols, type, d_x, ld_x, d_q, d_exponents, stream=None):
+    _check(None, load_library().netsim_act_save(device, rows, cols, type, d_x, ld_x, d_q, d_exponents,
+                                                _stream(stream)))
+
+
+def netsim_act_restore(device, rows, cols, d_q, d_exponents, type, d_x, ld_x, stream=None):
+    _check(None, load_library().netsim_act_restore(device, rows, cols, d_q, d_exponents, type, d_x, ld_x,
+                                                   _stream(stream)))
+
+
+def netsim_act_weight_grad_work_bytes(experts, slots, n, cols, type) -> int:
+    return load_library().netsim_act_weight_grad_work_bytes(experts, slots, n, cols, type)
+
+
+def netsim_act_weight_grad(device, experts, slots, n, cols, type, d_dy, ld_dy, rows, d_q, d_exponents, d_row_of_slot,
+                           d_offsets, out_type, d_dw, d_work, work_bytes, stream=None):
+    _check(None, load_library().netsim_act_weight_grad(device, experts, slots, n, cols, type, d_dy, ld_dy, rows, d_q,
+                                                       d_exponents, d_row_of_slot, d_offsets, out_type, d_dw, d_work,
+                                                       work_bytes, _stream(stream)))
 
 
 def netsim_last_error(h=None) -> str:
