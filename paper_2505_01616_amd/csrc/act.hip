@@ -8,6 +8,8 @@
 // rows exactly, and its only roundings are those of its 32-bit sums.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ops.h"
 
 namespace netsim_ops {
@@ -77,16 +79,29 @@ __global__ __launch_bounds__(256) void restore_kernel(int64_t rows, int cols, in
 
 // --------------------------------------------------------- weight gradient
 // dW[e][n][c] = sum over the slots s of expert e of dy[s][n] x[row(s)][c].
-// A workgroup per 128 x 128 tile of one expert's gradient; a step takes 32
-// slots through shared memory.  dy enters the matrix cores as bfloat16: one
-// term for bfloat16, two for float16 and three for float32, whose sum is the
-// value without rounding (down to bfloat16's smallest magnitude).
+// The sum runs over slots, so both factors lie with the summed index as
+// their slow one: tiles of KB slots go to shared memory as they lie, and the
+// matrix cores' operands (eight slots of one column in a lane) come from
+// transposing reads.  Saved rows are widened to bfloat16 on their way into
+// shared memory, once per workgroup.  dy enters as bfloat16: one term for
+// bfloat16, two for float16 and three for float32, whose sum is the value
+// without rounding (down to bfloat16's smallest magnitude).
 using bf16x8 = __attribute__((ext_vector_type(8))) __bf16;
+using s16x4 = __attribute__((ext_vector_type(4))) short;
+using s16x8 = __attribute__((ext_vector_type(8))) short;
 using f32x16 = __attribute__((ext_vector_type(16))) float;
+using lds_s16x4 = __attribute__((address_space(3))) s16x4;
 
 struct Grad {
-  int experts, n, cols, blocks;
-  int64_t slots, rows, ld;
+  int experts, n, cols, blocks, slots;
+  int64_t rows, ld;
+  bool wide_stores;   // four columns of dW at a time are aligned
+};
+
+// A part of an expert's slots.  partial < 0: the whole sum, written to dW;
+// otherwise the number of the partial sum in the workspace.
+struct Item {
+  int expert, from, to, partial;
 };
 
 template <class T>
@@ -110,75 +125,210 @@ __device__ __forceinline__ float top_bits(float y) {
   return __uint_as_float(b & 0xffff0000u);
 }
 
-// The bounds of an expert's slots, held to the arrays.
-__device__ __forceinline__ void segment(const int32_t* offsets, int e, int64_t slots, int64_t* from, int64_t* to) {
-  const int64_t a = offsets[e], b = offsets[e + 1];
-  *from = a < 0 ? 0 : a > slots ? slots : a;
-  *to = b < *from ? *from : b > slots ? slots : b;
+// Two floats of at most 8 significant bits as bfloat16, a in the low half.
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
-template <class T, class O>
-__global__ __launch_bounds__(256) void grad_kernel(Grad g, const T* __restrict__ dy, const int8_t* __restrict__ q,
-                                                   const int8_t* __restrict__ exponents,
-                                                   const int32_t* __restrict__ row_of_slot,
-                                                   const int32_t* __restrict__ offsets, O* __restrict__ dw) {
-  constexpr int TERMS = Terms<T>::value, K = 32, PITCH = K + 8;
-  __shared__ __align__(16) bf16 y_tile[TERMS][128 * PITCH];  // [n][slot]
-  __shared__ __align__(16) bf16 x_tile[128 * PITCH];         // [column][slot]
+// Eight values of a row of dy; beyond `left` of them zeros.
+template <class T>
+struct Eight {
+  T v[8];
+};
+template <class T>
+__device__ __forceinline__ Eight<T> load_eight(const T* p, int left) {
+  Eight<T> out;
+  if (left >= 8) {
+    __builtin_memcpy(&out, p, sizeof(out));   // at any alignment
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out.v[i] = i < left ? p[i] : (T)0.0f;
+  }
+  return out;
+}
+
+// The bounds of an expert's slots, held to the arrays.
+__device__ __forceinline__ Item segment(const int32_t* offsets, int e, int slots) {
+  const int a = min(max(offsets[e], 0), slots), b = min(max(offsets[e + 1], a), slots);
+  return Item{e, a, b, -1};
+}
+
+template <class T, class O, int BN, int BC, int WN, int WC, int KB>
+__global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* __restrict__ items,
+                                                            const T* __restrict__ dy, const int8_t* __restrict__ q,
+                                                            const int8_t* __restrict__ exponents,
+                                                            const int32_t* __restrict__ row_of_slot,
+                                                            const int32_t* __restrict__ offsets, O* __restrict__ dw,
+                                                            float* __restrict__ partials) {
+  constexpr int THREADS = 64 * WN * WC, TERMS = Terms<T>::value;
+  // 64 bytes more than a row: the four rows of a transposing read of 32
+  // columns lie in different quarters of the banks
+  constexpr int PY = BN + 32, PX = BC + 32, STAGE = KB * (TERMS * PY + PX);
+  constexpr int CY = BN / 8, NY = KB * CY / THREADS, CX = BC / 16, NX = KB * CX / THREADS;
+  constexpr int FN = BN / WN / 32, FC = BC / WC / 32;
+  static_assert(THREADS % CY == 0 && THREADS % CX == 0 && NY * THREADS == KB * CY && NX * THREADS == KB * CX, "");
+  extern __shared__ __align__(16) bf16 shared[];
+
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int e = blockIdx.z, n0 = blockIdx.y * 128, c0 = blockIdx.x * 128;
-  int64_t from, to;
-  segment(offsets, e, g.slots, &from, &to);
-  f32x16 acc[2][2] = {};
-  for (int64_t s0 = from; s0 < to; s0 += K) {
-    __syncthreads();
-    for (int i = tid; i < K * 128; i += 256) {
-      const int k = i >> 7, m = i & 127;
-      const int64_t s = s0 + k;
-      float y = s < to && n0 + m < g.n ? (float)dy[s * g.ld + n0 + m] : 0.0f;
+  const int tiles_n = (g.n + BN - 1) / BN;
+  const int n0 = (int)(blockIdx.x % tiles_n) * BN, c0 = (int)(blockIdx.x / tiles_n) * BC;
+  const Item it = items ? items[blockIdx.y] : segment(offsets, blockIdx.y, g.slots);
+  if (it.expert < 0) return;
+
+  // this thread's part of a tile of dy and of saved rows
+  const int y_chunk = tid % CY, y_row = tid / CY, x_chunk = tid % CX, x_row = tid / CX;
+  const int y_left = g.n - (n0 + y_chunk * 8);
+  const bool x_in = c0 + x_chunk * 16 < g.blocks * kBlock;
+  const T* y_at = dy + (int64_t)(it.from + y_row) * g.ld + n0 + y_chunk * 8;
+  Eight<T> y[NY];
+  uint4 x[NX];
+  int e[NX], row[NX];
+
+  auto load_rows = [&](int s0) {
 #pragma unroll
-      for (int t = 0; t < TERMS; ++t) {
-        const float part = top_bits(y);
-        y_tile[t][m * PITCH + k] = (bf16)part;
-        y = isfinite(y) ? y - part : 0.0f;
-      }
-      const int64_t row = s < to ? row_of_slot ? row_of_slot[s] : s : -1;
-      float x = 0.0f;
-      if (row >= 0 && row < g.rows && c0 + m < g.cols) {
-        const int p = exponents[row * g.blocks + (c0 + m) / kBlock];
-        x = (float)q[row * g.blocks * kBlock + c0 + m] * (p == kNotFinite ? NAN : pow2(p));
-      }
-      x_tile[m * PITCH + k] = (bf16)x;
+    for (int i = 0; i < NX; ++i) {
+      const int s = s0 + x_row + i * (THREADS / CX);
+      row[i] = s < it.to ? row_of_slot ? row_of_slot[s] : s : -1;
     }
-    __syncthreads();
-    const int wn = (wave >> 1) * 64, wc = (wave & 1) * 64;
+  };
+  auto load_tile = [&](int s0) {
 #pragma unroll
-    for (int k = 0; k < K; k += 16) {
-      const int kk = k + (lane >> 5) * 8;
-      bf16x8 b[2];
+    for (int i = 0; i < NY; ++i) {
+      const int k = y_row + i * (THREADS / CY);
+      y[i] = load_eight(y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld, s0 + k < it.to ? y_left : 0);
+    }
 #pragma unroll
-      for (int j = 0; j < 2; ++j) b[j] = *reinterpret_cast<bf16x8*>(&x_tile[(wc + j * 32 + (lane & 31)) * PITCH + kk]);
+    for (int i = 0; i < NX; ++i) {
+      x[i] = make_uint4(0, 0, 0, 0);
+      e[i] = 0;
+      if (x_in && row[i] >= 0 && row[i] < g.rows) {
+        const int64_t block = (int64_t)row[i] * g.blocks + (c0 + x_chunk * 16) / kBlock;
+        x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
+        e[i] = exponents[block];
+      }
+    }
+  };
+  auto store_tile = [&](bf16* stage) {
+#pragma unroll
+    for (int i = 0; i < NY; ++i) {
+      const int k = y_row + i * (THREADS / CY);
+      if constexpr (TERMS == 1) {
+        __builtin_memcpy(__builtin_assume_aligned(stage + k * PY + y_chunk * 8, 16), &y[i], 16);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)y[i].v[j];
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 8; j += 2) {
+            const float a = top_bits(v[j]), b = top_bits(v[j + 1]);
+            w[j / 2] = pack(a, b);
+            v[j] = isfinite(a) ? v[j] - a : 0.0f;
+            v[j + 1] = isfinite(b) ? v[j + 1] - b : 0.0f;
+          }
+          *reinterpret_cast<uint4*>(stage + (t * KB + k) * PY + y_chunk * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NX; ++i) {
+      const int k = x_row + i * (THREADS / CX);
+      const float step = e[i] == kNotFinite ? NAN : pow2(e[i]);
+      const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[2 * j] = pack((float)(int8_t)in[j] * step, (float)(int8_t)(in[j] >> 8) * step);
+        w[2 * j + 1] = pack((float)(int8_t)(in[j] >> 16) * step, (float)(int8_t)(in[j] >> 24) * step);
+      }
+      bf16* to = stage + TERMS * KB * PY + k * PX + x_chunk * 16;
+      *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  };
+
+  // A lane's place in a transposing read: lanes 0-15 give four slots of 16
+  // columns and get a column each; lanes 16-31 the next 16 columns, lanes
+  // 32-63 the slots 8 further on.
+  const int read_k = (lane >> 5) * 8 + ((lane & 15) >> 2), read_m = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+  const int wn = (wave / WC) * (BN / WN), wc = (wave % WC) * (BC / WC);
+  auto fragment = [&](const bf16* from, int pitch) {
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 4 * pitch));
+    const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, both);
+  };
+
+  f32x16 acc[FC][FN] = {};
+  if (it.from < it.to) {
+    load_rows(it.from);
+    load_tile(it.from);
+    load_rows(it.from + KB);
+    store_tile(shared);
+  }
+  __syncthreads();
+  int now = 0;
+  for (int s0 = it.from; s0 < it.to; s0 += KB) {
+    const bool more = s0 + KB < it.to;
+    if (more) {
+      load_tile(s0 + KB);
+      load_rows(s0 + 2 * KB);
+    }
+    const bf16* stage = shared + now * STAGE;
+    const bf16* ys = stage + read_k * PY + wn + read_m;
+    const bf16* xs = stage + TERMS * KB * PY + read_k * PX + wc + read_m;
+#pragma unroll
+    for (int k = 0; k < KB; k += 16) {
+      bf16x8 a[FC];
+#pragma unroll
+      for (int i = 0; i < FC; ++i) a[i] = fragment(xs + k * PX + i * 32, PX);
 #pragma unroll
       for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const bf16x8 a = *reinterpret_cast<bf16x8*>(&y_tile[t][(wn + i * 32 + (lane & 31)) * PITCH + kk]);
+        for (int j = 0; j < FN; ++j) {
+          const bf16x8 b = fragment(ys + (t * KB + k) * PY + j * 32, PY);
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b[j], acc[i][j], 0, 0, 0);
+          for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b, acc[i][j], 0, 0, 0);
         }
     }
+    now ^= 1;
+    if (more) store_tile(shared + now * STAGE);
+    __syncthreads();
   }
-  O* out = dw + (int64_t)e * g.n * g.cols;
+
+  auto write = [&](auto* out) {
+    using D = std::remove_reference_t<decltype(*out)>;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < FN; ++j) {
+      const int n = n0 + wn + j * 32 + (lane & 31);
+      if (n >= g.n) continue;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+      for (int i = 0; i < FC; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int n = n0 + (wave >> 1) * 64 + i * 32 + (r >> 2) * 8 + (lane >> 5) * 4 + (r & 3);
-        const int c = c0 + (wave & 1) * 64 + j * 32 + (lane & 31);
-        if (n < g.n && c < g.cols) out[(int64_t)n * g.cols + c] = (O)acc[i][j][r];
-      }
+        for (int r = 0; r < 16; r += 4) {
+          const int c = c0 + wc + i * 32 + r * 2 + (lane >> 5) * 4;
+          D* to = out + (int64_t)n * g.cols + c;
+          if (g.wide_stores) {
+            struct alignas(4 * sizeof(D)) Four {
+              D v[4];
+            } four;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) four.v[h] = (D)acc[i][j][r + h];
+            if (c < g.cols) *reinterpret_cast<Four*>(to) = four;
+          } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+              if (c + h < g.cols) to[h] = (D)acc[i][j][r + h];
+          }
+        }
+    }
+  };
+  if (it.partial < 0)
+    write(dw + (int64_t)it.expert * g.n * g.cols);
+  else
+    write(partials + (int64_t)it.partial * g.n * g.cols);
 }
 
 constexpr int kMaxCols = 1 << 20;
@@ -266,15 +416,25 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
     if (!aligned(d_dy, type_size(type)) || !aligned(d_dw, type_size(out_type)) || !aligned(d_q, 16) ||
         !aligned(d_row_of_slot, 4) || !aligned(d_offsets, 4) || !aligned(d_work, 16))
       return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or d_q or d_work to 16 bytes");
-    const Grad g{experts, n, cols, (int)ceil_div(cols, kBlock), slots, rows, ld_dy};
+    const Grad g{experts, n, cols, (int)ceil_div(cols, kBlock), (int)slots, rows, ld_dy,
+                 cols % 4 == 0 && aligned(d_dw, 4 * type_size(out_type))};
     return launch(what, device, [&] {
       with_type(type, [&](auto t) {
         with_type(out_type, [&](auto o) {
           using T = decltype(t);
           using O = decltype(o);
-          hipLaunchKernelGGL((grad_kernel<T, O>), dim3((unsigned)ceil_div(cols, 128), (unsigned)ceil_div(n, 128), experts),
-                             dim3(256), 0, static_cast<hipStream_t>(hip_stream), g, static_cast<const T*>(d_dy), d_q,
-                             d_exponents, d_row_of_slot, d_offsets, static_cast<O*>(d_dw));
+          constexpr int KB = Terms<T>::value == 1 ? 64 : 32;
+          auto run = [&](auto kernel, int bn, int bc, int threads) {
+            const int lds = 2 * 2 * KB * (Terms<T>::value * (bn + 32) + bc + 32);
+            (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(n, bn) * ceil_div(cols, bc)), experts), dim3(threads), lds,
+                               static_cast<hipStream_t>(hip_stream), g, (const Item*)nullptr, static_cast<const T*>(d_dy),
+                               d_q, d_exponents, d_row_of_slot, d_offsets, static_cast<O*>(d_dw), (float*)nullptr);
+          };
+          if (ceil_div(n, 256) * ceil_div(cols, 256) * experts >= 512)
+            run(grad_kernel<T, O, 256, 256, 2, 4, KB>, 256, 256, 512);
+          else
+            run(grad_kernel<T, O, 128, 128, 2, 2, KB>, 128, 128, 256);
         });
       });
     });
