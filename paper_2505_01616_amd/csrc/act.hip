@@ -172,40 +172,52 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tiles_n = (g.n + BN - 1) / BN;
   const int n0 = (int)(blockIdx.x % tiles_n) * BN, c0 = (int)(blockIdx.x / tiles_n) * BC;
-  const Item it = items ? items[blockIdx.y] : segment(offsets, blockIdx.y, g.slots);
+  Item it = items ? items[blockIdx.y] : segment(offsets, blockIdx.y, g.slots);
   if (it.expert < 0) return;
+  if (g.rows == 0) it.to = it.from;   // no row to read: all count as zeros
 
   // this thread's part of a tile of dy and of saved rows
   const int y_chunk = tid % CY, y_row = tid / CY, x_chunk = tid % CX, x_row = tid / CX;
   const int y_left = g.n - (n0 + y_chunk * 8);
   const bool x_in = c0 + x_chunk * 16 < g.blocks * kBlock;
-  const T* y_at = dy + (int64_t)(it.from + y_row) * g.ld + n0 + y_chunk * 8;
+  // columns beyond the row reach no output: a chunk wholly beyond reads the
+  // row's first one
+  const T* y_at = dy + (int64_t)(it.from + y_row) * g.ld + (y_left > 0 ? n0 + y_chunk * 8 : 0);
+  const int64_t x_at = x_in ? (int64_t)(c0 + x_chunk * 16) / kBlock : 0;
+  // Tiles wholly inside the part are read without conditions; a row's last
+  // chunk then reads into the next row, so not where there is none.
+  const int plain_to = it.to - (it.to == g.slots && g.n % 8 != 0);
+  const bool y_wide = g.n >= 8;
   Eight<T> y[NY];
   uint4 x[NX];
   int e[NX], row[NX];
+  bool held[NX];   // whether x and e are a row's
 
   auto load_rows = [&](int s0) {
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       const int s = s0 + x_row + i * (THREADS / CX);
-      row[i] = s < it.to ? row_of_slot ? row_of_slot[s] : s : -1;
+      row[i] = row_of_slot ? row_of_slot[min(s, it.to - 1)] : s;   // not looked at before the next step
     }
   };
   auto load_tile = [&](int s0) {
+    if (y_wide && s0 + KB <= plain_to) {
 #pragma unroll
-    for (int i = 0; i < NY; ++i) {
-      const int k = y_row + i * (THREADS / CY);
-      y[i] = load_eight(y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld, s0 + k < it.to ? y_left : 0);
+      for (int i = 0; i < NY; ++i)
+        __builtin_memcpy(&y[i], y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld, sizeof(y[i]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NY; ++i) {
+        const int k = y_row + i * (THREADS / CY);
+        y[i] = load_eight(y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld, s0 + k < it.to ? y_left : 0);
+      }
     }
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
-      x[i] = make_uint4(0, 0, 0, 0);
-      e[i] = 0;
-      if (x_in && row[i] >= 0 && row[i] < g.rows) {
-        const int64_t block = (int64_t)row[i] * g.blocks + (c0 + x_chunk * 16) / kBlock;
-        x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
-        e[i] = exponents[block];
-      }
+      held[i] = s0 + x_row + i * (THREADS / CX) < it.to && row[i] >= 0 && row[i] < g.rows;
+      const int64_t block = (held[i] ? (int64_t)row[i] : 0) * g.blocks + x_at;
+      x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
+      e[i] = exponents[block];
     }
   };
   auto store_tile = [&](bf16* stage) {
@@ -235,7 +247,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       const int k = x_row + i * (THREADS / CX);
-      const float step = e[i] == kNotFinite ? NAN : pow2(e[i]);
+      const float step = !held[i] ? 0.0f : e[i] == kNotFinite ? NAN : pow2(e[i]);
       const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
       uint32_t w[8];
 #pragma unroll
