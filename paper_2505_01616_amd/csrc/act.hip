@@ -190,7 +190,8 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
   const bool y_wide = g.n >= 8;
   Eight<T> y[NY];
   uint4 x[NX];
-  int e[NX], row[NX];
+  int row[NX];
+  uint8_t e[NX];   // as loaded: widening it would wait for it
   bool held[NX];   // whether x and e are a row's
 
   auto load_rows = [&](int s0) {
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
       held[i] = s0 + x_row + i * (THREADS / CX) < it.to && row[i] >= 0 && row[i] < g.rows;
       const int64_t block = (held[i] ? (int64_t)row[i] : 0) * g.blocks + x_at;
       x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
-      e[i] = exponents[block];
+      e[i] = (uint8_t)exponents[block];
     }
   };
   auto store_tile = [&](bf16* stage) {
@@ -247,7 +248,8 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       const int k = x_row + i * (THREADS / CX);
-      const float step = !held[i] ? 0.0f : e[i] == kNotFinite ? NAN : pow2(e[i]);
+      const int exponent = (int8_t)e[i];
+      const float step = !held[i] ? 0.0f : exponent == kNotFinite ? NAN : pow2(exponent);
       const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
       uint32_t w[8];
 #pragma unroll
