@@ -741,7 +741,7 @@ netsim_status netsim_act_restore(int32_t device, int64_t rows, int32_t cols, con
  * bfloat16 terms, magnitudes below 2^-126 not kept exactly), x as restored,
  * the sums in 32 bits, rounded once to out_type.  A slot whose row is out of
  * range counts as a row of zeros.  experts: 1 .. 1024; n, cols: 1 .. 2^20;
- * slots <= 2^31-1.  d_work: netsim_act_weight_grad_work_bytes(...) bytes
+ * slots < 2^31-4096.  d_work: netsim_act_weight_grad_work_bytes(...) bytes
  * (-1 for refused sizes), aligned to 16.
  */
 int64_t netsim_act_weight_grad_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,

@@ -100,8 +100,13 @@ struct Grad {
 
 // A part of an expert's slots.  partial < 0: the whole sum, written to dW;
 // otherwise the number of the partial sum in the workspace.
-struct Item {
+struct alignas(16) Item {
   int expert, from, to, partial;
+};
+
+// An expert whose sum is in parts: `parts` partial sums from `first` on.
+struct alignas(16) Join {
+  int expert, first, parts, unused;
 };
 
 template <class T>
@@ -151,6 +156,117 @@ __device__ __forceinline__ Eight<T> load_eight(const T* p, int left) {
 __device__ __forceinline__ Item segment(const int32_t* offsets, int e, int slots) {
   const int a = min(max(offsets[e], 0), slots), b = min(max(offsets[e + 1], a), slots);
   return Item{e, a, b, -1};
+}
+
+// How the sums of a call are cut.  An expert with more than `longest` slots
+// is cut into equal parts of at most that many.
+struct Cut {
+  int tile;          // rows and columns of dW a workgroup computes
+  int64_t longest;
+  int64_t items, partials, joins;   // at most
+  bool planned;      // whether the parts are laid out by plan_kernel
+  int64_t bytes;     // workspace
+};
+
+// Orders the experts' sums by length, longest first, and cuts the long ones:
+// workgroups start in this order, so the last to end are short (a sum over
+// the hot expert of 131,072 routed slots, 25,480 long, started last would
+// add 15%).
+__global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, int step, const int32_t* __restrict__ offsets,
+                                                    Item* __restrict__ items, Join* __restrict__ joins) {
+  __shared__ int length[1024], count[1024], cuts[1024];
+  __shared__ int sums[3][16];
+  const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+  Item it{-1, 0, 0, -1};
+  int parts = 0, each = 0;
+  if (e < g.experts) {
+    it = segment(offsets, e, g.slots);
+    const int64_t n = it.to - it.from;
+    parts = n > cut.longest ? (int)((n + cut.longest - 1) / cut.longest) : 1;
+    each = (int)((n + parts - 1) / parts + step - 1) / step * step;
+    if (parts > 1) parts = (int)((n + each - 1) / each);
+  }
+  length[e] = e < g.experts ? each : -1;
+  __syncthreads();
+  int place = 0;
+  for (int h = 0; h < g.experts; ++h) place += length[h] > each || (length[h] == each && h < e);
+  __syncthreads();
+  // per place in the order: parts, and parts and joins of experts that are cut
+  if (e >= g.experts) place = e;
+  count[place] = parts;
+  cuts[place] = parts > 1 ? parts : 0;
+  __syncthreads();
+  int v[3] = {count[e], cuts[e], cuts[e] ? 1 : 0};
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int w = __shfl_up(v[i], o, 64);
+      if (lane >= o) v[i] += w;
+    }
+    if (lane == 63) sums[i][wave] = v[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    for (int w = 0; w < wave; ++w) v[i] += sums[i][w];
+  int all_items = 0, all_joins = 0;
+  for (int w = 0; w < 16; ++w) {
+    all_items += sums[0][w];
+    all_joins += sums[2][w];
+  }
+  const int my_count = count[e], my_cut = cuts[e];
+  __syncthreads();
+  length[e] = v[0] - my_count;          // first item, partial and join of place e
+  count[e] = v[1] - my_cut;
+  cuts[e] = v[2] - (my_cut ? 1 : 0);
+  __syncthreads();
+  if (e < g.experts) {
+    const int first = length[place], partial = count[place];
+    // offsets that decrease could ask for more than there is room for
+    const bool fits = first + parts <= cut.items && (parts == 1 || partial + parts <= cut.partials);
+    for (int p = 0; p < parts && first + p < cut.items; ++p) {
+      const int64_t from = it.from + (int64_t)p * each, to = min((int64_t)it.to, from + each);
+      items[first + p] = fits ? Item{e, (int)from, (int)to, parts > 1 ? partial + p : -1} : Item{-1, 0, 0, -1};
+    }
+    if (parts > 1 && cuts[place] < cut.joins) joins[cuts[place]] = fits ? Join{e, partial, parts, 0} : Join{-1, 0, 0, 0};
+  }
+  for (int64_t i = all_items + e; i < cut.items; i += 1024) items[i] = Item{-1, 0, 0, -1};
+  for (int64_t i = all_joins + e; i < cut.joins; i += 1024) joins[i] = Join{-1, 0, 0, 0};
+}
+
+// dW of the experts whose sums are in parts; the parts are added in order.
+template <class O>
+__global__ __launch_bounds__(256) void join_kernel(Grad g, const Join* __restrict__ joins,
+                                                   const float* __restrict__ partials, O* __restrict__ dw) {
+  const Join j = joins[blockIdx.y];
+  const int64_t size = (int64_t)g.n * g.cols;
+  const float* from = partials + j.first * size;
+  if (j.parts == 0) return;
+  O* out = dw + j.expert * size;
+  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (g.wide_stores) {
+      for (int p = 0; p < j.parts; ++p) {
+        const float4 v = *reinterpret_cast<const float4*>(from + p * size + i);
+        sum[0] += v.x;
+        sum[1] += v.y;
+        sum[2] += v.z;
+        sum[3] += v.w;
+      }
+      struct alignas(4 * sizeof(O)) Four {
+        O v[4];
+      } four;
+#pragma unroll
+      for (int h = 0; h < 4; ++h) four.v[h] = (O)sum[h];
+      *reinterpret_cast<Four*>(out + i) = four;
+    } else {
+      for (int h = 0; h < 4 && i + h < size; ++h) {
+        for (int p = 0; p < j.parts; ++p) sum[h] += from[p * size + i + h];
+        out[i + h] = (O)sum[h];
+      }
+    }
+  }
 }
 
 template <class T, class O, int BN, int BC, int WN, int WC, int KB>
@@ -346,6 +462,28 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
 }
 
 constexpr int kMaxCols = 1 << 20;
+constexpr int64_t kMaxSlots = 0x7fffffff - 4096;   // a step past the end stays in 32 bits
+
+// How a call's sums are cut, from its sizes alone.
+Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols) {
+  Cut c{};
+  c.tile = ceil_div(n, 256) * ceil_div(cols, 256) * experts >= 512 ? 256 : 128;
+  const int64_t tiles = ceil_div(n, c.tile) * ceil_div(cols, c.tile);   // of one expert
+  // the slots that each of the 256 compute units would have of one tile if
+  // all were busy to the end; parts of a few steps cost more in partial sums
+  // than they save
+  c.longest = ceil_div(slots * tiles, 256);
+  if (c.longest < 256) c.longest = 256;
+  // laying the parts out and joining them takes two more launches, about as
+  // long as 1,024 slots of one tile
+  c.planned = slots > 1024;
+  if (!c.planned) return c;
+  c.items = experts + slots / c.longest;
+  c.joins = slots / c.longest < experts ? slots / c.longest : experts;
+  c.partials = 2 * (slots / c.longest);
+  c.bytes = 16 * (c.items + c.joins) + 4 * c.partials * n * cols;
+  return c;
+}
 
 }  // namespace
 }  // namespace netsim_ops
@@ -403,10 +541,10 @@ extern "C" netsim_status netsim_act_restore(int32_t device, int64_t rows, int32_
 
 extern "C" int64_t netsim_act_weight_grad_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
                                                      int32_t type) {
-  if (experts < 1 || experts > 1024 || slots < 0 || slots > 0x7fffffff || n < 1 || n > kMaxCols || cols < 1 ||
+  if (experts < 1 || experts > 1024 || slots < 0 || slots > kMaxSlots || n < 1 || n > kMaxCols || cols < 1 ||
       cols > kMaxCols || !type_ok(type))
     return -1;
-  return 0;
+  return make_cut(experts, slots, n, cols).bytes;
 }
 
 extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts, int64_t slots, int32_t n,
@@ -420,7 +558,7 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
     if (!type_ok(type) || !type_ok(out_type)) return fail(NETSIM_E_INVALID, what, "bad type");
     const int64_t work = netsim_act_weight_grad_work_bytes(experts, slots, n, cols, type);
     if (work < 0)
-      return fail(NETSIM_E_INVALID, what, "experts must be 1 .. 1024, n and cols 1 .. 2^20, slots 0 .. 2^31-1");
+      return fail(NETSIM_E_INVALID, what, "experts must be 1 .. 1024, n and cols 1 .. 2^20, slots 0 .. 2^31-4097");
     if (rows < 0) return fail(NETSIM_E_INVALID, what, "rows is below 0");
     if (ld_dy < n) return fail(NETSIM_E_INVALID, what, "ld_dy is below n");
     if (!d_offsets || !d_dw || (slots > 0 && !d_dy) || (rows > 0 && (!d_q || !d_exponents)))
@@ -432,23 +570,37 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
       return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or d_q or d_work to 16 bytes");
     const Grad g{experts, n, cols, (int)ceil_div(cols, kBlock), (int)slots, rows, ld_dy,
                  cols % 4 == 0 && aligned(d_dw, 4 * type_size(out_type))};
+    const Cut cut = make_cut(experts, slots, n, cols);
     return launch(what, device, [&] {
       with_type(type, [&](auto t) {
         with_type(out_type, [&](auto o) {
           using T = decltype(t);
           using O = decltype(o);
           constexpr int KB = Terms<T>::value == 1 ? 64 : 32;
-          auto run = [&](auto kernel, int bn, int bc, int threads) {
-            const int lds = 2 * 2 * KB * (Terms<T>::value * (bn + 32) + bc + 32);
+          hipStream_t s = static_cast<hipStream_t>(hip_stream);
+          Item* items = cut.planned ? static_cast<Item*>(d_work) : nullptr;
+          Join* joins = reinterpret_cast<Join*>(items + cut.items);
+          float* partials = reinterpret_cast<float*>(joins + cut.joins);
+          if (cut.planned)
+            hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, g, cut, KB, d_offsets, items, joins);
+          auto run = [&](auto kernel, int threads) {
+            const int lds = 2 * 2 * KB * (Terms<T>::value + 1) * (cut.tile + 32);
             (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(n, bn) * ceil_div(cols, bc)), experts), dim3(threads), lds,
-                               static_cast<hipStream_t>(hip_stream), g, (const Item*)nullptr, static_cast<const T*>(d_dy),
-                               d_q, d_exponents, d_row_of_slot, d_offsets, static_cast<O*>(d_dw), (float*)nullptr);
+            hipLaunchKernelGGL(kernel,
+                               dim3((unsigned)(ceil_div(n, cut.tile) * ceil_div(cols, cut.tile)),
+                                    (unsigned)(cut.planned ? cut.items : experts)),
+                               dim3(threads), lds, s, g, items, static_cast<const T*>(d_dy), d_q, d_exponents,
+                               d_row_of_slot, d_offsets, static_cast<O*>(d_dw), partials);
           };
-          if (ceil_div(n, 256) * ceil_div(cols, 256) * experts >= 512)
-            run(grad_kernel<T, O, 256, 256, 2, 4, KB>, 256, 256, 512);
+          if (cut.tile == 256)
+            run(grad_kernel<T, O, 256, 256, 2, 4, KB>, 512);
           else
-            run(grad_kernel<T, O, 128, 128, 2, 2, KB>, 128, 128, 256);
+            run(grad_kernel<T, O, 128, 128, 2, 2, KB>, 256);
+          if (cut.joins > 0) {
+            const int64_t groups = ceil_div((int64_t)n * cols, 1024);
+            hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)(groups < 4096 ? groups : 4096), (unsigned)cut.joins),
+                               dim3(256), 0, s, g, joins, partials, static_cast<O*>(d_dw));
+          }
         });
       });
     });
