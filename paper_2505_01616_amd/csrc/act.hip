@@ -135,21 +135,51 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
 
-// Eight values of a row of dy; beyond `left` of them zeros.
+// Eight values of a row of dy, as words (values of 16 bits two by two).
 template <class T>
 struct Eight {
-  T v[8];
+  static constexpr int WORDS = 2 * sizeof(T);
+  uint32_t w[WORDS];
 };
+// Reads of 16 bytes at any alignment of the elements.
+typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 template <class T>
-__device__ __forceinline__ Eight<T> load_eight(const T* p, int left) {
+__device__ __forceinline__ Eight<T> load_eight(const T* p) {
+  using Words = std::conditional_t<sizeof(T) == 2, words_at_2, words_at_4>;
   Eight<T> out;
-  if (left >= 8) {
-    __builtin_memcpy(&out, p, sizeof(out));   // at any alignment
-  } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) out.v[i] = i < left ? p[i] : (T)0.0f;
+  for (int i = 0; i < Eight<T>::WORDS; i += 4) {
+    const Words v = reinterpret_cast<const Words*>(p)[i / 4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out.w[i + j] = v[j];
   }
   return out;
+}
+// The same with zeros beyond `left` values.
+template <class T>
+__device__ __forceinline__ Eight<T> load_some(const T* p, int left) {
+  if (left >= 8) return load_eight(p);
+  Eight<T> out;
+#pragma unroll
+  for (int i = 0; i < Eight<T>::WORDS; ++i) out.w[i] = 0;
+  constexpr int PER = 4 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < left) {
+      if constexpr (PER == 1)
+        out.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      else
+        out.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    }
+  return out;
+}
+template <class T>
+__device__ __forceinline__ float value_of(const Eight<T>& v, int i) {
+  if constexpr (sizeof(T) == 4)
+    return __uint_as_float(v.w[i]);
+  else
+    return (float)__builtin_bit_cast(T, (uint16_t)(v.w[i / 2] >> (16 * (i & 1))));
 }
 
 // The bounds of an expert's slots, held to the arrays.
@@ -317,66 +347,54 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
       row[i] = row_of_slot ? row_of_slot[min(s, it.to - 1)] : s;   // not looked at before the next step
     }
   };
-  auto load_tile = [&](int s0) {
-    if (y_wide && s0 + KB <= plain_to) {
-#pragma unroll
-      for (int i = 0; i < NY; ++i)
-        __builtin_memcpy(&y[i], y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld, sizeof(y[i]));
+  auto load_y = [&](int s0, int i, bool plain) {
+    const T* from = y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld;
+    if (plain)
+      y[i] = load_eight(from);
+    else
+      y[i] = load_some(from, s0 + y_row + i * (THREADS / CY) < it.to ? y_left : 0);
+  };
+  auto load_x = [&](int s0, int i) {
+    held[i] = s0 + x_row + i * (THREADS / CX) < it.to && row[i] >= 0 && row[i] < g.rows;
+    const int64_t block = (held[i] ? (int64_t)row[i] : 0) * g.blocks + x_at;
+    x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
+    e[i] = (uint8_t)exponents[block];
+  };
+  auto store_y = [&](bf16* stage, int i) {
+    const int k = y_row + i * (THREADS / CY);
+    if constexpr (TERMS == 1) {
+      *reinterpret_cast<uint4*>(stage + k * PY + y_chunk * 8) = make_uint4(y[i].w[0], y[i].w[1], y[i].w[2], y[i].w[3]);
     } else {
+      float v[8];
 #pragma unroll
-      for (int i = 0; i < NY; ++i) {
-        const int k = y_row + i * (THREADS / CY);
-        y[i] = load_eight(y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld, s0 + k < it.to ? y_left : 0);
+      for (int j = 0; j < 8; ++j) v[j] = value_of(y[i], j);
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const float a = top_bits(v[j]), b = top_bits(v[j + 1]);
+          w[j / 2] = pack(a, b);
+          v[j] = isfinite(a) ? v[j] - a : 0.0f;
+          v[j + 1] = isfinite(b) ? v[j + 1] - b : 0.0f;
+        }
+        *reinterpret_cast<uint4*>(stage + (t * KB + k) * PY + y_chunk * 8) = make_uint4(w[0], w[1], w[2], w[3]);
       }
-    }
-#pragma unroll
-    for (int i = 0; i < NX; ++i) {
-      held[i] = s0 + x_row + i * (THREADS / CX) < it.to && row[i] >= 0 && row[i] < g.rows;
-      const int64_t block = (held[i] ? (int64_t)row[i] : 0) * g.blocks + x_at;
-      x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
-      e[i] = (uint8_t)exponents[block];
     }
   };
-  auto store_tile = [&](bf16* stage) {
+  auto store_x = [&](bf16* stage, int i) {
+    const int k = x_row + i * (THREADS / CX), exponent = (int8_t)e[i];
+    const float step = !held[i] ? 0.0f : exponent == kNotFinite ? NAN : pow2(exponent);
+    const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < NY; ++i) {
-      const int k = y_row + i * (THREADS / CY);
-      if constexpr (TERMS == 1) {
-        __builtin_memcpy(__builtin_assume_aligned(stage + k * PY + y_chunk * 8, 16), &y[i], 16);
-      } else {
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (float)y[i].v[j];
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 8; j += 2) {
-            const float a = top_bits(v[j]), b = top_bits(v[j + 1]);
-            w[j / 2] = pack(a, b);
-            v[j] = isfinite(a) ? v[j] - a : 0.0f;
-            v[j + 1] = isfinite(b) ? v[j + 1] - b : 0.0f;
-          }
-          *reinterpret_cast<uint4*>(stage + (t * KB + k) * PY + y_chunk * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-      }
+    for (int j = 0; j < 4; ++j) {
+      w[2 * j] = pack((float)(int8_t)in[j] * step, (float)(int8_t)(in[j] >> 8) * step);
+      w[2 * j + 1] = pack((float)(int8_t)(in[j] >> 16) * step, (float)(int8_t)(in[j] >> 24) * step);
     }
-#pragma unroll
-    for (int i = 0; i < NX; ++i) {
-      const int k = x_row + i * (THREADS / CX);
-      const int exponent = (int8_t)e[i];
-      const float step = !held[i] ? 0.0f : exponent == kNotFinite ? NAN : pow2(exponent);
-      const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-      uint32_t w[8];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        w[2 * j] = pack((float)(int8_t)in[j] * step, (float)(int8_t)(in[j] >> 8) * step);
-        w[2 * j + 1] = pack((float)(int8_t)(in[j] >> 16) * step, (float)(int8_t)(in[j] >> 24) * step);
-      }
-      bf16* to = stage + TERMS * KB * PY + k * PX + x_chunk * 16;
-      *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-      *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-    }
+    bf16* to = stage + TERMS * KB * PY + k * PX + x_chunk * 16;
+    *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(to + 8) = make_uint4(w[4], w[5], w[6], w[7]);
   };
 
   // A lane's place in a transposing read: lanes 0-15 give four slots of 16
@@ -392,25 +410,21 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
   };
 
   f32x16 acc[FC][FN] = {};
-  if (it.from < it.to) {
-    load_rows(it.from);
-    load_tile(it.from);
-    load_rows(it.from + KB);
-    store_tile(shared);
-  }
-  __syncthreads();
-  int now = 0;
-  for (int s0 = it.from; s0 < it.to; s0 += KB) {
-    const bool more = s0 + KB < it.to;
-    if (more) {
-      load_tile(s0 + KB);
-      load_rows(s0 + 2 * KB);
-    }
-    const bf16* stage = shared + now * STAGE;
+  // A step multiplies the tile at s0 from one half of the shared memory
+  // while the next one goes from registers to the other half and the one
+  // after that from memory to the registers, a slice of each between the
+  // products of every 16 slots: conversions and addresses run in the shadow
+  // of the matrix cores.  PLAIN: all of that lies inside the part.
+  auto step = [&](int s0, const bf16* stage, bf16* next, auto plain_step) {
+    constexpr bool PLAIN = decltype(plain_step)::value;
+    constexpr int SLICES = KB / 16;
+    const bool store = PLAIN || s0 + KB < it.to, load = PLAIN || s0 + 2 * KB < it.to;
+    const bool plain = PLAIN || (y_wide && s0 + 3 * KB <= plain_to);
     const bf16* ys = stage + read_k * PY + wn + read_m;
     const bf16* xs = stage + TERMS * KB * PY + read_k * PX + wc + read_m;
 #pragma unroll
-    for (int k = 0; k < KB; k += 16) {
+    for (int h = 0; h < SLICES; ++h) {
+      const int k = h * 16;
       bf16x8 a[FC];
 #pragma unroll
       for (int i = 0; i < FC; ++i) a[i] = fragment(xs + k * PX + i * 32, PX);
@@ -422,11 +436,45 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
 #pragma unroll
           for (int i = 0; i < FC; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b, acc[i][j], 0, 0, 0);
         }
+#pragma unroll
+      for (int i = h * NY / SLICES; i < (h + 1) * NY / SLICES; ++i) {
+        if (store) store_y(next, i);
+        if (load) load_y(s0 + 2 * KB, i, plain);
+      }
+#pragma unroll
+      for (int i = h * NX / SLICES; i < (h + 1) * NX / SLICES; ++i) {
+        if (store) store_x(next, i);
+        if (load) load_x(s0 + 2 * KB, i);
+      }
     }
-    now ^= 1;
-    if (more) store_tile(shared + now * STAGE);
+    if (load) load_rows(s0 + 3 * KB);
     __syncthreads();
+  };
+
+  if (it.from < it.to) {
+    auto load_all = [&](int s0) {
+      for (int i = 0; i < NY; ++i) load_y(s0, i, y_wide && s0 + KB <= plain_to);
+      for (int i = 0; i < NX; ++i) load_x(s0, i);
+      load_rows(s0 + KB);
+    };
+    load_rows(it.from);
+    load_all(it.from);
+    for (int i = 0; i < NY; ++i) store_y(shared, i);
+    for (int i = 0; i < NX; ++i) store_x(shared, i);
+    if (it.from + KB < it.to) load_all(it.from + KB);
   }
+  __syncthreads();
+  int s0 = it.from;
+  bf16 *stage = shared, *next = shared + STAGE;
+  auto turn = [&] {
+    bf16* was = stage;
+    stage = next;
+    next = was;
+    s0 += KB;
+  };
+  if (y_wide)
+    for (; s0 + 3 * KB <= plain_to; turn()) step(s0, stage, next, std::true_type{});
+  for (; s0 < it.to; turn()) step(s0, stage, next, std::false_type{});
 
   auto write = [&](auto* out) {
     using D = std::remove_reference_t<decltype(*out)>;
