@@ -719,7 +719,7 @@ netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_t top_k, in
  * never overflows.  A block with an infinity or a NaN has e = -128 and
  * restores as NaN.
  *   d_x[rows x ld_x], d_q[rows x 32*blocks] (aligned to 16),
- *   d_exponents[rows x blocks]; cols: 1 .. 2^20.
+ *   d_exponents[rows x blocks]; cols: 1 .. 2^20; rows * blocks <= 2^37.
  */
 netsim_status netsim_act_save(int32_t device, int64_t rows, int32_t cols, int32_t type,
                               const void* d_x, int64_t ld_x, int8_t* d_q, int8_t* d_exponents,

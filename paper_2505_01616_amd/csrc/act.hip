@@ -21,42 +21,124 @@ constexpr int kNotFinite = -128;    // exponent of a block that held an infinity
 // 2^e as a float, -126 <= e <= 127.
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+// Eight values of a row, as words (values of 16 bits two by two).
+template <class T>
+struct Eight {
+  static constexpr int WORDS = 2 * sizeof(T);
+  uint32_t w[WORDS];
+};
+// Reads of 16 bytes at any alignment of the elements.
+typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
+template <class T>
+__device__ __forceinline__ Eight<T> load_eight(const T* p) {
+  using Words = std::conditional_t<sizeof(T) == 2, words_at_2, words_at_4>;
+  Eight<T> out;
+#pragma unroll
+  for (int i = 0; i < Eight<T>::WORDS; i += 4) {
+    const Words v = reinterpret_cast<const Words*>(p)[i / 4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) out.w[i + j] = v[j];
+  }
+  return out;
+}
+// The same with zeros beyond `left` values.
+template <class T>
+__device__ __forceinline__ Eight<T> load_some(const T* p, int left) {
+  if (left >= 8) return load_eight(p);
+  Eight<T> out;
+#pragma unroll
+  for (int i = 0; i < Eight<T>::WORDS; ++i) out.w[i] = 0;
+  constexpr int PER = 4 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i < left) {
+      if constexpr (PER == 1)
+        out.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      else
+        out.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    }
+  return out;
+}
+template <class T>
+__device__ __forceinline__ float value_of(const Eight<T>& v, int i) {
+  if constexpr (sizeof(T) == 4)
+    return __uint_as_float(v.w[i]);
+  else
+    return (float)__builtin_bit_cast(T, (uint16_t)(v.w[i / 2] >> (16 * (i & 1))));
+}
+
+template <class T>
+__device__ __forceinline__ void store_some(T* p, const float (&v)[8], int left) {
+  if (left >= 8) {
+    using Words = std::conditional_t<sizeof(T) == 2, words_at_2, words_at_4>;
+#pragma unroll
+    for (int i = 0; i < Eight<T>::WORDS; i += 4) {
+      Words w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4)
+          w[j] = __float_as_uint(v[i + j]);
+        else
+          w[j] = (uint32_t)__builtin_bit_cast(uint16_t, (T)v[2 * (i + j)]) |
+                 (uint32_t)__builtin_bit_cast(uint16_t, (T)v[2 * (i + j) + 1]) << 16;
+      }
+      reinterpret_cast<Words*>(p)[i / 4] = w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = (T)v[i];
+  }
+}
+
 // ----------------------------------------------------------- save, restore
-// Four lanes per block, eight columns each.
+// Both pass over the data once and are bound by memory.  A lane takes half a
+// block (16 columns: 16 bytes of q, 32 or 64 of x), so a block's largest
+// magnitude is one exchange between neighbours away.
+struct Unit {
+  int64_t row, block;   // row and block, counted over all rows
+  int col;
+};
+// The half block of this thread: number blockIdx.x * 256 + threadIdx.x.
+__device__ __forceinline__ Unit unit_of(int blocks) {
+  const uint32_t per_row = 2 * blocks;
+  const int64_t first = (int64_t)blockIdx.x * 256, row0 = first / per_row;   // the same for the workgroup
+  const uint32_t at = (uint32_t)(first - row0 * per_row) + threadIdx.x, rows = at / per_row;
+  return Unit{row0 + rows, (first + threadIdx.x) >> 1, (int)(at - rows * per_row) * 16};
+}
+
 template <class T>
 __global__ __launch_bounds__(256) void save_kernel(int64_t rows, int cols, int blocks, const T* __restrict__ x,
                                                    int64_t ld, int8_t* __restrict__ q, int8_t* __restrict__ exponents) {
-  const int64_t n = rows * blocks * 4;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t block = i >> 2, row = block / blocks;
-    const int at = (int)(block % blocks), col = at * kBlock + ((int)i & 3) * 8;
-    const T* from = x + row * ld + col;
-    float v[8], top = 0.0f;
-    bool odd = false;
+  const Unit u = unit_of(blocks);
+  if (u.row >= rows) return;
+  const T* from = x + u.row * ld + u.col;
+  float v[16], top = 0.0f;
+  bool odd = false;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const Eight<T> in = load_some(from + 8 * h, cols - u.col - 8 * h);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      v[j] = col + j < cols ? (float)from[j] : 0.0f;
-      odd |= !isfinite(v[j]);
-      top = fmaxf(top, fabsf(v[j]));
+      v[8 * h + j] = value_of(in, j);
+      odd |= !isfinite(v[8 * h + j]);
+      top = fmaxf(top, fabsf(v[8 * h + j]));
     }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      top = fmaxf(top, __shfl_xor(top, o, 64));
-      odd |= __shfl_xor((int)odd, o, 64) != 0;
-    }
-    int e = (int)(__float_as_uint(top) >> 23) - 127 - 6;
-    e = e < -126 ? -126 : e;
-    // 2^-e as two factors: -e reaches 126, and a subnormal needs no more
-    const float up = pow2(-e);
-    uint32_t word[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float r = odd ? 0.0f : fminf(fmaxf(rintf(v[j] * up), -127.0f), 127.0f);
-      word[j >> 2] |= (uint32_t)(uint8_t)(int8_t)(int)r << (8 * (j & 3));
-    }
-    *reinterpret_cast<uint2*>(q + i * 8) = make_uint2(word[0], word[1]);
-    if ((i & 3) == 0) exponents[block] = odd ? (int8_t)kNotFinite : (int8_t)e;
   }
+  top = fmaxf(top, __shfl_xor(top, 1, 64));   // the other half: the next thread, of the same row
+  odd |= __shfl_xor((int)odd, 1, 64) != 0;
+  int e = (int)(__float_as_uint(top) >> 23) - 127 - 6;
+  e = e < -126 ? -126 : e;
+  const float up = pow2(-e);
+  uint32_t word[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const float r = odd ? 0.0f : fminf(fmaxf(rintf(v[j] * up), -127.0f), 127.0f);
+    word[j >> 2] |= (uint32_t)(uint8_t)(int8_t)(int)r << (8 * (j & 3));
+  }
+  *reinterpret_cast<uint4*>(q + u.block * kBlock + (u.col & 16)) = make_uint4(word[0], word[1], word[2], word[3]);
+  if ((u.col & 16) == 0) exponents[u.block] = odd ? (int8_t)kNotFinite : (int8_t)e;
 }
 
 template <class T>
@@ -64,16 +146,19 @@ __global__ __launch_bounds__(256) void restore_kernel(int64_t rows, int cols, in
                                                       const int8_t* __restrict__ q,
                                                       const int8_t* __restrict__ exponents, T* __restrict__ x,
                                                       int64_t ld) {
-  const int64_t n = rows * blocks * 4;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t block = i >> 2, row = block / blocks;
-    const int at = (int)(block % blocks), col = at * kBlock + ((int)i & 3) * 8;
-    const int e = exponents[block];
-    const float step = e == kNotFinite ? NAN : pow2(e);
-    T* to = x + row * ld + col;
+  const Unit u = unit_of(blocks);
+  if (u.row >= rows) return;
+  const int e = exponents[u.block];
+  const float step = e == kNotFinite ? NAN : pow2(e);
+  const uint4 in = *reinterpret_cast<const uint4*>(q + u.block * kBlock + (u.col & 16));
+  const uint32_t word[4] = {in.x, in.y, in.z, in.w};
+  T* to = x + u.row * ld + u.col;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (col + j < cols) to[j] = (T)((float)q[i * 8 + j] * step);
+  for (int h = 0; h < 2; ++h) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)(word[2 * h + (j >> 2)] >> (8 * (j & 3))) * step;
+    store_some(to + 8 * h, v, cols - u.col - 8 * h);
   }
 }
 
@@ -133,53 +218,6 @@ __device__ __forceinline__ float top_bits(float y) {
 // Two floats of at most 8 significant bits as bfloat16, a in the low half.
 __device__ __forceinline__ uint32_t pack(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-}
-
-// Eight values of a row of dy, as words (values of 16 bits two by two).
-template <class T>
-struct Eight {
-  static constexpr int WORDS = 2 * sizeof(T);
-  uint32_t w[WORDS];
-};
-// Reads of 16 bytes at any alignment of the elements.
-typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
-template <class T>
-__device__ __forceinline__ Eight<T> load_eight(const T* p) {
-  using Words = std::conditional_t<sizeof(T) == 2, words_at_2, words_at_4>;
-  Eight<T> out;
-#pragma unroll
-  for (int i = 0; i < Eight<T>::WORDS; i += 4) {
-    const Words v = reinterpret_cast<const Words*>(p)[i / 4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) out.w[i + j] = v[j];
-  }
-  return out;
-}
-// The same with zeros beyond `left` values.
-template <class T>
-__device__ __forceinline__ Eight<T> load_some(const T* p, int left) {
-  if (left >= 8) return load_eight(p);
-  Eight<T> out;
-#pragma unroll
-  for (int i = 0; i < Eight<T>::WORDS; ++i) out.w[i] = 0;
-  constexpr int PER = 4 / sizeof(T);
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < left) {
-      if constexpr (PER == 1)
-        out.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-      else
-        out.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-    }
-  return out;
-}
-template <class T>
-__device__ __forceinline__ float value_of(const Eight<T>& v, int i) {
-  if constexpr (sizeof(T) == 4)
-    return __uint_as_float(v.w[i]);
-  else
-    return (float)__builtin_bit_cast(T, (uint16_t)(v.w[i / 2] >> (16 * (i & 1))));
 }
 
 // The bounds of an expert's slots, held to the arrays.
@@ -550,11 +588,12 @@ extern "C" netsim_status netsim_act_save(int32_t device, int64_t rows, int32_t c
     if (!aligned(d_x, type_size(type)) || !aligned(d_q, 16))
       return fail(NETSIM_E_INVALID, what, "d_x is not aligned to its type, or d_q to 16 bytes");
     const int blocks = (int)ceil_div(cols, kBlock);
+    if (rows > ((int64_t)1 << 37) / blocks) return fail(NETSIM_E_INVALID, what, "more than 2^37 blocks of 32 columns");
     return launch(what, device, [&] {
-      const int64_t groups = ceil_div(rows * blocks * 4, 256);
+      const int64_t groups = ceil_div(rows * blocks, 128);
       with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(save_kernel<T>, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0,
+        hipLaunchKernelGGL(save_kernel<T>, dim3((unsigned)groups), dim3(256), 0,
                            static_cast<hipStream_t>(hip_stream), rows, cols, blocks, static_cast<const T*>(d_x), ld_x,
                            d_q, d_exponents);
       });
@@ -575,11 +614,12 @@ extern "C" netsim_status netsim_act_restore(int32_t device, int64_t rows, int32_
     if (!aligned(d_x, type_size(type)) || !aligned(d_q, 16))
       return fail(NETSIM_E_INVALID, what, "d_x is not aligned to its type, or d_q to 16 bytes");
     const int blocks = (int)ceil_div(cols, kBlock);
+    if (rows > ((int64_t)1 << 37) / blocks) return fail(NETSIM_E_INVALID, what, "more than 2^37 blocks of 32 columns");
     return launch(what, device, [&] {
-      const int64_t groups = ceil_div(rows * blocks * 4, 256);
+      const int64_t groups = ceil_div(rows * blocks, 128);
       with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(restore_kernel<T>, dim3((unsigned)(groups < 8192 ? groups : 8192)), dim3(256), 0,
+        hipLaunchKernelGGL(restore_kernel<T>, dim3((unsigned)groups), dim3(256), 0,
                            static_cast<hipStream_t>(hip_stream), rows, cols, blocks, d_q, d_exponents,
                            static_cast<T*>(d_x), ld_x);
       });

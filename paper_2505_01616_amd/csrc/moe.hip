@@ -3,6 +3,8 @@
 // rank sends to every other one (the matrix of netsim_add_all_to_all).
 #include <math.h>
 
+#include <type_traits>
+
 #include "ops.h"
 
 namespace netsim_ops {
@@ -11,19 +13,73 @@ namespace {
 constexpr int kMaxExperts = 1024, kMaxTopK = 32, kMaxRanks = 1024;
 constexpr float kNone = -INFINITY;
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+// ------------------------------------------------ exchanges between L lanes
+// L = 8, 16 or 64 neighbouring lanes hold a row.  Exchanges inside 16 lanes
+// are register moves; over a whole wave the last lane holds the result and
+// is read from there.  Every lane ends up with the result, and sums are
+// formed in the same order everywhere.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int old, int v) {
+  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float old, float v) {
+  return __int_as_float(moved<CTRL, ROWS>(__float_as_int(old), __float_as_int(v)));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double old, double v) {
+  const long long o = __double_as_longlong(old), b = __double_as_longlong(v);
+  const int lo = moved<CTRL, ROWS>((int)o, (int)b), hi = moved<CTRL, ROWS>((int)(o >> 32), (int)(b >> 32));
+  return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
+}
+__device__ __forceinline__ float last_lane(float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63)); }
+__device__ __forceinline__ double last_lane(double v) {
+  const long long b = __double_as_longlong(v);
+  const int lo = __builtin_amdgcn_readlane((int)b, 63), hi = __builtin_amdgcn_readlane((int)(b >> 32), 63);
+  return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
+}
+// old(v): what a lane without a partner combines with.
+template <int L, class V, class Old, class Op>
+__device__ __forceinline__ V over(V v, Old old, Op op) {
+  v = op(v, moved<0xB1, 0xF>(old(v), v));   // 1 lane apart
+  v = op(v, moved<0x4E, 0xF>(old(v), v));   // 2 apart
+  v = op(v, moved<0x141, 0xF>(old(v), v));  // mirrored in 8 lanes
+  if constexpr (L > 8) v = op(v, moved<0x140, 0xF>(old(v), v));  // mirrored in 16
+  if constexpr (L > 16) {
+    v = op(v, moved<0x142, 0xA>(old(v), v));  // the last lane of the 16 before
+    v = op(v, moved<0x143, 0xC>(old(v), v));  // lane 31
+    v = last_lane(v);
+  }
   return v;
 }
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+template <int L>
+__device__ __forceinline__ float max_over(float v) {
+  return over<L>(v, [](float x) { return x; }, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ __forceinline__ float sum_over(float v) {
+  return over<L>(v, [](float) { return 0.0f; }, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ bool any_over(bool v) {
+  const uint64_t set = __ballot(v);
+  if constexpr (L == 64)
+    return set != 0;
+  else
+    return (set >> (threadIdx.x & 63 & ~(L - 1)) & ((1ull << L) - 1)) != 0;
 }
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+// exp(x) to about two units in the last place: 2^(x log2 e) with the part of
+// the product that 32 bits cut off put back.
+__device__ __forceinline__ float exp_of(float x) {
+  constexpr float LOG2E = 1.44269504088896340736f, LOG2E_LOW = 1.925963033500e-8f, LN2 = 0.69314718055994530942f;
+  const float hi = x * LOG2E;
+  const float low = __builtin_fmaf(x, LOG2E_LOW, __builtin_fmaf(x, LOG2E, -hi));
+  const float p = __builtin_amdgcn_exp2f(hi);
+  // beyond the range hi alone decides (0 or infinity); low may not be finite there
+  return fabsf(hi) < 150.0f ? __builtin_fmaf(p, low * LN2, p) : p;
+}
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + exp_of(-x)); }
 
 struct Router {
   int experts, top_k, groups, kept, best;
@@ -31,63 +87,132 @@ struct Router {
   float scale;
 };
 
+// N values of a row in each of L lanes, in vectors of V neighbouring ones:
+// value i of lane j is element (i / V * L + j) * V + i % V.
+template <class T, int L, int N>
+struct Row {
+  static constexpr int V = N < (int)(16 / sizeof(T)) ? N : (int)(16 / sizeof(T));
+  static __device__ __forceinline__ int element(int i, int j) { return (i / V * L + j) * V + i % V; }
+  // wide: every vector lies wholly inside or outside the row, and is aligned
+  static __device__ __forceinline__ void load(const T* row, int n, int j, bool wide, float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += V) {
+      const int e = element(i, j);
+      struct alignas(V * sizeof(T)) Vector {
+        T v[V];
+      } in;
+      if (wide) {
+        if (e < n) in = *reinterpret_cast<const Vector*>(row + e);
+      } else {
+#pragma unroll
+        for (int h = 0; h < V; ++h)
+          if (e + h < n) in.v[h] = row[e + h];
+      }
+#pragma unroll
+      for (int h = 0; h < V; ++h) x[i + h] = e + h < n ? (float)in.v[h] : kNone;
+    }
+  }
+};
+
 // ---------------------------------------------------------------- routing
-// A wave per row.  A lane holds the logits lane, lane + 64, ... of its row;
-// every choice is the largest value of the wave, the lowest expert among
-// equal ones, and is then taken out.
-template <class T>
+// L lanes per row, N logits each, in registers; one pass over the logits.
+//
+// A choice value and its expert are one 64-bit float: a 32-bit value leaves
+// the low 29 bits of a 64-bit one free, and the low 10 get the expert's
+// number so that of equal values the lowest expert is the largest key.  A
+// compare-and-exchange is then a minimum and a maximum.  Each lane sorts its
+// keys; the largest of a row is the largest of the lanes' first ones, and
+// the lane that gave it moves on to its next.
+//
+// Bound by instructions per row: few lanes per row mean few exchanges (8
+// lanes: three per choice, eight rows at once), many lanes mean short sorts
+// and enough waves where rows are few.
+constexpr double kNoKey = -1.0e300;
+
+__device__ __forceinline__ double key_of(float value, int expert) {
+  const double wide = value == INFINITY ? 1.0e200 : (double)(value + 0.0f);   // + 0: -0 is 0
+  const long long b = __double_as_longlong(wide) & ~0x1FFFFFFFll;
+  return value == kNone ? kNoKey : __longlong_as_double(b | (b < 0 ? expert : kMaxExperts - 1 - expert));
+}
+__device__ __forceinline__ int expert_of(double key) {
+  const long long b = __double_as_longlong(key);
+  const int low = (int)b & (kMaxExperts - 1);
+  return key == kNoKey ? -1 : b < 0 ? low : kMaxExperts - 1 - low;
+}
+// Keys are never NaN.
+__device__ __forceinline__ double larger(double a, double b) { return a > b ? a : b; }
+__device__ __forceinline__ double smaller(double a, double b) { return a > b ? b : a; }
+
+// Descending order by odd-even merges (Batcher 1968).
+template <int N>
+__device__ __forceinline__ void sort_keys(double (&k)[N]) {
+#pragma unroll
+  for (int p = 1; p < N; p *= 2)
+#pragma unroll
+    for (int h = p; h >= 1; h /= 2)
+#pragma unroll
+      for (int j = h % p; j + h < N; j += 2 * h)
+#pragma unroll
+        for (int i = 0; i < h; ++i)
+          if (i + j + h < N && (i + j) / (2 * p) == (i + j + h) / (2 * p)) {
+            const double a = k[i + j], b = k[i + j + h];
+            k[i + j] = larger(a, b);
+            k[i + j + h] = smaller(a, b);
+          }
+}
+
+template <class T, int L, int N>
 __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, const T* __restrict__ logits, int64_t ld,
-                                                    const float* __restrict__ bias, int32_t* __restrict__ experts,
-                                                    float* __restrict__ weights) {
+                                                    bool wide, const float* __restrict__ bias,
+                                                    int32_t* __restrict__ experts, float* __restrict__ weights) {
   extern __shared__ float shared[];
-  constexpr int N = kMaxExperts / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-  if (row >= tokens) return;
+  using R = Row<T, L, N>;
+  constexpr int SLOTS = (kMaxTopK + L - 1) / L;
+  const int j = threadIdx.x & (L - 1);
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
+  const int64_t row = at < tokens ? at : tokens - 1;   // lanes beyond repeat the last row and write nothing
   const T* x_row = logits + row * ld;
   const bool by_score = bias || r.best > 1;  // else the logits give the same order
 
   float x[N], top = kNone;
+  R::load(x_row, r.experts, j, wide, x);
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int e = i * 64 + lane;
-    x[i] = e < r.experts ? (float)x_row[e] : kNone;
     bad |= isnan(x[i]) || (r.softmax && x[i] == INFINITY);
     top = fmaxf(top, x[i]);
   }
-  top = wave_max(top);
-  const float base = top == kNone ? 0.0f : top;
-  float z = 1.0f;
+  float base = 0.0f, z = 1.0f;
   if (r.softmax && (by_score || !r.renorm)) {
+    top = max_over<L>(top);
+    base = top == kNone ? 0.0f : top;
     z = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) z += expf(x[i] - base);
-    z = wave_sum(z);
+    for (int i = 0; i < N; ++i) z += exp_of(x[i] - base);
+    z = sum_over<L>(z);
   }
-
-  float c[N];
+  if (by_score) {
+    const float inverse = 1.0f / z;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int e = i * 64 + lane;
-    c[i] = x[i];
-    if (by_score && x[i] > kNone) {
-      c[i] = r.softmax ? expf(x[i] - base) / z : sigmoid(x[i]);
-      if (bias) c[i] += bias[e];
-      bad |= isnan(c[i]);
+    for (int i = 0; i < N; ++i) {
+      if (x[i] == kNone) continue;
+      x[i] = r.softmax ? exp_of(x[i] - base) * inverse : sigmoid(x[i]);
+      if (bias) x[i] += bias[R::element(i, j)];
+      bad |= isnan(x[i]);
     }
   }
 
   if (r.groups > 1) {
-    float* row_c = shared + wave * (r.experts + 2 * r.groups);
-    float* score = row_c + r.experts;
+    // the row's choice values in shared memory; a lane takes whole groups
+    const int size = r.experts / r.groups, pitch = r.experts + 1;
+    float* row_c = shared + (threadIdx.x / L) * (pitch + 2 * r.groups);
+    float* score = row_c + pitch;
     float* keep = score + r.groups;
-    const int size = r.experts / r.groups;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (i * 64 + lane < r.experts) row_c[i * 64 + lane] = c[i];
+      if (R::element(i, j) < r.experts) row_c[R::element(i, j)] = x[i];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int g = lane; g < r.groups; g += 64) {
+    for (int g = j; g < r.groups; g += L) {
       float a = kNone, b = kNone;  // the two largest
       for (int i = 0; i < size; ++i) {
         const float v = row_c[g * size + i];
@@ -97,141 +222,252 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
       score[g] = r.best > 1 && b > kNone ? a + b : a;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int g = lane; g < r.groups; g += 64) {
+    for (int g = j; g < r.groups; g += L) {
       const float mine = score[g];
       int before = 0;
       for (int h = 0; h < r.groups; ++h) before += score[h] > mine || (score[h] == mine && h < g);
       keep[g] = before < r.kept ? 1.0f : 0.0f;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const float per = 1.0f / size;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = i * 64 + lane;
-      if (e < r.experts && keep[e / size] == 0.0f) c[i] = kNone;
+      const int e = R::element(i, j);
+      // (e + 1/2) / size in 32 bits is never off by half a step below 2^10
+      if (e < r.experts && keep[(int)((e + 0.5f) * per)] == 0.0f) x[i] = kNone;
     }
   }
 
-  const bool row_bad = __any(bad);
-  int mine = -1;  // lane j keeps the j-th choice
-  for (int j = 0; j < r.top_k; ++j) {
-    float v = kNone;
-    int at = kMaxExperts;
+  const bool row_bad = any_over<L>(bad);
+  double k[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (c[i] > v) {
-        v = c[i];
-        at = i * 64 + lane;
-      }
+  for (int i = 0; i < N; ++i) k[i] = key_of(row_bad ? kNone : x[i], R::element(i, j) & (kMaxExperts - 1));
+  sort_keys(k);
+  int mine[SLOTS];  // lane j keeps the choices j, j + L, ...
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float w = __shfl_xor(v, o, 64);
-      const int b = __shfl_xor(at, o, 64);
-      if (w > v || (w == v && b < at)) {
-        v = w;
-        at = b;
-      }
-    }
-    if (v == kNone || row_bad) break;
-    if (lane == j) mine = at;
+  for (int s = 0; s < SLOTS; ++s) mine[s] = -1;
+  for (int c = 0; c < r.top_k; ++c) {
+    const double best = over<L>(k[0], [](double v) { return v; }, larger);
+    const bool taken = k[0] == best;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i * 64 + lane == at) c[i] = kNone;
+    for (int i = 0; i + 1 < N; ++i) k[i] = taken ? k[i + 1] : k[i];
+    k[N - 1] = taken ? kNoKey : k[N - 1];
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s)
+      if (c == s * L + j) mine[s] = expert_of(best);
   }
 
-  float w = 0.0f;
-  if (mine >= 0) {
-    const float l = (float)x_row[mine];
-    w = r.softmax ? expf(l - base) : sigmoid(l);
+  float l[SLOTS], w[SLOTS], sum = 0.0f, most = kNone;
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    l[s] = mine[s] >= 0 ? (float)x_row[mine[s]] : kNone;
+    most = fmaxf(most, l[s]);
   }
-  if (r.renorm) {
-    if (r.softmax) {  // from the largest chosen logit: the sum is 1 or more
-      const float l = mine >= 0 ? (float)x_row[mine] : kNone;
-      const float m = wave_max(l);
-      w = mine >= 0 ? expf(l - m) : 0.0f;
+  // renormalised softmax from the largest chosen logit: the sum is 1 or more
+  if (r.softmax && r.renorm) base = max_over<L>(most);
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    w[s] = mine[s] < 0 ? 0.0f : r.softmax ? exp_of(l[s] - base) : sigmoid(l[s]);
+    sum += w[s];
+  }
+  if (r.renorm) z = sum_over<L>(sum);
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s)
+    if (at < tokens && s * L + j < r.top_k) {
+      const int64_t to = row * r.top_k + s * L + j;
+      experts[to] = mine[s];
+      weights[to] = row_bad ? NAN : mine[s] >= 0 && z > 0.0f ? w[s] / z * r.scale : 0.0f;
     }
-    const float sum = wave_sum(w);
-    w = sum > 0.0f ? w / sum : 0.0f;
-  } else if (r.softmax) {
-    w /= z;
-  }
-  if (lane < r.top_k) {
-    experts[row * r.top_k + lane] = mine;
-    weights[row * r.top_k + lane] = row_bad ? NAN : mine >= 0 ? w * r.scale : 0.0f;
-  }
 }
 
 // --------------------------------------------------------- routing's gradient
 // With p_j the chosen scores and w_j = scale p_j / Z (Z their sum, or 1):
 //   dp_j = scale (dw_j - sum_i dw_i p_i / Z) / Z   (without the sum if Z = 1)
 //   sigmoid: dl_j = dp_j p_j (1 - p_j);   softmax: dl_e = p_e (dp_e - sum_j dp_j p_j)
-// A wave per row; lane j holds choice j.
+// With renormalised scores softmax's last sum is 0, so there, and for
+// sigmoid, only the chosen logits matter: only they are read, and the rest
+// of a row is zeros.
+struct Chosen {
+  int at;         // the expert, -1 for none
+  float l, dw;    // its logit, and its weight's gradient times scale
+};
 template <class T>
-__global__ __launch_bounds__(256) void route_back_kernel(Router r, int64_t tokens, const T* __restrict__ logits,
-                                                         int64_t ld, const int32_t* __restrict__ experts,
-                                                         const float* __restrict__ dweights, T* __restrict__ dlogits,
-                                                         int64_t ldd) {
-  extern __shared__ float shared[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t row = (int64_t)blockIdx.x * 4 + wave;
-  if (row >= tokens) return;
-  const T* x_row = logits + row * ld;
-  T* out = dlogits + row * ldd;
-  float* d = shared + wave * r.experts;
-  for (int e = lane; e < r.experts; e += 64) d[e] = 0.0f;
+__device__ __forceinline__ Chosen choice(const Router& r, const T* x_row, const int32_t* experts, const float* dweights,
+                                         int64_t row, int c) {
+  Chosen out{-1, kNone, 0.0f};
+  if (c < r.top_k) {
+    const int e = experts[row * r.top_k + c];
+    if (e >= 0 && e < r.experts) out = Chosen{e, (float)x_row[e], dweights[row * r.top_k + c] * r.scale};
+  }
+  return out;
+}
 
-  int at = -1;
-  float l = kNone, dw = 0.0f;
-  if (lane < r.top_k) {
-    at = experts[row * r.top_k + lane];
-    if (at >= r.experts) at = -1;
-    if (at >= 0) {
-      l = (float)x_row[at];
-      dw = dweights[row * r.top_k + lane] * r.scale;
-    }
-  }
-  const bool any = __any(at >= 0);
-  float base = 0.0f, z = 1.0f;
-  if (r.softmax && any) {
-    if (r.renorm) {  // only the chosen scores' ratios matter
-      base = wave_max(l);
-    } else {
-      float top = kNone;
-      for (int e = lane; e < r.experts; e += 64) top = fmaxf(top, (float)x_row[e]);
-      base = wave_max(top);
-      z = 0.0f;
-      for (int e = lane; e < r.experts; e += 64) z += expf((float)x_row[e] - base);
-      z = wave_sum(z);
-    }
-  }
+// Only the chosen logits: K lanes per row, K >= top_k, 64 / K rows per wave.
+// Gradients are scattered into a row of shared memory, from where the wave
+// writes its rows as vectors.
+template <class T, int K>
+__global__ __launch_bounds__(256) void route_back_chosen_kernel(Router r, int64_t tokens, const T* __restrict__ logits,
+                                                                int64_t ld, const int32_t* __restrict__ experts,
+                                                                const float* __restrict__ dweights,
+                                                                T* __restrict__ dlogits, int64_t ldd, bool wide) {
+  extern __shared__ float shared[];
+  constexpr int ROWS = 64 / K, V = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = lane & (K - 1);
+  const int pitch = (r.experts + V - 1) / V * V;
+  float* mine = shared + wave * ROWS * pitch;
+  for (int i = lane * 4; i < ROWS * pitch; i += 256) *reinterpret_cast<float4*>(mine + i) = make_float4(0, 0, 0, 0);
+  const int64_t first = ((int64_t)blockIdx.x * 4 + wave) * ROWS, row = first + lane / K;
+  if (first >= tokens) return;
+  Chosen c{-1, kNone, 0.0f};
+  if (row < tokens) c = choice(r, logits + row * ld, experts, dweights, row, j);
   float p = 0.0f, slope = 1.0f;
-  if (at >= 0) {
-    if (r.softmax) {
-      p = expf(l - base) / z;
+  // lanes exchange over 8, 16 or 64: rows of 32 lanes take two steps more
+  auto total = [](float v) {
+    if constexpr (K == 32) {
+      v = sum_over<16>(v);
+      return v + __shfl_xor(v, 16, 64);
     } else {
-      p = sigmoid(l);
-      slope = sigmoid(-l);  // 1 - p without its cancellation
+      return sum_over<K>(v);
+    }
+  };
+  if (r.softmax) {
+    float base = c.l;
+    if constexpr (K == 32) {
+      base = max_over<16>(base);
+      base = fmaxf(base, __shfl_xor(base, 16, 64));
+    } else {
+      base = max_over<K>(base);
+    }
+    if (c.at >= 0) p = exp_of(c.l - base);
+  } else if (c.at >= 0) {
+    p = sigmoid(c.l);
+    slope = sigmoid(-c.l);  // 1 - p without its cancellation
+  }
+  float dl = c.dw * p * slope;
+  if (r.renorm) {
+    const float sum = total(p), w = sum > 0.0f ? p / sum : 0.0f;
+    dl = w * (c.dw - total(c.dw * w)) * slope;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (c.at >= 0) mine[lane / K * pitch + c.at] = dl;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int rows = (int)(tokens - first < ROWS ? tokens - first : ROWS);
+  if (wide) {
+    const int vectors = r.experts / V;
+    for (int i = lane; i < rows * vectors; i += 64) {
+      const int line = i / vectors, e = (i - line * vectors) * V;
+      struct alignas(16) Vector {
+        T v[V];
+      } out;
+#pragma unroll
+      for (int h = 0; h < V; ++h) out.v[h] = (T)mine[line * pitch + e + h];
+      *reinterpret_cast<Vector*>(dlogits + (first + line) * ldd + e) = out;
+    }
+  } else {
+    for (int line = 0; line < rows; ++line)
+      for (int e = lane; e < r.experts; e += 64) dlogits[(first + line) * ldd + e] = (T)mine[line * pitch + e];
+  }
+}
+
+// Softmax without renormalisation: every logit of a row has a gradient.  The
+// row in registers as for routing; the chosen ones' dp through shared memory.
+template <class T, int L, int N>
+__global__ __launch_bounds__(256) void route_back_kernel(Router r, int64_t tokens, const T* __restrict__ logits,
+                                                         int64_t ld, bool wide, const int32_t* __restrict__ experts,
+                                                         const float* __restrict__ dweights, T* __restrict__ dlogits,
+                                                         int64_t ldd, bool wide_out) {
+  using R = Row<T, L, N>;
+  constexpr int SLOTS = (kMaxTopK + L - 1) / L;
+  __shared__ float shared[256 * N + 256 / L];
+  const int j = threadIdx.x & (L - 1);
+  const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L, row = id < tokens ? id : tokens - 1;
+  const T* x_row = logits + row * ld;
+  float* d = shared + threadIdx.x / L * (L * N + 1);
+  float x[N], top = kNone;
+  R::load(x_row, r.experts, j, wide, x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    d[R::element(i, j)] = 0.0f;
+    top = fmaxf(top, x[i]);
+  }
+  top = max_over<L>(top);
+  const float base = top == kNone ? 0.0f : top;
+  float z = 0.0f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    x[i] = exp_of(x[i] - base);
+    z += x[i];
+  }
+  z = sum_over<L>(z);
+  const float inverse = z > 0.0f ? 1.0f / z : 0.0f;
+  float mean = 0.0f;
+  bool any = false;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int s = 0; s < SLOTS; ++s) {
+    const Chosen c = choice(r, x_row, experts, dweights, row, s * L + j);
+    if (c.at >= 0) {
+      d[c.at] = c.dw;
+      mean += c.dw * exp_of(c.l - base) * inverse;
+      any = true;
     }
   }
-  float dl;
-  if (r.renorm) {
-    const float sum = wave_sum(p), w = sum > 0.0f ? p / sum : 0.0f;
-    const float mean = wave_sum(dw * w);
-    dl = w * (dw - mean) * slope;  // softmax: the chosen scores alone
-  } else if (!r.softmax) {
-    dl = dw * p * slope;
-  } else {
-    dl = dw;
-  }
+  mean = sum_over<L>(mean);
+  any = any_over<L>(any);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (at >= 0) d[at] = dl;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (r.softmax && !r.renorm) {
-    const float mean = wave_sum(dw * p);
-    for (int e = lane; e < r.experts; e += 64)
-      out[e] = any ? (T)(expf((float)x_row[e] - base) / z * (d[e] - mean)) : (T)0.0f;
-  } else {
-    for (int e = lane; e < r.experts; e += 64) out[e] = (T)d[e];
+  if (id >= tokens) return;
+  T* out = dlogits + row * ldd;
+#pragma unroll
+  for (int i = 0; i < N; i += R::V) {
+    const int e = R::element(i, j);
+    struct alignas(R::V * sizeof(T)) Vector {
+      T v[R::V];
+    } v;
+#pragma unroll
+    for (int h = 0; h < R::V; ++h) v.v[h] = any ? (T)(x[i + h] * inverse * (d[e + h] - mean)) : (T)0.0f;
+    if (wide_out) {
+      if (e < r.experts) *reinterpret_cast<Vector*>(out + e) = v;
+    } else {
+#pragma unroll
+      for (int h = 0; h < R::V; ++h)
+        if (e + h < r.experts) out[e + h] = v.v[h];
+    }
   }
+}
+
+// Calls f with the lanes per row and the values per lane as constants.
+// Fewer lanes per row exchange less per row, as long as a lane holds at most
+// 16 values and the rows still make 4,096 waves (4 for each of the 1,024
+// SIMDs): MEASURED.
+template <class F>
+void with_shape(int64_t tokens, int experts, F&& f) {
+  int lanes = 64;
+  for (int fewer : {16, 8})
+    if (experts <= fewer * 16 && tokens * fewer >= 64 * 4096) lanes = fewer;
+  auto values = [&](auto l) {
+    constexpr int L = decltype(l)::value;
+    const int n = (experts + L - 1) / L;
+    if (n <= 1)
+      f(l, std::integral_constant<int, 1>{});
+    else if (n <= 4)
+      f(l, std::integral_constant<int, 4>{});
+    else if (n <= 8)
+      f(l, std::integral_constant<int, 8>{});
+    else
+      f(l, std::integral_constant<int, 16>{});
+  };
+  if (lanes == 8)
+    values(std::integral_constant<int, 8>{});
+  else if (lanes == 16)
+    values(std::integral_constant<int, 16>{});
+  else
+    values(std::integral_constant<int, 64>{});
+}
+
+// Whether vectors of V elements of every row are aligned and whole.
+template <class T>
+bool whole_vectors(const void* p, int64_t ld, int experts, int vector) {
+  return experts % vector == 0 && ld % vector == 0 && aligned(p, vector * (int64_t)sizeof(T));
 }
 
 // --------------------------------------------------------------- dispatch
@@ -239,7 +475,7 @@ __global__ __launch_bounds__(256) void route_back_kernel(Router r, int64_t token
 // chunks of whole tokens of one source rank; a wave counts its chunk's
 // choices per expert (and per destination rank), a second kernel turns the
 // counts into the chunk's first place within every expert, and a third puts
-// every choice in its slot.
+// every choice in its slot.  Few choices take one workgroup and one launch.
 struct Plan {
   int experts, top_k, ranks;
   int64_t tokens, per_rank;   // tokens of a source rank
@@ -247,13 +483,67 @@ struct Plan {
   int64_t rank_chunks;        // chunks of a source rank
   int64_t chunks;
   bool once;
+  bool small;                 // one workgroup does it all
 };
+constexpr int kSmallChoices = 4096, kSmallInts = 16000;   // 64 KB of shared memory
 
 __device__ __forceinline__ void chunk_bounds(const Plan& p, int64_t chunk, int64_t* from, int64_t* to) {
   const int64_t rank = chunk / p.rank_chunks, part = chunk % p.rank_chunks;
   const int64_t end = min((rank + 1) * p.per_rank, p.tokens);
   *from = min(rank * p.per_rank + part * p.chunk_tokens, end);
   *to = min(*from + p.chunk_tokens, end);
+}
+
+// A quotient of numbers below 2^22 and 2^11 as a product: 1/size is off by
+// 2^-24 relative, the product by less than half a step.
+__device__ __forceinline__ int quotient(int e, float inverse) { return (int)((e + 0.5f) * inverse); }
+
+// Counts one token's choices per expert, and its rows per destination rank.
+__device__ __forceinline__ void count_token(const Plan& p, const int32_t* row, float per_size, int* per_expert,
+                                            int* per_rank) {
+  uint64_t seen = 0;   // destinations so far, where 64 bits hold them
+  for (int j = 0; j < p.top_k; ++j) {
+    const int e = row[j];
+    if (e < 0 || e >= p.experts) continue;
+    if (per_expert) atomicAdd(&per_expert[e], 1);
+    if (!per_rank) continue;
+    const int to = quotient(e, per_size);
+    bool counts = true;
+    if (p.once && p.ranks <= 64) {
+      counts = !(seen >> to & 1);
+      seen |= 1ull << to;
+    } else if (p.once) {
+      for (int h = 0; h < j; ++h)
+        counts &= row[h] < 0 || row[h] >= p.experts || quotient(row[h], per_size) != to;
+    }
+    if (counts) atomicAdd(&per_rank[to], 1);
+  }
+}
+
+// The places of 64 choices (e < 0: none), each behind the wave's earlier ones
+// of its expert: next[e] is the expert's next place and moves on.
+__device__ __forceinline__ int place_wave(int e, int experts, int lane, int* next) {
+  uint64_t same = __ballot(e >= 0);  // lanes with this lane's expert
+  for (int bit = 0; (1 << bit) < experts; ++bit) {
+    const bool mine = (e >> bit) & 1;
+    const uint64_t set = __ballot(mine);
+    same &= mine ? set : ~set;
+  }
+  int place = -1;
+  if (e >= 0) place = next[e] + __popcll(same & ((1ull << lane) - 1));
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (e >= 0 && (same >> lane) == 1) next[e] = place + 1;  // the last lane of its expert
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return place;
+}
+
+__device__ __forceinline__ int sum_before(int mine, int lane) {   // inclusive
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(mine, o, 64);
+    if (lane >= o) mine += v;
+  }
+  return mine;
 }
 
 __global__ __launch_bounds__(64) void dispatch_count_kernel(Plan p, const int32_t* __restrict__ experts,
@@ -266,55 +556,54 @@ __global__ __launch_bounds__(64) void dispatch_count_kernel(Plan p, const int32_
   __syncthreads();
   int64_t from, to;
   chunk_bounds(p, blockIdx.x, &from, &to);
-  const int size = p.experts / p.ranks;
-  for (int64_t i = from * p.top_k + lane; i < to * p.top_k; i += 64) {
-    const int e = experts[i];
-    if (e < 0 || e >= p.experts) continue;
-    atomicAdd(&per_expert[e], 1);
-    if (!sent) continue;
-    bool counts_once = true;
-    if (p.once)
-      for (int64_t j = i - i % p.top_k; j < i; ++j) {
-        const int before = experts[j];
-        counts_once &= before < 0 || before >= p.experts || before / size != e / size;
-      }
-    if (counts_once) atomicAdd(&per_rank[e / size], 1);
-  }
+  const float per_size = 1.0f / (p.experts / p.ranks);
+  for (int64_t t = from + lane; t < to; t += 64)
+    count_token(p, experts + t * p.top_k, per_size, per_expert, sent ? per_rank : nullptr);
   __syncthreads();
   for (int e = lane; e < p.experts; e += 64) counts[(int64_t)blockIdx.x * p.experts + e] = per_expert[e];
   if (sent)
     for (int d = lane; d < p.ranks; d += 64) sent[(int64_t)blockIdx.x * p.ranks + d] = per_rank[d];
 }
 
-// A wave per expert: counts[chunk][e] becomes the sum over the chunks before.
-__global__ __launch_bounds__(64) void dispatch_scan_kernel(Plan p, int32_t* __restrict__ counts,
-                                                           int32_t* __restrict__ totals,
-                                                           const int32_t* __restrict__ sent, double row_bytes,
-                                                           double* __restrict__ traffic) {
-  const int lane = threadIdx.x;
-  if ((int)blockIdx.x < p.experts) {
-    const int e = blockIdx.x;
-    int carry = 0;
-    for (int64_t c0 = 0; c0 < p.chunks; c0 += 64) {
-      const int64_t c = c0 + lane;
-      const int mine = c < p.chunks ? counts[c * p.experts + e] : 0;
-      int sum = mine;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += v;
-      }
-      if (c < p.chunks) counts[c * p.experts + e] = carry + sum - mine;
-      carry += __shfl(sum, 63, 64);
-    }
-    if (lane == 0) totals[e] = carry;
-    return;
-  }
-  const int from = blockIdx.x - p.experts;  // a source rank
-  for (int to = lane; to < p.ranks; to += 64) {
+// counts[chunk][e] becomes the sum over the chunks before: a workgroup takes
+// 16 experts, 64 threads each for as many runs of chunks.  Further
+// workgroups add up the traffic, 1,024 pairs of ranks each.
+constexpr int kScanExperts = 16;
+__global__ __launch_bounds__(1024) void dispatch_scan_kernel(Plan p, int32_t* __restrict__ counts,
+                                                             int32_t* __restrict__ totals,
+                                                             const int32_t* __restrict__ sent, double row_bytes,
+                                                             double* __restrict__ traffic) {
+  const int groups = (p.experts + kScanExperts - 1) / kScanExperts, tid = threadIdx.x;
+  if ((int)blockIdx.x >= groups) {
+    const int pair = ((int)blockIdx.x - groups) * 1024 + tid;
+    if (pair >= p.ranks * p.ranks) return;
+    const int from = pair / p.ranks, to = pair % p.ranks;
     int64_t rows = 0;
     for (int64_t c = 0; c < p.rank_chunks; ++c) rows += sent[(from * p.rank_chunks + c) * p.ranks + to];
-    traffic[(int64_t)from * p.ranks + to] = (double)rows * row_bytes;
+    traffic[pair] = (double)rows * row_bytes;
+    return;
+  }
+  __shared__ int runs[64][kScanExperts + 1];
+  const int e = blockIdx.x * kScanExperts + tid % kScanExperts, run = tid / kScanExperts;
+  const int64_t each = (p.chunks + 63) / 64, first = min(run * each, p.chunks), last = min(first + each, p.chunks);
+  int sum = 0;
+  if (e < p.experts)
+    for (int64_t c = first; c < last; ++c) sum += counts[c * p.experts + e];
+  runs[run][tid % kScanExperts] = sum;
+  __syncthreads();
+  // a wave per expert over its 64 runs
+  const int lane = tid & 63, of = tid >> 6;
+  const int mine = runs[lane][of], upto = sum_before(mine, lane);
+  __syncthreads();
+  runs[lane][of] = upto - mine;
+  if (lane == 63 && blockIdx.x * kScanExperts + of < p.experts) totals[blockIdx.x * kScanExperts + of] = upto;
+  __syncthreads();
+  if (e >= p.experts) return;
+  sum = runs[run][tid % kScanExperts];
+  for (int64_t c = first; c < last; ++c) {
+    const int here = counts[c * p.experts + e];
+    counts[c * p.experts + e] = sum;
+    sum += here;
   }
 }
 
@@ -324,24 +613,17 @@ __global__ __launch_bounds__(64) void dispatch_place_kernel(Plan p, const int32_
                                                             int32_t* __restrict__ offsets,
                                                             int32_t* __restrict__ token_of_slot,
                                                             int32_t* __restrict__ slot_of_choice) {
-  extern __shared__ int ints[];  // the next free slot of every expert
+  extern __shared__ int next[];  // the next free slot of every expert
   const int lane = threadIdx.x;
   int carry = 0;
   for (int e0 = 0; e0 < p.experts; e0 += 64) {
-    const int e = e0 + lane;
-    const int mine = e < p.experts ? totals[e] : 0;
-    int sum = mine;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(sum, o, 64);
-      if (lane >= o) sum += v;
-    }
+    const int e = e0 + lane, mine = e < p.experts ? totals[e] : 0, upto = sum_before(mine, lane);
     if (e < p.experts) {
-      const int first = carry + sum - mine;
-      ints[e] = first + counts[(int64_t)blockIdx.x * p.experts + e];
+      const int first = carry + upto - mine;
+      next[e] = first + counts[(int64_t)blockIdx.x * p.experts + e];
       if (blockIdx.x == 0) offsets[e] = first;
     }
-    carry += __shfl(sum, 63, 64);
+    carry += __shfl(upto, 63, 64);
   }
   if (blockIdx.x == 0 && lane == 0) offsets[p.experts] = carry;
   // slots that no choice fills
@@ -350,25 +632,79 @@ __global__ __launch_bounds__(64) void dispatch_place_kernel(Plan p, const int32_
   __syncthreads();
   int64_t from, to;
   chunk_bounds(p, blockIdx.x, &from, &to);
-  for (int64_t i0 = from * p.top_k; i0 < to * p.top_k; i0 += 64) {
-    const int64_t i = i0 + lane;
-    int e = i < to * p.top_k ? experts[i] : -1;
+  const int32_t* mine = experts + from * p.top_k;
+  const int n = (int)(to - from) * p.top_k;     // at most 1,024, or one token's
+  const float per_token = 1.0f / p.top_k;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const int i = i0 + lane;
+    int e = i < n ? mine[i] : -1;
     if (e >= p.experts || e < 0) e = -1;
-    uint64_t same = __ballot(e >= 0);  // lanes with this lane's expert
-    for (int bit = 0; (1 << bit) < p.experts; ++bit) {
-      const uint64_t set = __ballot((e >> bit) & 1);
-      same &= (e >> bit) & 1 ? set : ~set;
+    const int slot = place_wave(e, p.experts, lane, next);
+    if (slot >= 0) token_of_slot[slot] = (int32_t)from + quotient(i, per_token);
+    if (i < n) slot_of_choice[from * p.top_k + i] = slot;
+  }
+}
+
+// All of it in one workgroup: at most kSmallChoices choices, a sixteenth of
+// them per wave, and a traffic matrix that shared memory holds.
+__global__ __launch_bounds__(1024) void dispatch_small_kernel(Plan p, const int32_t* __restrict__ experts,
+                                                              int32_t* __restrict__ offsets,
+                                                              int32_t* __restrict__ token_of_slot,
+                                                              int32_t* __restrict__ slot_of_choice, double row_bytes,
+                                                              double* __restrict__ traffic) {
+  extern __shared__ int ints[];
+  __shared__ int ends[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = p.experts, pairs = traffic ? p.ranks * p.ranks : 0;
+  int* counts = ints;              // [16][E]
+  int* sent = ints + 16 * E;       // [ranks][ranks]
+  for (int i = tid; i < 16 * E + pairs; i += 1024) ints[i] = 0;
+  __syncthreads();
+  const int n = (int)p.tokens * p.top_k, each = (n + 1023) / 1024 * 64;   // choices of a wave
+  const float per_token = 1.0f / p.top_k, per_size = 1.0f / (E / p.ranks);
+  int mine[kSmallChoices / 1024];
+#pragma unroll
+  for (int h = 0; h < kSmallChoices / 1024; ++h) {
+    const int i = wave * each + h * 64 + lane;
+    int e = h * 64 < each && i < n ? experts[i] : -1;
+    if (e >= E) e = -1;
+    mine[h] = e;
+    if (e >= 0) atomicAdd(&counts[wave * E + e], 1);
+  }
+  if (traffic)
+    for (int t = tid; t < p.tokens; t += 1024)
+      count_token(p, experts + (int64_t)t * p.top_k, per_size, nullptr, sent + t / p.per_rank * p.ranks);
+  __syncthreads();
+  // counts to first places: over the waves, then over the experts
+  int sum = 0;
+  if (tid < E)
+    for (int w = 0; w < 16; ++w) {
+      const int here = counts[w * E + tid];
+      counts[w * E + tid] = sum;
+      sum += here;
     }
-    int slot = -1;
-    if (e >= 0) {
-      const int before = __popcll(same & ((1ull << lane) - 1));
-      slot = ints[e] + before;
-      token_of_slot[slot] = (int32_t)(i / p.top_k);
-    }
-    __syncthreads();
-    if (e >= 0 && (same >> lane) == 1) ints[e] = slot + 1;  // the last lane of its expert
-    __syncthreads();
-    if (i < to * p.top_k) slot_of_choice[i] = slot;
+  const int upto = sum_before(sum, lane);
+  if (lane == 63) ends[wave] = upto;
+  __syncthreads();
+  int first = upto - sum, all = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) first += ends[w];
+    all += ends[w];
+  }
+  if (tid < E) {
+    for (int w = 0; w < 16; ++w) counts[w * E + tid] += first;
+    offsets[tid] = first;
+  }
+  if (tid == 0) offsets[E] = all;
+  for (int s = all + tid; s < n; s += 1024) token_of_slot[s] = -1;
+  for (int i = tid; i < pairs; i += 1024) traffic[i] = (double)sent[i] * row_bytes;
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < kSmallChoices / 1024; ++h) {
+    if (h * 64 >= each) break;
+    const int i = wave * each + h * 64 + lane;
+    const int slot = place_wave(mine[h], E, lane, counts + wave * E);
+    if (slot >= 0) token_of_slot[slot] = quotient(i, per_token);
+    if (i < n) slot_of_choice[i] = slot;
   }
 }
 
@@ -411,6 +747,7 @@ Plan make_plan(int32_t experts, int32_t top_k, int64_t tokens, int32_t ranks, in
   p.chunk_tokens = 1024 / top_k;
   p.rank_chunks = ceil_div(p.per_rank, p.chunk_tokens);
   p.chunks = p.rank_chunks * ranks;
+  p.small = tokens * top_k <= kSmallChoices && 16 * experts + ranks * ranks <= kSmallInts;
   return p;
 }
 
@@ -446,12 +783,16 @@ extern "C" netsim_status netsim_route(int32_t device, const netsim_router* route
     if (!aligned(d_logits, type_size(type)) || !aligned(d_bias, 4) || !aligned(d_experts, 4) || !aligned(d_weights, 4))
       return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type");
     return launch(what, device, [&] {
-      const size_t lds = r.groups > 1 ? 4 * sizeof(float) * (r.experts + 2 * r.groups) : 0;
       with_type(type, [&](auto t) {
-        using T = decltype(t);
-        hipLaunchKernelGGL(route_kernel<T>, dim3((unsigned)ceil_div(tokens, 4)), dim3(256), lds,
-                           static_cast<hipStream_t>(hip_stream), r, tokens, static_cast<const T*>(d_logits), ld_logits,
-                           d_bias, d_experts, d_weights);
+        with_shape(tokens, r.experts, [&](auto l, auto n) {
+          using T = decltype(t);
+          constexpr int L = decltype(l)::value, N = decltype(n)::value;
+          const size_t lds = r.groups > 1 ? 256 / L * sizeof(float) * (r.experts + 1 + 2 * r.groups) : 0;
+          hipLaunchKernelGGL((route_kernel<T, L, N>), dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), lds,
+                             static_cast<hipStream_t>(hip_stream), r, tokens, static_cast<const T*>(d_logits), ld_logits,
+                             whole_vectors<T>(d_logits, ld_logits, r.experts, Row<T, L, N>::V), d_bias, d_experts,
+                             d_weights);
+        });
       });
     });
   });
@@ -479,10 +820,32 @@ extern "C" netsim_status netsim_route_backward(int32_t device, const netsim_rout
     return launch(what, device, [&] {
       with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(route_back_kernel<T>, dim3((unsigned)ceil_div(tokens, 4)), dim3(256),
-                           4 * sizeof(float) * r.experts, static_cast<hipStream_t>(hip_stream), r, tokens,
-                           static_cast<const T*>(d_logits), ld_logits, d_experts, d_dweights,
-                           static_cast<T*>(d_dlogits), ld_dlogits);
+        hipStream_t s = static_cast<hipStream_t>(hip_stream);
+        const T* in = static_cast<const T*>(d_logits);
+        T* out = static_cast<T*>(d_dlogits);
+        if (r.softmax && !r.renorm) {
+          with_shape(tokens, r.experts, [&](auto l, auto n) {
+            constexpr int L = decltype(l)::value, N = decltype(n)::value, V = Row<T, L, N>::V;
+            hipLaunchKernelGGL((route_back_kernel<T, L, N>), dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), 0, s,
+                               r, tokens, in, ld_logits, whole_vectors<T>(in, ld_logits, r.experts, V), d_experts,
+                               d_dweights, out, ld_dlogits, whole_vectors<T>(out, ld_dlogits, r.experts, V));
+          });
+          return;
+        }
+        auto run = [&](auto lanes) {
+          constexpr int K = decltype(lanes)::value, V = 16 / sizeof(T);
+          const size_t lds = 256 / K * sizeof(float) * (ceil_div(r.experts, V) * V);
+          hipLaunchKernelGGL((route_back_chosen_kernel<T, K>), dim3((unsigned)ceil_div(tokens, 256 / K)), dim3(256), lds,
+                             s, r, tokens, in, ld_logits, d_experts, d_dweights, out, ld_dlogits,
+                             whole_vectors<T>(out, ld_dlogits, r.experts, V));
+        };
+        // the rows of a workgroup have to fit its shared memory (64 KB)
+        if (r.top_k <= 8 && r.experts <= 512)
+          run(std::integral_constant<int, 8>{});
+        else if (r.top_k <= 16)
+          run(std::integral_constant<int, 16>{});
+        else
+          run(std::integral_constant<int, 32>{});
       });
     });
   });
@@ -523,13 +886,20 @@ extern "C" netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_
         hipLaunchKernelGGL(dispatch_nothing_kernel, dim3(64), dim3(256), 0, s, experts, ranks, d_offsets, d_traffic);
         return;
       }
+      if (p.small) {
+        hipLaunchKernelGGL(dispatch_small_kernel, dim3(1), dim3(1024),
+                           sizeof(int) * (16 * experts + (d_traffic ? ranks * ranks : 0)), s, p, d_experts, d_offsets,
+                           d_token_of_slot, d_slot_of_choice, row_bytes, d_traffic);
+        return;
+      }
       int32_t* counts = static_cast<int32_t*>(d_work);
       int32_t* sent = counts + p.chunks * p.experts;
       int32_t* totals = sent + p.chunks * p.ranks;
       hipLaunchKernelGGL(dispatch_count_kernel, dim3((unsigned)p.chunks), dim3(64), sizeof(int) * (experts + ranks), s,
                          p, d_experts, counts, d_traffic ? sent : nullptr);
-      hipLaunchKernelGGL(dispatch_scan_kernel, dim3(experts + (d_traffic ? ranks : 0)), dim3(64), 0, s, p, counts,
-                         totals, sent, row_bytes, d_traffic);
+      const int64_t scans = ceil_div(experts, kScanExperts) + (d_traffic ? ceil_div((int64_t)ranks * ranks, 1024) : 0);
+      hipLaunchKernelGGL(dispatch_scan_kernel, dim3((unsigned)scans), dim3(1024), 0, s, p, counts, totals, sent,
+                         row_bytes, d_traffic);
       hipLaunchKernelGGL(dispatch_place_kernel, dim3((unsigned)p.chunks), dim3(64), sizeof(int) * experts, s, p,
                          d_experts, counts, totals, d_offsets, d_token_of_slot, d_slot_of_choice);
     });
