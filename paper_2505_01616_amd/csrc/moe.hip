@@ -20,11 +20,17 @@ constexpr float kNone = -INFINITY;
 // formed in the same order everywhere.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int moved(int old, int v) {
-  return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xF, false);
+  // with all rows taking part every lane has a partner, and the move can be
+  // part of the instruction that uses it
+  return __builtin_amdgcn_update_dpp(ROWS == 0xF ? 0 : old, v, CTRL, ROWS, 0xF, ROWS == 0xF);
 }
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float moved(float old, float v) {
   return __int_as_float(moved<CTRL, ROWS>(__float_as_int(old), __float_as_int(v)));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t old, uint32_t v) {
+  return (uint32_t)moved<CTRL, ROWS>((int)old, (int)v);
 }
 template <int CTRL, int ROWS>
 __device__ __forceinline__ double moved(double old, double v) {
@@ -32,6 +38,7 @@ __device__ __forceinline__ double moved(double old, double v) {
   const int lo = moved<CTRL, ROWS>((int)o, (int)b), hi = moved<CTRL, ROWS>((int)(o >> 32), (int)(b >> 32));
   return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
 }
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return __builtin_amdgcn_readlane((int)v, 63); }
 __device__ __forceinline__ float last_lane(float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63)); }
 __device__ __forceinline__ double last_lane(double v) {
   const long long b = __double_as_longlong(v);
@@ -79,6 +86,8 @@ __device__ __forceinline__ float exp_of(float x) {
   // beyond the range hi alone decides (0 or infinity); low may not be finite there
   return fabsf(hi) < 150.0f ? __builtin_fmaf(p, low * LN2, p) : p;
 }
+// exp(x) for x <= 0 with the product rounded: off by |x| half steps more.
+__device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + exp_of(-x)); }
 
 struct Router {
@@ -117,35 +126,69 @@ struct Row {
 // ---------------------------------------------------------------- routing
 // L lanes per row, N logits each, in registers; one pass over the logits.
 //
-// A choice value and its expert are one 64-bit float: a 32-bit value leaves
-// the low 29 bits of a 64-bit one free, and the low 10 get the expert's
-// number so that of equal values the lowest expert is the largest key.  A
-// compare-and-exchange is then a minimum and a maximum.  Each lane sorts its
-// keys; the largest of a row is the largest of the lanes' first ones, and
-// the lane that gave it moves on to its next.
+// A choice value and its expert make one key, so that a compare-and-exchange
+// is a minimum and a maximum: of equal values the lowest expert is the
+// largest key.  Each lane sorts its keys; the largest of a row is the
+// largest of the lanes' first ones, and the lane that gave it moves on to
+// its next.
 //
 // Bound by instructions per row: few lanes per row mean few exchanges (8
 // lanes: three per choice, eight rows at once), many lanes mean short sorts
 // and enough waves where rows are few.
-constexpr double kNoKey = -1.0e300;
 
-__device__ __forceinline__ double key_of(float value, int expert) {
-  const double wide = value == INFINITY ? 1.0e200 : (double)(value + 0.0f);   // + 0: -0 is 0
-  const long long b = __double_as_longlong(wide) & ~0x1FFFFFFFll;
-  return value == kNone ? kNoKey : __longlong_as_double(b | (b < 0 ? expert : kMaxExperts - 1 - expert));
-}
-__device__ __forceinline__ int expert_of(double key) {
-  const long long b = __double_as_longlong(key);
-  const int low = (int)b & (kMaxExperts - 1);
-  return key == kNoKey ? -1 : b < 0 ? low : kMaxExperts - 1 - low;
-}
-// Keys are never NaN.
-__device__ __forceinline__ double larger(double a, double b) { return a > b ? a : b; }
-__device__ __forceinline__ double smaller(double a, double b) { return a > b ? b : a; }
+// A 32-bit value in a 64-bit float leaves its low 29 bits free.
+struct WideKey {
+  using type = double;
+  static constexpr double NONE = -0x1p996;    // below every value; infinities move to +-2^996
+  static __device__ __forceinline__ double larger(double a, double b) {
+    double r;
+    asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));   // keys are never NaN
+    return r;
+  }
+  static __device__ __forceinline__ double smaller(double a, double b) {
+    double r;
+    asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+  }
+  static __device__ __forceinline__ double of(float value, int expert) {
+    // + 0: -0 is 0
+    const long long b = __double_as_longlong(larger(smaller((double)(value + 0.0f), 0x1p996), NONE));
+    const int hi = (int)(b >> 32), low = (expert ^ (kMaxExperts - 1)) ^ ((hi >> 31) & (kMaxExperts - 1));
+    return __longlong_as_double((b & ~0x1FFFFFFFll) | low);
+  }
+  static __device__ __forceinline__ int expert(double key) {
+    const long long b = __double_as_longlong(key);
+    const int low = (int)b & (kMaxExperts - 1);
+    return key <= NONE ? -1 : b < 0 ? low : low ^ (kMaxExperts - 1);
+  }
+};
+// Values of 16 bits as 32-bit floats end in 13 zeros or more: 19 bits in the
+// order of the values, and 10 for the expert.
+struct ShortKey {
+  using type = uint32_t;
+  static constexpr uint32_t NONE = 0;
+  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) { return a > b ? b : a; }
+  static __device__ __forceinline__ uint32_t of(float value, int expert) {
+    const uint32_t b = __float_as_uint(value + 0.0f);
+    const uint32_t order = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+    return (order >> 13) << 10 | (kMaxExperts - 1 - expert);
+  }
+  static __device__ __forceinline__ int expert(uint32_t key) {
+    // minus infinity, 0xFF800000, has the order 0x007FFFFF
+    return key >= ((0x007FFFFFu >> 13) + 1) << 10 ? kMaxExperts - 1 - (int)(key & (kMaxExperts - 1)) : -1;
+  }
+};
 
-// Descending order by odd-even merges (Batcher 1968).
-template <int N>
-__device__ __forceinline__ void sort_keys(double (&k)[N]) {
+template <class Key, class K>
+__device__ __forceinline__ void exchange(K& a, K& b) {
+  const K more = Key::larger(a, b), less = Key::smaller(a, b);
+  a = more;
+  b = less;
+}
+// Descending order of FROM .. FROM + N - 1 by odd-even merges (Batcher 1968).
+template <class Key, int FROM, int N, class K, int SIZE>
+__device__ __forceinline__ void sort_keys(K (&k)[SIZE]) {
 #pragma unroll
   for (int p = 1; p < N; p *= 2)
 #pragma unroll
@@ -154,44 +197,62 @@ __device__ __forceinline__ void sort_keys(double (&k)[N]) {
       for (int j = h % p; j + h < N; j += 2 * h)
 #pragma unroll
         for (int i = 0; i < h; ++i)
-          if (i + j + h < N && (i + j) / (2 * p) == (i + j + h) / (2 * p)) {
-            const double a = k[i + j], b = k[i + j + h];
-            k[i + j] = larger(a, b);
-            k[i + j + h] = smaller(a, b);
-          }
+          if (i + j + h < N && (i + j) / (2 * p) == (i + j + h) / (2 * p))
+            exchange<Key>(k[FROM + i + j], k[FROM + i + j + h]);
+}
+// The M largest of N keys in descending order, in k[0 .. M-1].
+template <class Key, int M, class K, int N>
+__device__ __forceinline__ void largest_keys(K (&k)[N]) {
+  if constexpr (M == N) {
+    sort_keys<Key, 0, N>(k);
+  } else {
+    static_assert(N == 2 * M, "two lists are merged");
+    sort_keys<Key, 0, M>(k);
+    sort_keys<Key, M, M>(k);
+    // the larger of each pair from the two ends rises and falls once
+#pragma unroll
+    for (int i = 0; i < M; ++i) k[i] = Key::larger(k[i], k[N - 1 - i]);
+#pragma unroll
+    for (int h = M / 2; h >= 1; h /= 2)
+#pragma unroll
+      for (int i = 0; i < M; ++i)
+        if ((i & h) == 0) exchange<Key>(k[i], k[i + h]);
+  }
 }
 
-template <class T, int L, int N>
+// FEW: top_k <= 8.  BY_SCORE: scores are compared, not logits.
+template <class T, int L, int N, bool FEW, bool BY_SCORE>
 __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, const T* __restrict__ logits, int64_t ld,
                                                     bool wide, const float* __restrict__ bias,
                                                     int32_t* __restrict__ experts, float* __restrict__ weights) {
   extern __shared__ float shared[];
   using R = Row<T, L, N>;
-  constexpr int SLOTS = (kMaxTopK + L - 1) / L;
+  using Key = std::conditional_t<sizeof(T) == 2 && !BY_SCORE, ShortKey, WideKey>;
+  using K = typename Key::type;
+  constexpr int M = FEW && N > 8 ? 8 : N, SLOTS = FEW ? 1 : (kMaxTopK + L - 1) / L;
   const int j = threadIdx.x & (L - 1);
   const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / L;
   const int64_t row = at < tokens ? at : tokens - 1;   // lanes beyond repeat the last row and write nothing
   const T* x_row = logits + row * ld;
-  const bool by_score = bias || r.best > 1;  // else the logits give the same order
 
   float x[N], top = kNone;
   R::load(x_row, r.experts, j, wide, x);
+  const int undefined = r.softmax ? 0x203 : 0x003;   // NaN, and plus infinity
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    bad |= isnan(x[i]) || (r.softmax && x[i] == INFINITY);
-    top = fmaxf(top, x[i]);
-  }
+  for (int i = 0; i < N; ++i) bad |= __builtin_amdgcn_classf(x[i], undefined);
   float base = 0.0f, z = 1.0f;
-  if (r.softmax && (by_score || !r.renorm)) {
+  if (r.softmax && (BY_SCORE || !r.renorm)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, x[i]);
     top = max_over<L>(top);
     base = top == kNone ? 0.0f : top;
     z = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) z += exp_of(x[i] - base);
+    for (int i = 0; i < N; ++i) z += exp_near(x[i] - base);
     z = sum_over<L>(z);
   }
-  if (by_score) {
+  if constexpr (BY_SCORE) {
     const float inverse = 1.0f / z;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -238,25 +299,25 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
     }
   }
 
-  const bool row_bad = any_over<L>(bad);
-  double k[N];
+  K k[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) k[i] = key_of(row_bad ? kNone : x[i], R::element(i, j) & (kMaxExperts - 1));
-  sort_keys(k);
+  for (int i = 0; i < N; ++i) k[i] = Key::of(x[i], R::element(i, j));
+  largest_keys<Key, M>(k);
   int mine[SLOTS];  // lane j keeps the choices j, j + L, ...
 #pragma unroll
   for (int s = 0; s < SLOTS; ++s) mine[s] = -1;
   for (int c = 0; c < r.top_k; ++c) {
-    const double best = over<L>(k[0], [](double v) { return v; }, larger);
+    const K best = over<L>(k[0], [](K v) { return v; }, [](K a, K b) { return Key::larger(a, b); });
     const bool taken = k[0] == best;
 #pragma unroll
-    for (int i = 0; i + 1 < N; ++i) k[i] = taken ? k[i + 1] : k[i];
-    k[N - 1] = taken ? kNoKey : k[N - 1];
+    for (int i = 0; i + 1 < M; ++i) k[i] = taken ? k[i + 1] : k[i];
+    k[M - 1] = taken ? Key::NONE : k[M - 1];
+    const int expert = Key::expert(best);
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s)
-      if (c == s * L + j) mine[s] = expert_of(best);
+    for (int s = 0; s < SLOTS; ++s) mine[s] = c == s * L + j ? expert : mine[s];
   }
 
+  const bool row_bad = any_over<L>(bad);
   float l[SLOTS], w[SLOTS], sum = 0.0f, most = kNone;
 #pragma unroll
   for (int s = 0; s < SLOTS; ++s) {
@@ -271,12 +332,13 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
     sum += w[s];
   }
   if (r.renorm) z = sum_over<L>(sum);
+  const float factor = z > 0.0f ? r.scale / z : 0.0f;
 #pragma unroll
   for (int s = 0; s < SLOTS; ++s)
     if (at < tokens && s * L + j < r.top_k) {
       const int64_t to = row * r.top_k + s * L + j;
-      experts[to] = mine[s];
-      weights[to] = row_bad ? NAN : mine[s] >= 0 && z > 0.0f ? w[s] / z * r.scale : 0.0f;
+      experts[to] = row_bad ? -1 : mine[s];
+      weights[to] = row_bad ? NAN : w[s] * factor;
     }
 }
 
@@ -447,9 +509,7 @@ void with_shape(int64_t tokens, int experts, F&& f) {
   auto values = [&](auto l) {
     constexpr int L = decltype(l)::value;
     const int n = (experts + L - 1) / L;
-    if (n <= 1)
-      f(l, std::integral_constant<int, 1>{});
-    else if (n <= 4)
+    if (n <= 4)
       f(l, std::integral_constant<int, 4>{});
     else if (n <= 8)
       f(l, std::integral_constant<int, 8>{});
@@ -788,10 +848,18 @@ extern "C" netsim_status netsim_route(int32_t device, const netsim_router* route
           using T = decltype(t);
           constexpr int L = decltype(l)::value, N = decltype(n)::value;
           const size_t lds = r.groups > 1 ? 256 / L * sizeof(float) * (r.experts + 1 + 2 * r.groups) : 0;
-          hipLaunchKernelGGL((route_kernel<T, L, N>), dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), lds,
-                             static_cast<hipStream_t>(hip_stream), r, tokens, static_cast<const T*>(d_logits), ld_logits,
-                             whole_vectors<T>(d_logits, ld_logits, r.experts, Row<T, L, N>::V), d_bias, d_experts,
-                             d_weights);
+          auto run = [&](auto kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), lds,
+                               static_cast<hipStream_t>(hip_stream), r, tokens, static_cast<const T*>(d_logits),
+                               ld_logits, whole_vectors<T>(d_logits, ld_logits, r.experts, Row<T, L, N>::V), d_bias,
+                               d_experts, d_weights);
+          };
+          // without a bias and sums of scores the logits give the same order
+          const bool by_score = d_bias || r.best > 1;
+          if (r.top_k <= 8)
+            run(by_score ? route_kernel<T, L, N, true, true> : route_kernel<T, L, N, true, false>);
+          else
+            run(by_score ? route_kernel<T, L, N, false, true> : route_kernel<T, L, N, false, false>);
         });
       });
     });
