@@ -310,11 +310,14 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
     const K best = over<L>(k[0], [](K v) { return v; }, [](K a, K b) { return Key::larger(a, b); });
     const bool taken = k[0] == best;
 #pragma unroll
-    for (int i = 0; i + 1 < M; ++i) k[i] = taken ? k[i + 1] : k[i];
-    k[M - 1] = taken ? Key::NONE : k[M - 1];
+    for (int i = 0; i < M; ++i) {
+      const K here = k[i], after = i + 1 < M ? k[i + 1] : Key::NONE;   // values: an index chosen at run time costs M selects
+      k[i] = taken ? after : here;
+    }
     const int expert = Key::expert(best);
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s) mine[s] = c == s * L + j ? expert : mine[s];
+    for (int s = 0; s < SLOTS; ++s)
+      if (c == s * L + j) mine[s] = expert;
   }
 
   const bool row_bad = any_over<L>(bad);
