@@ -264,7 +264,8 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
   }
 
   if (r.groups > 1) {
-    // the row's choice values in shared memory; a lane takes whole groups
+    // the row's choice values in shared memory; as many lanes as there are
+    // for each group look through its members
     const int size = r.experts / r.groups, pitch = r.experts + 1;
     float* row_c = shared + (threadIdx.x / L) * (pitch + 2 * r.groups);
     float* score = row_c + pitch;
@@ -273,19 +274,30 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
     for (int i = 0; i < N; ++i)
       if (R::element(i, j) < r.experts) row_c[R::element(i, j)] = x[i];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int g = j; g < r.groups; g += L) {
+    int share = 1;   // lanes of a group, a power of two
+    while (2 * share * r.groups <= L) share *= 2;
+    for (int g0 = 0; g0 < r.groups; g0 += L / share) {
+      const int g = g0 + j / share;
+      const float* member = row_c + (g < r.groups ? g : 0) * size;
       float a = kNone, b = kNone;  // the two largest
-      for (int i = 0; i < size; ++i) {
-        const float v = row_c[g * size + i];
-        b = v > a ? a : fmaxf(b, v);
+#pragma unroll 4
+      for (int i = j & (share - 1); i < size; i += share) {
+        const float v = member[i];
+        b = fmaxf(b, fminf(a, v));
         a = fmaxf(a, v);
       }
-      score[g] = r.best > 1 && b > kNone ? a + b : a;
+      for (int o = 1; o < share; o *= 2) {
+        const float a2 = __shfl_xor(a, o, 64), b2 = __shfl_xor(b, o, 64);
+        b = fmaxf(fmaxf(b, b2), fminf(a, a2));
+        a = fmaxf(a, a2);
+      }
+      if (g < r.groups && (j & (share - 1)) == 0) score[g] = r.best > 1 && b > kNone ? a + b : a;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     for (int g = j; g < r.groups; g += L) {
       const float mine = score[g];
       int before = 0;
+#pragma unroll 4
       for (int h = 0; h < r.groups; ++h) before += score[h] > mine || (score[h] == mine && h < g);
       keep[g] = before < r.kept ? 1.0f : 0.0f;
     }
