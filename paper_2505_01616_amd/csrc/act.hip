@@ -240,31 +240,37 @@ struct Cut {
 // workgroups start in this order, so the last to end are short (a sum over
 // the hot expert of 131,072 routed slots, 25,480 long, started last would
 // add 15%).
+// One workgroup with a thread per expert.
 __global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, int step, const int32_t* __restrict__ offsets,
                                                     Item* __restrict__ items, Join* __restrict__ joins) {
-  __shared__ int length[1024], count[1024], cuts[1024];
+  __shared__ int length[1024], first_item[1024], first_partial[1024];
+  __shared__ Item whole[1024];     // by place in the order; `partial` holds the slots of a part
   __shared__ int sums[3][16];
   const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
-  Item it{-1, 0, 0, -1};
-  int parts = 0, each = 0;
+  Item it{-1, 0, 0, 0};
+  uint32_t parts = 0, each = 0;
   if (e < g.experts) {
     it = segment(offsets, e, g.slots);
-    const int64_t n = it.to - it.from;
-    parts = n > cut.longest ? (int)((n + cut.longest - 1) / cut.longest) : 1;
-    each = (int)((n + parts - 1) / parts + step - 1) / step * step;
-    if (parts > 1) parts = (int)((n + each - 1) / each);
+    const uint32_t n = it.to - it.from, longest = (uint32_t)cut.longest;
+    parts = n > longest ? (n + longest - 1) / longest : 1;
+    each = ((n + parts - 1) / parts + step - 1) / step * step;
+    if (parts > 1) parts = (n + each - 1) / each;
+    it.partial = (int)each;
   }
-  length[e] = e < g.experts ? each : -1;
+  length[e] = e < g.experts ? (int)each : -1;
   __syncthreads();
-  int place = 0;
-  for (int h = 0; h < g.experts; ++h) place += length[h] > each || (length[h] == each && h < e);
+  int place = e;
+  if (e < g.experts) {
+    place = 0;
+#pragma unroll 8
+    for (int h = 0; h < g.experts; ++h) place += length[h] > (int)each || (length[h] == (int)each && h < e);
+  }
+  whole[place] = it;
+  first_item[place] = parts;
   __syncthreads();
-  // per place in the order: parts, and parts and joins of experts that are cut
-  if (e >= g.experts) place = e;
-  count[place] = parts;
-  cuts[place] = parts > 1 ? parts : 0;
-  __syncthreads();
-  int v[3] = {count[e], cuts[e], cuts[e] ? 1 : 0};
+  // per place: the parts, partial sums and joins of the places before
+  const int here = first_item[e], cuts = here > 1 ? here : 0;
+  int v[3] = {here, cuts, cuts ? 1 : 0};
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
 #pragma unroll
@@ -275,65 +281,91 @@ __global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, int step, c
     if (lane == 63) sums[i][wave] = v[i];
   }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 3; ++i)
-    for (int w = 0; w < wave; ++w) v[i] += sums[i][w];
   int all_items = 0, all_joins = 0;
-  for (int w = 0; w < 16; ++w) {
+  for (int w = 0; w < (int)blockDim.x / 64; ++w) {
+    if (w < wave)
+      for (int i = 0; i < 3; ++i) v[i] += sums[i][w];
     all_items += sums[0][w];
     all_joins += sums[2][w];
   }
-  const int my_count = count[e], my_cut = cuts[e];
+  // offsets that decrease could ask for more than there is room for: such
+  // sums are left out
+  const int item = v[0] - here, partial = v[1] - cuts, join = v[2] - (cuts ? 1 : 0);
+  const bool fits = item + here <= cut.items && partial + cuts <= cut.partials;
+  first_item[e] = item;
+  first_partial[e] = !fits ? -2 : cuts ? partial : -1;
+  if (cuts && join < cut.joins) joins[join] = fits ? Join{whole[e].expert, partial, here, 0} : Join{-1, 0, 0, 0};
+  for (int64_t i = all_joins + e; i < cut.joins; i += blockDim.x) joins[i] = Join{-1, 0, 0, 0};
   __syncthreads();
-  length[e] = v[0] - my_count;          // first item, partial and join of place e
-  count[e] = v[1] - my_cut;
-  cuts[e] = v[2] - (my_cut ? 1 : 0);
-  __syncthreads();
-  if (e < g.experts) {
-    const int first = length[place], partial = count[place];
-    // offsets that decrease could ask for more than there is room for
-    const bool fits = first + parts <= cut.items && (parts == 1 || partial + parts <= cut.partials);
-    for (int p = 0; p < parts && first + p < cut.items; ++p) {
-      const int64_t from = it.from + (int64_t)p * each, to = min((int64_t)it.to, from + each);
-      items[first + p] = fits ? Item{e, (int)from, (int)to, parts > 1 ? partial + p : -1} : Item{-1, 0, 0, -1};
+  for (int i = e; i < cut.items; i += blockDim.x) {
+    Item out{-1, 0, 0, -1};
+    if (i < all_items) {
+      int low = 0, high = g.experts;   // the last place whose first item is at most i
+      while (high - low > 1) {
+        const int mid = (low + high) / 2;
+        (first_item[mid] <= i ? low : high) = mid;
+      }
+      const Item w = whole[low];
+      const int p = i - first_item[low], before = first_partial[low];
+      const int64_t from = w.from + (int64_t)p * w.partial, to = min((int64_t)w.to, from + w.partial);
+      if (before == -1)
+        out = Item{w.expert, w.from, w.to, -1};
+      else if (before >= 0)
+        out = Item{w.expert, (int)from, (int)to, before + p};
     }
-    if (parts > 1 && cuts[place] < cut.joins) joins[cuts[place]] = fits ? Join{e, partial, parts, 0} : Join{-1, 0, 0, 0};
+    items[i] = out;
   }
-  for (int64_t i = all_items + e; i < cut.items; i += 1024) items[i] = Item{-1, 0, 0, -1};
-  for (int64_t i = all_joins + e; i < cut.joins; i += 1024) joins[i] = Join{-1, 0, 0, 0};
 }
 
-// dW of the experts whose sums are in parts; the parts are added in order.
+// dW of the experts whose sums are in parts.  Four threads take every fourth
+// part of four elements; the order of the sum depends on the parts alone.
 template <class O>
 __global__ __launch_bounds__(256) void join_kernel(Grad g, const Join* __restrict__ joins,
                                                    const float* __restrict__ partials, O* __restrict__ dw) {
+  __shared__ float sums[4][64][4];
   const Join j = joins[blockIdx.y];
+  if (j.parts == 0) return;
   const int64_t size = (int64_t)g.n * g.cols;
   const float* from = partials + j.first * size;
-  if (j.parts == 0) return;
   O* out = dw + j.expert * size;
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)gridDim.x * 1024) {
+  const int quarter = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int64_t i0 = (int64_t)blockIdx.x * 256; i0 < size; i0 += (int64_t)gridDim.x * 256) {
+    const int64_t i = i0 + lane * 4;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (g.wide_stores) {
-      for (int p = 0; p < j.parts; ++p) {
-        const float4 v = *reinterpret_cast<const float4*>(from + p * size + i);
-        sum[0] += v.x;
-        sum[1] += v.y;
-        sum[2] += v.z;
-        sum[3] += v.w;
+      if (i < size) {
+#pragma unroll 4
+        for (int p = quarter; p < j.parts; p += 4) {
+          const float4 v = *reinterpret_cast<const float4*>(from + p * size + i);
+          sum[0] += v.x;
+          sum[1] += v.y;
+          sum[2] += v.z;
+          sum[3] += v.w;
+        }
       }
+    } else {
+      for (int h = 0; h < 4; ++h)
+        if (i + h < size)
+          for (int p = quarter; p < j.parts; p += 4) sum[h] += from[p * size + i + h];
+    }
+#pragma unroll
+    for (int h = 0; h < 4; ++h) sums[quarter][lane][h] = sum[h];
+    __syncthreads();
+    if (quarter == 0 && i < size) {
       struct alignas(4 * sizeof(O)) Four {
         O v[4];
       } four;
 #pragma unroll
-      for (int h = 0; h < 4; ++h) four.v[h] = (O)sum[h];
-      *reinterpret_cast<Four*>(out + i) = four;
-    } else {
-      for (int h = 0; h < 4 && i + h < size; ++h) {
-        for (int p = 0; p < j.parts; ++p) sum[h] += from[p * size + i + h];
-        out[i + h] = (O)sum[h];
+      for (int h = 0; h < 4; ++h)
+        four.v[h] = (O)((sums[0][lane][h] + sums[1][lane][h]) + (sums[2][lane][h] + sums[3][lane][h]));
+      if (g.wide_stores) {
+        *reinterpret_cast<Four*>(out + i) = four;
+      } else {
+        for (int h = 0; h < 4; ++h)
+          if (i + h < size) out[i + h] = four.v[h];
       }
     }
+    __syncthreads();
   }
 }
 
@@ -560,6 +592,7 @@ Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols) {
   // than they save
   c.longest = ceil_div(slots * tiles, 256);
   if (c.longest < 256) c.longest = 256;
+  if (c.longest > kMaxSlots) c.longest = kMaxSlots;   // no sum is longer
   // laying the parts out and joining them takes two more launches, about as
   // long as 1,024 slots of one tile
   c.planned = slots > 1024;
@@ -670,7 +703,7 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
           Join* joins = reinterpret_cast<Join*>(items + cut.items);
           float* partials = reinterpret_cast<float*>(joins + cut.joins);
           if (cut.planned)
-            hipLaunchKernelGGL(plan_kernel, dim3(1), dim3(1024), 0, s, g, cut, KB, d_offsets, items, joins);
+            hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(experts, 64) * 64), 0, s, g, cut, KB, d_offsets, items, joins);
           auto run = [&](auto kernel, int threads) {
             const int lds = 2 * 2 * KB * (Terms<T>::value + 1) * (cut.tile + 32);
             (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -685,8 +718,10 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
           else
             run(grad_kernel<T, O, 128, 128, 2, 2, KB>, 256);
           if (cut.joins > 0) {
-            const int64_t groups = ceil_div((int64_t)n * cols, 1024);
-            hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)(groups < 4096 ? groups : 4096), (unsigned)cut.joins),
+            // mostly there are few experts to join, or none: groups that find
+            // nothing to do cost 4 us at 14,000 of them
+            const int64_t groups = ceil_div((int64_t)n * cols, 256), most = cut.joins < 32 ? 4096 / cut.joins : 128;
+            hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)(groups < most ? groups : most), (unsigned)cut.joins),
                                dim3(256), 0, s, g, joins, partials, static_cast<O*>(d_dw));
           }
         });

@@ -88,7 +88,7 @@ __device__ __forceinline__ float exp_of(float x) {
 }
 // exp(x) for x <= 0 with the product rounded: off by |x| half steps more.
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + exp_of(-x)); }
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }   // to 1 unit more
 
 struct Router {
   int experts, top_k, groups, kept, best;
@@ -515,7 +515,9 @@ __global__ __launch_bounds__(256) void route_back_kernel(Router r, int64_t token
 // Calls f with the lanes per row and the values per lane as constants.
 // Fewer lanes per row exchange less per row, as long as a lane holds at most
 // 16 values and the rows still make 4,096 waves (4 for each of the 1,024
-// SIMDs): MEASURED.
+// SIMDs).  131,072 rows of 128 bfloat16 logits take 18 us in 8 lanes, 20 in
+// 16 and 51 in 64; 16,384 rows of 256 float32 ones in groups 15 us in 16 lanes
+// and 20 in 64.
 template <class F>
 void with_shape(int64_t tokens, int experts, F&& f) {
   int lanes = 64;
@@ -573,15 +575,12 @@ __device__ __forceinline__ void chunk_bounds(const Plan& p, int64_t chunk, int64
 // 2^-24 relative, the product by less than half a step.
 __device__ __forceinline__ int quotient(int e, float inverse) { return (int)((e + 0.5f) * inverse); }
 
-// Counts one token's choices per expert, and its rows per destination rank.
-__device__ __forceinline__ void count_token(const Plan& p, const int32_t* row, float per_size, int* per_expert,
-                                            int* per_rank) {
+// Counts one token's rows per destination rank.
+__device__ __forceinline__ void count_token(const Plan& p, const int32_t* row, float per_size, int* per_rank) {
   uint64_t seen = 0;   // destinations so far, where 64 bits hold them
   for (int j = 0; j < p.top_k; ++j) {
     const int e = row[j];
     if (e < 0 || e >= p.experts) continue;
-    if (per_expert) atomicAdd(&per_expert[e], 1);
-    if (!per_rank) continue;
     const int to = quotient(e, per_size);
     bool counts = true;
     if (p.once && p.ranks <= 64) {
@@ -612,38 +611,68 @@ __device__ __forceinline__ int place_wave(int e, int experts, int lane, int* nex
   return place;
 }
 
-__device__ __forceinline__ int sum_before(int mine, int lane) {   // inclusive
+// The sum over this lane and the lanes before it.
+__device__ __forceinline__ int sum_before(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // 1, 2, 4, 8 lanes on, inside 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // the last lane of the 16 before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // lane 31
+  return v;
+}
+
+// The choices of a chunk, 64 at a time: all loads are on their way before
+// the first is used.
+constexpr int kChunk = 1024;
+struct Chunk {
+  int64_t from;             // first token
+  int n;                    // choices
+  int e[kChunk / 64];       // this lane's: choice 64 i + lane; -1 for none
+};
+__device__ __forceinline__ void load_chunk(const Plan& p, const int32_t* experts, int lane, Chunk* c) {
+  int64_t to;
+  chunk_bounds(p, blockIdx.x, &c->from, &to);
+  c->n = (int)(to - c->from) * p.top_k;
+  const int32_t* mine = experts + c->from * p.top_k;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(mine, o, 64);
-    if (lane >= o) mine += v;
-  }
-  return mine;
+  for (int i = 0; i < kChunk / 64; ++i) c->e[i] = i * 64 + lane < c->n ? mine[i * 64 + lane] : -1;
+#pragma unroll
+  for (int i = 0; i < kChunk / 64; ++i)
+    if (c->e[i] < 0 || c->e[i] >= p.experts) c->e[i] = -1;
 }
 
 __global__ __launch_bounds__(64) void dispatch_count_kernel(Plan p, const int32_t* __restrict__ experts,
                                                             int32_t* __restrict__ counts, int32_t* __restrict__ sent) {
   extern __shared__ int ints[];
   int* per_expert = ints;
-  int* per_rank = ints + p.experts;
+  int* per_rank = per_expert + p.experts;
+  int* row = per_rank + p.ranks;       // the chunk's choices
   const int lane = threadIdx.x;
+  Chunk c;
+  load_chunk(p, experts, lane, &c);
   for (int i = lane; i < p.experts + p.ranks; i += 64) ints[i] = 0;
   __syncthreads();
-  int64_t from, to;
-  chunk_bounds(p, blockIdx.x, &from, &to);
-  const float per_size = 1.0f / (p.experts / p.ranks);
-  for (int64_t t = from + lane; t < to; t += 64)
-    count_token(p, experts + t * p.top_k, per_size, per_expert, sent ? per_rank : nullptr);
+#pragma unroll
+  for (int i = 0; i < kChunk / 64; ++i) {
+    if (i * 64 >= c.n) break;
+    if (c.e[i] >= 0) atomicAdd(&per_expert[c.e[i]], 1);
+    row[i * 64 + lane] = c.e[i];
+  }
   __syncthreads();
   for (int e = lane; e < p.experts; e += 64) counts[(int64_t)blockIdx.x * p.experts + e] = per_expert[e];
-  if (sent)
-    for (int d = lane; d < p.ranks; d += 64) sent[(int64_t)blockIdx.x * p.ranks + d] = per_rank[d];
+  if (!sent) return;
+  const float per_size = 1.0f / (p.experts / p.ranks);
+  const int tokens = c.n / p.top_k;
+  for (int t = lane; t < tokens; t += 64) count_token(p, row + t * p.top_k, per_size, per_rank);
+  __syncthreads();
+  for (int d = lane; d < p.ranks; d += 64) sent[(int64_t)blockIdx.x * p.ranks + d] = per_rank[d];
 }
 
 // counts[chunk][e] becomes the sum over the chunks before: a workgroup takes
 // 16 experts, 64 threads each for as many runs of chunks.  Further
 // workgroups add up the traffic, 1,024 pairs of ranks each.
-constexpr int kScanExperts = 16;
+constexpr int kScanExperts = 16, kScanAhead = 16;
 __global__ __launch_bounds__(1024) void dispatch_scan_kernel(Plan p, int32_t* __restrict__ counts,
                                                              int32_t* __restrict__ totals,
                                                              const int32_t* __restrict__ sent, double row_bytes,
@@ -654,6 +683,7 @@ __global__ __launch_bounds__(1024) void dispatch_scan_kernel(Plan p, int32_t* __
     if (pair >= p.ranks * p.ranks) return;
     const int from = pair / p.ranks, to = pair % p.ranks;
     int64_t rows = 0;
+#pragma unroll 8
     for (int64_t c = 0; c < p.rank_chunks; ++c) rows += sent[(from * p.rank_chunks + c) * p.ranks + to];
     traffic[pair] = (double)rows * row_bytes;
     return;
@@ -661,21 +691,32 @@ __global__ __launch_bounds__(1024) void dispatch_scan_kernel(Plan p, int32_t* __
   __shared__ int runs[64][kScanExperts + 1];
   const int e = blockIdx.x * kScanExperts + tid % kScanExperts, run = tid / kScanExperts;
   const int64_t each = (p.chunks + 63) / 64, first = min(run * each, p.chunks), last = min(first + each, p.chunks);
-  int sum = 0;
+  // the run's first counts stay in registers, which is all of them up to
+  // 1,024 chunks
+  int ahead[kScanAhead], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kScanAhead; ++i) ahead[i] = e < p.experts && first + i < last ? counts[(first + i) * p.experts + e] : 0;
+#pragma unroll
+  for (int i = 0; i < kScanAhead; ++i) sum += ahead[i];
   if (e < p.experts)
-    for (int64_t c = first; c < last; ++c) sum += counts[c * p.experts + e];
+    for (int64_t c = first + kScanAhead; c < last; ++c) sum += counts[c * p.experts + e];
   runs[run][tid % kScanExperts] = sum;
   __syncthreads();
   // a wave per expert over its 64 runs
   const int lane = tid & 63, of = tid >> 6;
-  const int mine = runs[lane][of], upto = sum_before(mine, lane);
+  const int mine = runs[lane][of], upto = sum_before(mine);
   __syncthreads();
   runs[lane][of] = upto - mine;
   if (lane == 63 && blockIdx.x * kScanExperts + of < p.experts) totals[blockIdx.x * kScanExperts + of] = upto;
   __syncthreads();
   if (e >= p.experts) return;
   sum = runs[run][tid % kScanExperts];
-  for (int64_t c = first; c < last; ++c) {
+#pragma unroll
+  for (int i = 0; i < kScanAhead; ++i) {
+    if (first + i < last) counts[(first + i) * p.experts + e] = sum;
+    sum += ahead[i];
+  }
+  for (int64_t c = first + kScanAhead; c < last; ++c) {
     const int here = counts[c * p.experts + e];
     counts[c * p.experts + e] = sum;
     sum += here;
@@ -690,33 +731,41 @@ __global__ __launch_bounds__(64) void dispatch_place_kernel(Plan p, const int32_
                                                             int32_t* __restrict__ slot_of_choice) {
   extern __shared__ int next[];  // the next free slot of every expert
   const int lane = threadIdx.x;
+  Chunk c;
+  load_chunk(p, experts, lane, &c);
   int carry = 0;
-  for (int e0 = 0; e0 < p.experts; e0 += 64) {
-    const int e = e0 + lane, mine = e < p.experts ? totals[e] : 0, upto = sum_before(mine, lane);
-    if (e < p.experts) {
-      const int first = carry + upto - mine;
-      next[e] = first + counts[(int64_t)blockIdx.x * p.experts + e];
-      if (blockIdx.x == 0) offsets[e] = first;
+  for (int e0 = 0; e0 < p.experts; e0 += 256) {
+    int all[4], before[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = e0 + i * 64 + lane;
+      all[i] = e < p.experts ? totals[e] : 0;
+      before[i] = e < p.experts ? counts[(int64_t)blockIdx.x * p.experts + e] : 0;
     }
-    carry += __shfl(upto, 63, 64);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = e0 + i * 64 + lane, upto = sum_before(all[i]);
+      if (e < p.experts) {
+        const int first = carry + upto - all[i];
+        next[e] = first + before[i];
+        if (blockIdx.x == 0) offsets[e] = first;
+      }
+      carry += __builtin_amdgcn_readlane(upto, 63);
+    }
   }
   if (blockIdx.x == 0 && lane == 0) offsets[p.experts] = carry;
   // slots that no choice fills
   for (int64_t s = carry + (int64_t)blockIdx.x * 64 + lane; s < p.tokens * p.top_k; s += (int64_t)gridDim.x * 64)
     token_of_slot[s] = -1;
   __syncthreads();
-  int64_t from, to;
-  chunk_bounds(p, blockIdx.x, &from, &to);
-  const int32_t* mine = experts + from * p.top_k;
-  const int n = (int)(to - from) * p.top_k;     // at most 1,024, or one token's
   const float per_token = 1.0f / p.top_k;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    const int i = i0 + lane;
-    int e = i < n ? mine[i] : -1;
-    if (e >= p.experts || e < 0) e = -1;
-    const int slot = place_wave(e, p.experts, lane, next);
-    if (slot >= 0) token_of_slot[slot] = (int32_t)from + quotient(i, per_token);
-    if (i < n) slot_of_choice[from * p.top_k + i] = slot;
+#pragma unroll
+  for (int i = 0; i < kChunk / 64; ++i) {
+    const int at = i * 64 + lane;
+    if (i * 64 >= c.n) break;
+    const int slot = place_wave(c.e[i], p.experts, lane, next);
+    if (slot >= 0) token_of_slot[slot] = (int32_t)c.from + quotient(at, per_token);
+    if (at < c.n) slot_of_choice[c.from * p.top_k + at] = slot;
   }
 }
 
@@ -747,7 +796,7 @@ __global__ __launch_bounds__(1024) void dispatch_small_kernel(Plan p, const int3
   }
   if (traffic)
     for (int t = tid; t < p.tokens; t += 1024)
-      count_token(p, experts + (int64_t)t * p.top_k, per_size, nullptr, sent + t / p.per_rank * p.ranks);
+      count_token(p, experts + (int64_t)t * p.top_k, per_size, sent + t / (int)p.per_rank * p.ranks);
   __syncthreads();
   // counts to first places: over the waves, then over the experts
   int sum = 0;
@@ -757,7 +806,7 @@ __global__ __launch_bounds__(1024) void dispatch_small_kernel(Plan p, const int3
       counts[w * E + tid] = sum;
       sum += here;
     }
-  const int upto = sum_before(sum, lane);
+  const int upto = sum_before(sum);
   if (lane == 63) ends[wave] = upto;
   __syncthreads();
   int first = upto - sum, all = 0;
@@ -819,7 +868,7 @@ Plan make_plan(int32_t experts, int32_t top_k, int64_t tokens, int32_t ranks, in
   p.tokens = tokens;
   p.per_rank = per_rank < tokens ? per_rank : tokens;
   p.once = once;
-  p.chunk_tokens = 1024 / top_k;
+  p.chunk_tokens = kChunk / top_k;
   p.rank_chunks = ceil_div(p.per_rank, p.chunk_tokens);
   p.chunks = p.rank_chunks * ranks;
   p.small = tokens * top_k <= kSmallChoices && 16 * experts + ranks * ranks <= kSmallInts;
@@ -978,8 +1027,8 @@ extern "C" netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_
       int32_t* counts = static_cast<int32_t*>(d_work);
       int32_t* sent = counts + p.chunks * p.experts;
       int32_t* totals = sent + p.chunks * p.ranks;
-      hipLaunchKernelGGL(dispatch_count_kernel, dim3((unsigned)p.chunks), dim3(64), sizeof(int) * (experts + ranks), s,
-                         p, d_experts, counts, d_traffic ? sent : nullptr);
+      hipLaunchKernelGGL(dispatch_count_kernel, dim3((unsigned)p.chunks), dim3(64),
+                         sizeof(int) * (experts + ranks + kChunk), s, p, d_experts, counts, d_traffic ? sent : nullptr);
       const int64_t scans = ceil_div(experts, kScanExperts) + (d_traffic ? ceil_div((int64_t)ranks * ranks, 1024) : 0);
       hipLaunchKernelGGL(dispatch_scan_kernel, dim3((unsigned)scans), dim3(1024), 0, s, p, counts, totals, sent,
                          row_bytes, d_traffic);
