@@ -230,6 +230,7 @@ __device__ __forceinline__ Item segment(const int32_t* offsets, int e, int slots
 // is cut into equal parts of at most that many.
 struct Cut {
   int tile;          // rows and columns of dW a workgroup computes
+  int step;          // slots of one pass through shared memory
   int64_t longest;
   int64_t items, partials, joins;   // at most
   bool planned;      // whether the parts are laid out by plan_kernel
@@ -241,7 +242,7 @@ struct Cut {
 // the hot expert of 131,072 routed slots, 25,480 long, started last would
 // add 15%).
 // One workgroup with a thread per expert.
-__global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, int step, const int32_t* __restrict__ offsets,
+__global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, const int32_t* __restrict__ offsets,
                                                     Item* __restrict__ items, Join* __restrict__ joins) {
   __shared__ int length[1024], first_item[1024], first_partial[1024];
   __shared__ Item whole[1024];     // by place in the order; `partial` holds the slots of a part
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, int step, c
     it = segment(offsets, e, g.slots);
     const uint32_t n = it.to - it.from, longest = (uint32_t)cut.longest;
     parts = n > longest ? (n + longest - 1) / longest : 1;
-    each = ((n + parts - 1) / parts + step - 1) / step * step;
+    each = ((n + parts - 1) / parts + cut.step - 1) / cut.step * cut.step;
     if (parts > 1) parts = (n + each - 1) / each;
     it.partial = (int)each;
   }
@@ -583,10 +584,20 @@ constexpr int kMaxCols = 1 << 20;
 constexpr int64_t kMaxSlots = 0x7fffffff - 4096;   // a step past the end stays in 32 bits
 
 // How a call's sums are cut, from its sizes alone.
-Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols) {
+Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols, int32_t type) {
   Cut c{};
-  c.tile = ceil_div(n, 256) * ceil_div(cols, 256) * experts >= 512 ? 256 : 128;
+  // Tiles of 256 read half as much per product, those of 128 leave less over
+  // at the edges of dW and of the parts: with 4,096 slots (times the terms of
+  // dy) for each compute unit the larger ones are 14% faster, with 2,048 the
+  // smaller ones 5%, with 512 26%.
+  const int64_t terms = type == NETSIM_BF16 ? 1 : type == NETSIM_F16 ? 2 : 3;
+  c.tile = slots * terms * ceil_div(n, 256) * ceil_div(cols, 256) / 256 >= 3000 ? 256 : 128;
   const int64_t tiles = ceil_div(n, c.tile) * ceil_div(cols, c.tile);   // of one expert
+  // Steps of 64 slots keep a compute unit's shared memory to one workgroup,
+  // those of 32 leave room for two or three smaller ones, which takes many
+  // tiles to be of use: 2,048 tiles of 128 are 10% faster by 32 slots, 128 of
+  // them 13% slower.
+  c.step = terms == 1 && (c.tile == 256 || tiles * experts < 1024) ? 64 : 32;
   // the slots that each of the 256 compute units would have of one tile if
   // all were busy to the end; parts of a few steps cost more in partial sums
   // than they save
@@ -665,7 +676,7 @@ extern "C" int64_t netsim_act_weight_grad_work_bytes(int32_t experts, int64_t sl
   if (experts < 1 || experts > 1024 || slots < 0 || slots > kMaxSlots || n < 1 || n > kMaxCols || cols < 1 ||
       cols > kMaxCols || !type_ok(type))
     return -1;
-  return make_cut(experts, slots, n, cols).bytes;
+  return make_cut(experts, slots, n, cols, type).bytes;
 }
 
 extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts, int64_t slots, int32_t n,
@@ -691,21 +702,21 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
       return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or d_q or d_work to 16 bytes");
     const Grad g{experts, n, cols, (int)ceil_div(cols, kBlock), (int)slots, rows, ld_dy,
                  cols % 4 == 0 && aligned(d_dw, 4 * type_size(out_type))};
-    const Cut cut = make_cut(experts, slots, n, cols);
+    const Cut cut = make_cut(experts, slots, n, cols, type);
     return launch(what, device, [&] {
       with_type(type, [&](auto t) {
         with_type(out_type, [&](auto o) {
           using T = decltype(t);
           using O = decltype(o);
-          constexpr int KB = Terms<T>::value == 1 ? 64 : 32;
+          constexpr int LONG = Terms<T>::value == 1 ? 64 : 32;
           hipStream_t s = static_cast<hipStream_t>(hip_stream);
           Item* items = cut.planned ? static_cast<Item*>(d_work) : nullptr;
           Join* joins = reinterpret_cast<Join*>(items + cut.items);
           float* partials = reinterpret_cast<float*>(joins + cut.joins);
           if (cut.planned)
-            hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(experts, 64) * 64), 0, s, g, cut, KB, d_offsets, items, joins);
+            hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(experts, 64) * 64), 0, s, g, cut, d_offsets, items, joins);
           auto run = [&](auto kernel, int threads) {
-            const int lds = 2 * 2 * KB * (Terms<T>::value + 1) * (cut.tile + 32);
+            const int lds = 2 * 2 * cut.step * (Terms<T>::value + 1) * (cut.tile + 32);
             (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
             hipLaunchKernelGGL(kernel,
                                dim3((unsigned)(ceil_div(n, cut.tile) * ceil_div(cols, cut.tile)),
@@ -714,9 +725,9 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
                                d_row_of_slot, d_offsets, static_cast<O*>(d_dw), partials);
           };
           if (cut.tile == 256)
-            run(grad_kernel<T, O, 256, 256, 2, 4, KB>, 512);
+            run(grad_kernel<T, O, 256, 256, 2, 4, LONG>, 512);
           else
-            run(grad_kernel<T, O, 128, 128, 2, 2, KB>, 256);
+            run(cut.step == LONG ? grad_kernel<T, O, 128, 128, 2, 2, LONG> : grad_kernel<T, O, 128, 128, 2, 2, 32>, 256);
           if (cut.joins > 0) {
             // mostly there are few experts to join, or none: groups that find
             // nothing to do cost 4 us at 14,000 of them
