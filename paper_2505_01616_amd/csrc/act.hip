@@ -181,6 +181,9 @@ struct Grad {
   int experts, n, cols, blocks, slots;
   int64_t rows, ld;
   bool wide_stores;   // four columns of dW at a time are aligned
+  // -1: a slot's row is map[slot]; 0: the slot itself (map is then any word
+  // that may be read).  A mask, so that no branch parts the step's products.
+  int mapped;
 };
 
 // A part of an expert's slots.  partial < 0: the whole sum, written to dW;
@@ -374,7 +377,7 @@ template <class T, class O, int BN, int BC, int WN, int WC, int KB>
 __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* __restrict__ items,
                                                             const T* __restrict__ dy, const int8_t* __restrict__ q,
                                                             const int8_t* __restrict__ exponents,
-                                                            const int32_t* __restrict__ row_of_slot,
+                                                            const int32_t* __restrict__ map,
                                                             const int32_t* __restrict__ offsets, O* __restrict__ dw,
                                                             float* __restrict__ partials) {
   constexpr int THREADS = 64 * WN * WC, TERMS = Terms<T>::value;
@@ -405,6 +408,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
   // chunk then reads into the next row, so not where there is none.
   const int plain_to = it.to - (it.to == g.slots && g.n % 8 != 0);
   const bool y_wide = g.n >= 8;
+  const uint32_t row_limit = (uint32_t)min(g.rows, (int64_t)0x80000000);
   Eight<T> y[NY];
   uint4 x[NX];
   int row[NX];
@@ -415,7 +419,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
 #pragma unroll
     for (int i = 0; i < NX; ++i) {
       const int s = s0 + x_row + i * (THREADS / CX);
-      row[i] = row_of_slot ? row_of_slot[min(s, it.to - 1)] : s;   // not looked at before the next step
+      row[i] = map[min(s, it.to - 1) & g.mapped];   // not looked at before the next step
     }
   };
   auto load_y = [&](int s0, int i, bool plain) {
@@ -426,8 +430,10 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
       y[i] = load_some(from, s0 + y_row + i * (THREADS / CY) < it.to ? y_left : 0);
   };
   auto load_x = [&](int s0, int i) {
-    held[i] = s0 + x_row + i * (THREADS / CX) < it.to && row[i] >= 0 && row[i] < g.rows;
-    const int64_t block = (held[i] ? (int64_t)row[i] : 0) * g.blocks + x_at;
+    // no conditions that branch: the products on both sides stay one block
+    const int s = s0 + x_row + i * (THREADS / CX), r = (row[i] & g.mapped) | (s & ~g.mapped);
+    held[i] = (s < it.to) & ((uint32_t)r < row_limit);
+    const int64_t block = (int64_t)(held[i] ? r : 0) * g.blocks + x_at;
     x[i] = *reinterpret_cast<const uint4*>(q + block * kBlock + (x_chunk & 1) * 16);
     e[i] = (uint8_t)exponents[block];
   };
@@ -701,7 +707,7 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
         !aligned(d_row_of_slot, 4) || !aligned(d_offsets, 4) || !aligned(d_work, 16))
       return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or d_q or d_work to 16 bytes");
     const Grad g{experts, n, cols, (int)ceil_div(cols, kBlock), (int)slots, rows, ld_dy,
-                 cols % 4 == 0 && aligned(d_dw, 4 * type_size(out_type))};
+                 cols % 4 == 0 && aligned(d_dw, 4 * type_size(out_type)), d_row_of_slot ? -1 : 0};
     const Cut cut = make_cut(experts, slots, n, cols, type);
     return launch(what, device, [&] {
       with_type(type, [&](auto t) {
@@ -722,7 +728,7 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
                                dim3((unsigned)(ceil_div(n, cut.tile) * ceil_div(cols, cut.tile)),
                                     (unsigned)(cut.planned ? cut.items : experts)),
                                dim3(threads), lds, s, g, items, static_cast<const T*>(d_dy), d_q, d_exponents,
-                               d_row_of_slot, d_offsets, static_cast<O*>(d_dw), partials);
+                               d_row_of_slot ? d_row_of_slot : d_offsets, d_offsets, static_cast<O*>(d_dw), partials);
           };
           if (cut.tile == 256)
             run(grad_kernel<T, O, 256, 256, 2, 4, LONG>, 512);
