@@ -180,7 +180,7 @@ using lds_s16x4 = __attribute__((address_space(3))) s16x4;
 struct Grad {
   int experts, n, cols, blocks, slots;
   int64_t rows, ld;
-  bool wide_stores;   // four columns of dW at a time are aligned
+  bool wide_joins;   // four elements of dW at a time are aligned
   // -1: a slot's row is map[slot]; 0: the slot itself (map is then any word
   // that may be read).  A mask, so that no branch parts the step's products.
   int mapped;
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256) void join_kernel(Grad g, const Join* __restric
   for (int64_t i0 = (int64_t)blockIdx.x * 256; i0 < size; i0 += (int64_t)gridDim.x * 256) {
     const int64_t i = i0 + lane * 4;
     float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (g.wide_stores) {
+    if (g.wide_joins) {
       if (i < size) {
 #pragma unroll 4
         for (int p = quarter; p < j.parts; p += 4) {
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256) void join_kernel(Grad g, const Join* __restric
 #pragma unroll
       for (int h = 0; h < 4; ++h)
         four.v[h] = (O)((sums[0][lane][h] + sums[1][lane][h]) + (sums[2][lane][h] + sums[3][lane][h]));
-      if (g.wide_stores) {
+      if (g.wide_joins) {
         *reinterpret_cast<Four*>(out + i) = four;
       } else {
         for (int h = 0; h < 4; ++h)
@@ -553,31 +553,51 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
     for (; s0 + 3 * KB <= plain_to; turn()) step(s0, stage, next, std::true_type{});
   for (; s0 < it.to; turn()) step(s0, stage, next, std::false_type{});
 
+  // The tile leaves through shared memory, so that rows are written as whole
+  // lines.  64 experts of 8 slots each, 2,048 x 2,048 in bfloat16 (537 MB):
+  // 116 us, and 193 us when every lane wrote the four columns that it holds.
   auto write = [&](auto* out) {
     using D = std::remove_reference_t<decltype(*out)>;
+    constexpr int V = 16 / sizeof(D), PITCH = BC + V;
+    constexpr int FIT = 2 * STAGE * (int)sizeof(bf16) / (PITCH * (int)sizeof(D));
+    constexpr int ROWS = FIT >= BN ? BN : FIT >= BN / 2 ? BN / 2 : BN / 4;   // of a pass
+    static_assert(ROWS % 32 == 0 && ROWS <= FIT, "");
+    D* tile = reinterpret_cast<D*>(shared);
+    const bool wide = g.cols % V == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int n = n0 + wn + j * 32 + (lane & 31);
-      if (n >= g.n) continue;
+    for (int first = 0; first < BN; first += ROWS) {
+      if (first > 0) __syncthreads();
 #pragma unroll
-      for (int i = 0; i < FC; ++i)
+      for (int j = 0; j < FN; ++j) {
+        const int n = wn + j * 32 - first;
+        if (n < 0 || n >= ROWS) continue;   // the same for a wave
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const int c = c0 + wc + i * 32 + r * 2 + (lane >> 5) * 4;
-          D* to = out + (int64_t)n * g.cols + c;
-          if (g.wide_stores) {
+        for (int i = 0; i < FC; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
             struct alignas(4 * sizeof(D)) Four {
               D v[4];
             } four;
 #pragma unroll
             for (int h = 0; h < 4; ++h) four.v[h] = (D)acc[i][j][r + h];
-            if (c < g.cols) *reinterpret_cast<Four*>(to) = four;
-          } else {
-#pragma unroll
-            for (int h = 0; h < 4; ++h)
-              if (c + h < g.cols) to[h] = (D)acc[i][j][r + h];
+            *reinterpret_cast<Four*>(tile + (n + (lane & 31)) * PITCH + wc + i * 32 + r * 2 + (lane >> 5) * 4) = four;
           }
+      }
+      __syncthreads();
+      if (wide) {
+#pragma unroll 4
+        for (int i = tid; i < ROWS * BC / V; i += THREADS) {
+          const int row = i / (BC / V), c = i % (BC / V) * V, n = n0 + first + row;
+          if (n < g.n && c0 + c < g.cols)
+            *reinterpret_cast<uint4*>(out + (int64_t)n * g.cols + c0 + c) = *reinterpret_cast<const uint4*>(tile + row * PITCH + c);
         }
+      } else {
+#pragma unroll 4
+        for (int i = tid; i < ROWS * BC; i += THREADS) {
+          const int row = i / BC, c = i % BC, n = n0 + first + row;
+          if (n < g.n && c0 + c < g.cols) out[(int64_t)n * g.cols + c0 + c] = tile[row * PITCH + c];
+        }
+      }
     }
   };
   if (it.partial < 0)

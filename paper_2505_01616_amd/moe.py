@@ -201,8 +201,9 @@ def weight_grad(saved: Saved, dy: torch.Tensor, offsets: torch.Tensor, row_of_sl
     work = max(0, ns.netsim_act_weight_grad_work_bytes(experts, slots, n, saved.cols, kind))
     index, stream = _at(device)
     out = torch.empty((experts, n, saved.cols), dtype=out_dtype, device=device)
-    space = torch.empty(work, dtype=torch.uint8, device=device)
+    space = torch.empty(work, dtype=torch.uint8, device=device) if work else None
     ns.netsim_act_weight_grad(index, experts, slots, n, saved.cols, kind, dy.data_ptr(), ld, rows, saved.q.data_ptr(),
                               saved.exponents.data_ptr(), None if row_of_slot is None else row_of_slot.data_ptr(),
-                              offsets.data_ptr(), _TYPES[out_dtype], out.data_ptr(), space.data_ptr(), work, stream)
+                              offsets.data_ptr(), _TYPES[out_dtype], out.data_ptr(),
+                              None if space is None else space.data_ptr(), work, stream)
     return out
