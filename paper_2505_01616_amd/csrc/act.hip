@@ -210,15 +210,8 @@ struct Terms<f16> {
   static constexpr int value = 2;
 };
 
-// The leading 8 significant bits of y, the rest cut off (never an overflow,
-// and the rest is exact); a NaN stays one.
-__device__ __forceinline__ float top_bits(float y) {
-  uint32_t b = __float_as_uint(y);
-  b |= isnan(y) ? 0x400000u : 0u;
-  return __uint_as_float(b & 0xffff0000u);
-}
-
-// Two floats of at most 8 significant bits as bfloat16, a in the low half.
+// The upper halves of two floats: bfloat16 with what does not fit cut off
+// (never an overflow), a in the low half.
 __device__ __forceinline__ uint32_t pack(float a, float b) {
   return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
 }
@@ -387,6 +380,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
   constexpr int CY = BN / 8, NY = KB * CY / THREADS, CX = BC / 16, NX = KB * CX / THREADS;
   constexpr int FN = BN / WN / 32, FC = BC / WC / 32;
   static_assert(THREADS % CY == 0 && THREADS % CX == 0 && NY * THREADS == KB * CY && NX * THREADS == KB * CX, "");
+  constexpr float MOST = sizeof(T) == 2 ? 65504.0f : 3.402823466e38f;
   extern __shared__ __align__(16) bf16 shared[];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -442,20 +436,25 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
     if constexpr (TERMS == 1) {
       *reinterpret_cast<uint4*>(stage + k * PY + y_chunk * 8) = make_uint4(y[i].w[0], y[i].w[1], y[i].w[2], y[i].w[3]);
     } else {
-      float v[8];
+      // Each term is the leading 8 bits of what the terms before leave, cut
+      // off, so the rest is exact.  The rests are taken of the value held to
+      // finite numbers: an infinity stays one, and a NaN's first term (its
+      // quiet bit set) is one.
+      float first[8], v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = value_of(y[i], j);
+      for (int j = 0; j < 8; ++j) {
+        first[j] = __builtin_canonicalizef(value_of(y[i], j));
+        v[j] = __builtin_amdgcn_fmed3f(first[j], -MOST, MOST);
+      }
 #pragma unroll
       for (int t = 0; t < TERMS; ++t) {
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-          const float a = top_bits(v[j]), b = top_bits(v[j + 1]);
-          w[j / 2] = pack(a, b);
-          v[j] = isfinite(a) ? v[j] - a : 0.0f;
-          v[j + 1] = isfinite(b) ? v[j + 1] - b : 0.0f;
-        }
+        for (int j = 0; j < 8; j += 2) w[j / 2] = t == 0 ? pack(first[j], first[j + 1]) : pack(v[j], v[j + 1]);
         *reinterpret_cast<uint4*>(stage + (t * KB + k) * PY + y_chunk * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (t + 1 < TERMS)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] -= __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u);
       }
     }
   };
