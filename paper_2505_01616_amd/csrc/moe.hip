@@ -237,12 +237,17 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
 
   float x[N], top = kNone;
   R::load(x_row, r.experts, j, wide, x);
-  const int undefined = r.softmax ? 0x203 : 0x003;   // NaN, and plus infinity
+  // a NaN, and plus infinity under softmax, make the scores or their sum NaN;
+  // where neither is formed the logits are looked at
   bool bad = false;
+  const bool sum_all = r.softmax && (BY_SCORE || !r.renorm);
+  if (!BY_SCORE && !sum_all) {
+    const int undefined = r.softmax ? 0x203 : 0x003;
 #pragma unroll
-  for (int i = 0; i < N; ++i) bad |= __builtin_amdgcn_classf(x[i], undefined);
+    for (int i = 0; i < N; ++i) bad |= __builtin_amdgcn_classf(x[i], undefined);
+  }
   float base = 0.0f, z = 1.0f;
-  if (r.softmax && (BY_SCORE || !r.renorm)) {
+  if (sum_all) {
 #pragma unroll
     for (int i = 0; i < N; ++i) top = fmaxf(top, x[i]);
     top = max_over<L>(top);
@@ -251,6 +256,7 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
 #pragma unroll
     for (int i = 0; i < N; ++i) z += exp_near(x[i] - base);
     z = sum_over<L>(z);
+    bad = isnan(z);
   }
   if constexpr (BY_SCORE) {
     const float inverse = 1.0f / z;
@@ -303,11 +309,17 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const float per = 1.0f / size;
+    const bool aligned = size % R::V == 0;   // a vector lies in one group
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int e = R::element(i, j);
-      // (e + 1/2) / size in 32 bits is never off by half a step below 2^10
-      if (e < r.experts && keep[(int)((e + 0.5f) * per)] == 0.0f) x[i] = kNone;
+    for (int i = 0; i < N; i += R::V) {
+      float kept = 1.0f;
+#pragma unroll
+      for (int h = 0; h < R::V; ++h) {
+        const int e = R::element(i + h, j);
+        // (e + 1/2) / size in 32 bits is never off by half a step below 2^10
+        if ((h == 0 || !aligned) && e < r.experts) kept = keep[(int)((e + 0.5f) * per)];
+        x[i + h] = kept == 0.0f ? kNone : x[i + h];
+      }
     }
   }
 
