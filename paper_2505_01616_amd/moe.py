@@ -191,7 +191,7 @@ def weight_grad(saved: Saved, dy: torch.Tensor, offsets: torch.Tensor, row_of_sl
     ld = _rows("dy", dy, _TYPES)
     slots, n = dy.shape
     device = dy.device
-    experts = offsets.numel() - 1
+    experts = max(0, offsets.numel() - 1)
     _flat("offsets", offsets, torch.int32, (experts + 1,), device)
     if row_of_slot is not None:
         _flat("row_of_slot", row_of_slot, torch.int32, (slots,), device)
