@@ -606,19 +606,28 @@ __device__ __forceinline__ void count_token(const Plan& p, const int32_t* row, f
   }
 }
 
-// The places of 64 choices (e < 0: none), each behind the wave's earlier ones
-// of its expert: next[e] is the expert's next place and moves on.
-__device__ __forceinline__ int place_wave(int e, int experts, int lane, int* next) {
-  uint64_t same = __ballot(e >= 0);  // lanes with this lane's expert
-  for (int bit = 0; (1 << bit) < experts; ++bit) {
-    const bool mine = (e >> bit) & 1;
-    const uint64_t set = __ballot(mine);
-    same &= mine ? set : ~set;
+// The places of 64 choices (e < 0: none) of fewer than 2^BITS experts, each
+// behind the wave's earlier ones of its expert: next[e] is the expert's next
+// place and moves on.  Lanes of the same expert agree in every bit; with the
+// number of bits known the ballots overlap (a loop over them took twice as
+// long).
+template <int BITS>
+__device__ __forceinline__ int place_wave(int e, int lane, int* next) {
+  const uint64_t some = __ballot(e >= 0);
+  uint32_t low = (uint32_t)some, high = (uint32_t)(some >> 32);
+#pragma unroll
+  for (int bit = 0; bit < BITS; ++bit) {
+    const int mine = __builtin_amdgcn_sbfe(e, bit, 1);   // 0 or -1
+    const uint64_t set = __ballot(mine != 0);
+    low &= ~((uint32_t)set ^ (uint32_t)mine);
+    high &= ~((uint32_t)(set >> 32) ^ (uint32_t)mine);
   }
+  const int before = (int)__builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0));
+  const int all = __popc(low) + __popc(high);
   int place = -1;
-  if (e >= 0) place = next[e] + __popcll(same & ((1ull << lane) - 1));
+  if (e >= 0) place = next[e] + before;
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (e >= 0 && (same >> lane) == 1) next[e] = place + 1;  // the last lane of its expert
+  if (e >= 0 && before + 1 == all) next[e] = place + 1;  // the last lane of its expert
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   return place;
 }
@@ -735,6 +744,7 @@ __global__ __launch_bounds__(1024) void dispatch_scan_kernel(Plan p, int32_t* __
   }
 }
 
+template <int BITS>
 __global__ __launch_bounds__(64) void dispatch_place_kernel(Plan p, const int32_t* __restrict__ experts,
                                                             const int32_t* __restrict__ counts,
                                                             const int32_t* __restrict__ totals,
@@ -775,7 +785,7 @@ __global__ __launch_bounds__(64) void dispatch_place_kernel(Plan p, const int32_
   for (int i = 0; i < kChunk / 64; ++i) {
     const int at = i * 64 + lane;
     if (i * 64 >= c.n) break;
-    const int slot = place_wave(c.e[i], p.experts, lane, next);
+    const int slot = place_wave<BITS>(c.e[i], lane, next);
     if (slot >= 0) token_of_slot[slot] = (int32_t)c.from + quotient(at, per_token);
     if (at < c.n) slot_of_choice[c.from * p.top_k + at] = slot;
   }
@@ -783,6 +793,7 @@ __global__ __launch_bounds__(64) void dispatch_place_kernel(Plan p, const int32_
 
 // All of it in one workgroup: at most kSmallChoices choices, a sixteenth of
 // them per wave, and a traffic matrix that shared memory holds.
+template <int BITS>
 __global__ __launch_bounds__(1024) void dispatch_small_kernel(Plan p, const int32_t* __restrict__ experts,
                                                               int32_t* __restrict__ offsets,
                                                               int32_t* __restrict__ token_of_slot,
@@ -838,7 +849,7 @@ __global__ __launch_bounds__(1024) void dispatch_small_kernel(Plan p, const int3
   for (int h = 0; h < kSmallChoices / 1024; ++h) {
     if (h * 64 >= each) break;
     const int i = wave * each + h * 64 + lane;
-    const int slot = place_wave(mine[h], E, lane, counts + wave * E);
+    const int slot = place_wave<BITS>(mine[h], lane, counts + wave * E);
     if (slot >= 0) token_of_slot[slot] = quotient(i, per_token);
     if (i < n) slot_of_choice[i] = slot;
   }
@@ -1031,9 +1042,11 @@ extern "C" netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_
         return;
       }
       if (p.small) {
-        hipLaunchKernelGGL(dispatch_small_kernel, dim3(1), dim3(1024),
-                           sizeof(int) * (16 * experts + (d_traffic ? ranks * ranks : 0)), s, p, d_experts, d_offsets,
-                           d_token_of_slot, d_slot_of_choice, row_bytes, d_traffic);
+        auto run = [&](auto kernel) {
+          hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), sizeof(int) * (16 * experts + (d_traffic ? ranks * ranks : 0)),
+                             s, p, d_experts, d_offsets, d_token_of_slot, d_slot_of_choice, row_bytes, d_traffic);
+        };
+        run(experts <= 64 ? dispatch_small_kernel<6> : experts <= 256 ? dispatch_small_kernel<8> : dispatch_small_kernel<10>);
         return;
       }
       int32_t* counts = static_cast<int32_t*>(d_work);
@@ -1044,8 +1057,11 @@ extern "C" netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_
       const int64_t scans = ceil_div(experts, kScanExperts) + (d_traffic ? ceil_div((int64_t)ranks * ranks, 1024) : 0);
       hipLaunchKernelGGL(dispatch_scan_kernel, dim3((unsigned)scans), dim3(1024), 0, s, p, counts, totals, sent,
                          row_bytes, d_traffic);
-      hipLaunchKernelGGL(dispatch_place_kernel, dim3((unsigned)p.chunks), dim3(64), sizeof(int) * experts, s, p,
-                         d_experts, counts, totals, d_offsets, d_token_of_slot, d_slot_of_choice);
+      auto place = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)p.chunks), dim3(64), sizeof(int) * experts, s, p, d_experts, counts,
+                           totals, d_offsets, d_token_of_slot, d_slot_of_choice);
+      };
+      place(experts <= 64 ? dispatch_place_kernel<6> : experts <= 256 ? dispatch_place_kernel<8> : dispatch_place_kernel<10>);
     });
   });
 }
