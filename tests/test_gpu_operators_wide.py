@@ -24,6 +24,9 @@ ROUTERS = [
     (dict(experts=256, top_k=8, scores="sigmoid", groups=8, groups_kept=4, group_best=2, scale=2.5), 16385),
     (dict(experts=250, top_k=20, groups=25, groups_kept=10, group_best=2), 16500),
     (dict(experts=256, top_k=1), 16390),
+    (dict(experts=1024, top_k=8), 3001),
+    (dict(experts=1000, top_k=16, scores="sigmoid", scale=0.5), 2501),
+    (dict(experts=513, top_k=3, scores="sigmoid", renormalise=False), 2500),
 ]
 
 
