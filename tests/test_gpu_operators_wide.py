@@ -126,3 +126,73 @@ def test_dispatch(gpu, tokens, k, experts, ranks, per, once):  # noqa: F811
     want = plain.dispatch(e, experts, ranks, per or -(-tokens // ranks), 3.0, once)
     for name, g, w in zip(got._fields, got, want):
         np.testing.assert_array_equal(g.cpu().numpy(), w, err_msg=name)
+
+
+def test_weight_grad_against_differences(gpu):  # noqa: F811
+    """L(W) = sum over slots of dy_s . (W_e x_row(s)) is linear in W, so its
+    central differences are its gradient whatever the step (64-bit sums)."""
+    torch, moe = gpu
+    rng = np.random.default_rng(11)
+    off, token, (q, e) = grad_case(rng, 60, 2, 3, 20, 45)
+    dy = rng.normal(0, 1, (120, 20)).astype(np.float32)
+    saved = moe.Saved(torch.from_numpy(q).cuda(), torch.from_numpy(e).cuda(), 45)
+    got = host(moe.weight_grad(saved, torch.from_numpy(dy).cuda(), torch.from_numpy(off).int().cuda(),
+                               torch.from_numpy(token).int().cuda()))
+    x = plain.restore(q, e, 45)
+    expert = np.repeat(np.arange(3), np.diff(off))
+    slots = np.arange(off[-1])
+
+    def loss(w):
+        return np.einsum("si,sic,sc->", dy[slots].astype(np.float64), w[expert], x[token[slots]])
+
+    w = rng.normal(0, 1, (3, 20, 45))
+    size = plain.weight_grad(np.abs(x), np.abs(dy), off, token)
+    for _ in range(40):
+        at = (rng.integers(3), rng.integers(20), rng.integers(45))
+        up, down = w.copy(), w.copy()
+        up[at] += 0.5
+        down[at] -= 0.5
+        # the difference of two 64-bit sums of about 10^5 terms
+        assert abs(got[at] - (loss(up) - loss(down))) <= 130 * U * size[at] + 1e-8
+
+
+def test_operators_of_nothing(gpu):  # noqa: F811
+    torch, moe = gpu
+    r = moe.Router(8, 2)
+    none = torch.empty((0, 8), device="cuda")
+    e, w = moe.route(r, none)
+    assert e.shape == w.shape == (0, 2)
+    assert moe.route_backward(r, none, e, w).shape == (0, 8)
+    saved = moe.save(none)
+    assert moe.restore(saved).shape == (0, 8)
+    # slots whose rows do not exist count as zeros
+    off = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    got = moe.weight_grad(saved, torch.ones((3, 4), device="cuda"), off)
+    assert got.shape == (1, 4, 8) and (got == 0).all()
+
+
+def test_rows_past_32_bit_offsets(gpu):  # noqa: F811
+    """More than 2^31 saved values, and gradients in rows 60,000 apart."""
+    torch, moe = gpu
+    rows, cols = 60000, 40000
+    try:
+        x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+        dy = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")[:, :16]
+    except torch.cuda.OutOfMemoryError:
+        pytest.skip("no memory for it")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x[-1] = torch.randn(cols, generator=g, device="cuda").to(torch.bfloat16)
+    dy[-1] = torch.randn(16, generator=g, device="cuda").to(torch.bfloat16)
+    dy[0] = dy[-1]
+    saved = moe.save(x)
+    last = plain.restore(*plain.save(host(x[-1:])), cols)
+    assert (saved.q[:-1].max() == 0) and np.array_equal(host(moe.restore(saved)[-1:]), last)
+    # slot rows - 1 reads its own row, the last; slot 0 row 0 (zeros), then the last as well
+    off = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    once = host(moe.weight_grad(saved, dy, off))[0]
+    want = host(dy[-1])[:, None] * last
+    assert np.array_equal(once, want)       # one product each, of 15 bits
+    row = torch.arange(rows, dtype=torch.int32, device="cuda")
+    row[0] = rows - 1
+    twice = host(moe.weight_grad(saved, dy, off, row))[0]
+    assert np.array_equal(twice, 2 * want)
