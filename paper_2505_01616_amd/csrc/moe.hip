@@ -588,7 +588,10 @@ struct Plan {
   bool once;
   bool small;                 // one workgroup does it all
 };
-constexpr int kSmallChoices = 4096, kSmallInts = 16000;   // 64 KB of shared memory
+// One launch is shorter to enqueue than three: 8,192 choices of 256 experts
+// take 14.5 us a call in one workgroup and 19 in three launches, 16,384 take 22
+// and 19.
+constexpr int kSmallChoices = 8192, kSmallInts = 16000;   // 64 KB of shared memory
 
 __device__ __forceinline__ void chunk_bounds(const Plan& p, int64_t chunk, int64_t* from, int64_t* to) {
   const int64_t rank = chunk / p.rank_chunks, part = chunk % p.rank_chunks;

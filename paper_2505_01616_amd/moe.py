@@ -139,11 +139,13 @@ def dispatch(experts: torch.Tensor, num_experts: int, ranks: int = 1, tokens_per
     per = tokens_per_rank if tokens_per_rank is not None else max(1, -(-tokens // max(1, ranks)))
     work = max(0, ns.netsim_dispatch_work_bytes(num_experts, top_k, tokens, ranks, per))
     index, stream = _at(device)
-    out = Dispatch(torch.empty(max(0, num_experts) + 1, dtype=torch.int32, device=device),
-                   torch.empty(tokens * top_k, dtype=torch.int32, device=device),
-                   torch.empty((tokens, top_k), dtype=torch.int32, device=device),
+    # the whole numbers and the workspace are one allocation: each more would
+    # cost a tenth of a small call
+    whole = torch.empty(max(0, num_experts) + 1 + 2 * tokens * top_k + work // 4, dtype=torch.int32, device=device)
+    offsets, token_of_slot, slot_of_choice, space = whole.split_with_sizes(
+        (max(0, num_experts) + 1, tokens * top_k, tokens * top_k, work // 4))
+    out = Dispatch(offsets, token_of_slot, slot_of_choice.view(tokens, top_k),
                    torch.empty((max(0, ranks), max(0, ranks)), dtype=torch.float64, device=device))
-    space = torch.empty(work, dtype=torch.uint8, device=device)
     ns.netsim_dispatch(index, num_experts, top_k, tokens, experts.data_ptr(), ranks, per, row_bytes,
                        int(once_per_rank), out.offsets.data_ptr(), out.token_of_slot.data_ptr(),
                        out.slot_of_choice.data_ptr(), out.traffic.data_ptr(), space.data_ptr(), work, stream)
