@@ -239,8 +239,11 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
   const int64_t row = at < tokens ? at : tokens - 1;   // lanes beyond repeat the last row and write nothing
   const T* x_row = logits + row * ld;
 
-  float x[N], top = kNone;
+  float x[N], add[N], top = kNone;
   R::load(x_row, r.experts, j, wide, x);
+  if constexpr (BY_SCORE)   // here, where nothing waits for it yet
+#pragma unroll
+    for (int i = 0; i < N; ++i) add[i] = bias && R::element(i, j) < r.experts ? bias[R::element(i, j)] : 0.0f;
   // a NaN, and plus infinity under softmax, make the scores or their sum NaN;
   // where neither is formed the logits are looked at
   bool bad = false;
@@ -264,12 +267,19 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
   }
   if constexpr (BY_SCORE) {
     const float inverse = 1.0f / z;
+    float c[N];
+    if (r.softmax) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) c[i] = exp_of(x[i] - base) * inverse;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) c[i] = sigmoid(x[i]);
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (x[i] == kNone) continue;
-      x[i] = r.softmax ? exp_of(x[i] - base) * inverse : sigmoid(x[i]);
-      if (bias) x[i] += bias[R::element(i, j)];
-      bad |= isnan(x[i]);
+      const float value = c[i] + add[i];
+      bad |= x[i] != kNone && isnan(value);
+      x[i] = x[i] == kNone ? kNone : value;
     }
   }
 
