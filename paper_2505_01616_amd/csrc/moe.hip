@@ -286,13 +286,13 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
   if (r.groups > 1) {
     // the row's choice values in shared memory; as many lanes as there are
     // for each group look through its members
-    const int size = r.experts / r.groups, pitch = r.experts + 1;
+    const int size = r.experts / r.groups;
+    constexpr int pitch = L * N + 1;   // places beyond the experts hold minus infinity
     float* row_c = shared + (threadIdx.x / L) * (pitch + 2 * r.groups);
     float* score = row_c + pitch;
     float* keep = score + r.groups;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (R::element(i, j) < r.experts) row_c[R::element(i, j)] = x[i];
+    for (int i = 0; i < N; ++i) row_c[R::element(i, j)] = x[i];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     int share = 1;   // lanes of a group, a power of two
     while (2 * share * r.groups <= L) share *= 2;
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
       for (int h = 0; h < R::V; ++h) {
         const int e = R::element(i + h, j);
         // (e + 1/2) / size in 32 bits is never off by half a step below 2^10
-        if ((h == 0 || !aligned) && e < r.experts) kept = keep[(int)((e + 0.5f) * per)];
+        if (h == 0 || !aligned) kept = keep[min((int)((e + 0.5f) * per), r.groups - 1)];
         x[i + h] = kept == 0.0f ? kNone : x[i + h];
       }
     }
@@ -961,7 +961,7 @@ extern "C" netsim_status netsim_route(int32_t device, const netsim_router* route
         with_shape(tokens, r.experts, [&](auto l, auto n) {
           using T = decltype(t);
           constexpr int L = decltype(l)::value, N = decltype(n)::value;
-          const size_t lds = r.groups > 1 ? 256 / L * sizeof(float) * (r.experts + 1 + 2 * r.groups) : 0;
+          const size_t lds = r.groups > 1 ? 256 / L * sizeof(float) * (L * N + 1 + 2 * r.groups) : 0;
           auto run = [&](auto kernel) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), lds,
                                static_cast<hipStream_t>(hip_stream), r, tokens, static_cast<const T*>(d_logits),
