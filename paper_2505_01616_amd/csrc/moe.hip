@@ -29,16 +29,12 @@ __device__ __forceinline__ float moved(float old, float v) {
   return __int_as_float(moved<CTRL, ROWS>(__float_as_int(old), __float_as_int(v)));
 }
 template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t moved(uint32_t old, uint32_t v) {
-  return (uint32_t)moved<CTRL, ROWS>((int)old, (int)v);
-}
-template <int CTRL, int ROWS>
 __device__ __forceinline__ double moved(double old, double v) {
   const long long o = __double_as_longlong(old), b = __double_as_longlong(v);
   const int lo = moved<CTRL, ROWS>((int)o, (int)b), hi = moved<CTRL, ROWS>((int)(o >> 32), (int)(b >> 32));
   return __longlong_as_double((long long)hi << 32 | (unsigned)lo);
 }
-__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return __builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 __device__ __forceinline__ float last_lane(float v) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63)); }
 __device__ __forceinline__ double last_lane(double v) {
   const long long b = __double_as_longlong(v);
@@ -102,23 +98,26 @@ template <class T, int L, int N>
 struct Row {
   static constexpr int V = N < (int)(16 / sizeof(T)) ? N : (int)(16 / sizeof(T));
   static __device__ __forceinline__ int element(int i, int j) { return (i / V * L + j) * V + i % V; }
-  // wide: every vector lies wholly inside or outside the row, and is aligned
-  static __device__ __forceinline__ void load(const T* row, int n, int j, bool wide, float (&x)[N]) {
+  struct alignas(V * sizeof(T)) Vector {
+    T v[V];
+  };
+  // Places beyond the row hold minus infinity.  wide: every vector lies
+  // wholly inside or outside the row, and is aligned.
+  static __device__ __forceinline__ void load(const T* row, int n, int j, bool wide, Vector (&in)[N / V], float (&x)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; i += V) {
-      const int e = element(i, j);
-      struct alignas(V * sizeof(T)) Vector {
-        T v[V];
-      } in;
+    for (int i = 0; i < N / V; ++i) {
+      const int e = element(i * V, j);
+#pragma unroll
+      for (int h = 0; h < V; ++h) in[i].v[h] = (T)kNone;
       if (wide) {
-        if (e < n) in = *reinterpret_cast<const Vector*>(row + e);
+        if (e < n) in[i] = *reinterpret_cast<const Vector*>(row + e);
       } else {
 #pragma unroll
         for (int h = 0; h < V; ++h)
-          if (e + h < n) in.v[h] = row[e + h];
+          if (e + h < n) in[i].v[h] = row[e + h];
       }
 #pragma unroll
-      for (int h = 0; h < V; ++h) x[i + h] = e + h < n ? (float)in.v[h] : kNone;
+      for (int h = 0; h < V; ++h) x[i * V + h] = (float)in[i].v[h];
     }
   }
 };
@@ -135,10 +134,11 @@ struct Row {
 // Bound by instructions per row: few lanes per row mean few exchanges (8
 // lanes: three per choice, eight rows at once), many lanes mean short sorts
 // and enough waves where rows are few.  262,144 rows of 128 bfloat16 logits,
-// six choices: 29 us (2.7 TB/s), 568 vector instructions per eight rows, which
-// at four cycles each are that time.  16,384 rows of 256 float32 logits,
-// sigmoid scores, a bias and groups: 14.5 us, 1,227 instructions per four rows,
-// 9 us of it; the rest is the groups' passes through shared memory.
+// six choices: 27 us (2.9 TB/s), 507 vector instructions per eight rows, 16 of
+// them exponentials at a quarter of the rate: 31,000 cycles of each SIMD.
+// 16,384 rows of 256 float32 logits, sigmoid scores, a bias and groups: 14 us,
+// 1,254 instructions per four rows, 9 us of it, with four waves a SIMD to hide
+// the groups' passes through shared memory (131,072 rows: 70 us).
 
 // A 32-bit value in a 64-bit float leaves its low 29 bits free.
 struct WideKey {
@@ -166,21 +166,25 @@ struct WideKey {
     return key <= NONE ? -1 : b < 0 ? low : low ^ (kMaxExperts - 1);
   }
 };
-// Values of 16 bits as 32-bit floats end in 13 zeros or more: 19 bits in the
-// order of the values, and 10 for the expert.
+// Values of 16 bits in their order as signed whole numbers (-0 is 0), above
+// the expert.
+template <class T>
 struct ShortKey {
-  using type = uint32_t;
-  static constexpr uint32_t NONE = 0;
-  static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
-  static __device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) { return a > b ? b : a; }
-  static __device__ __forceinline__ uint32_t of(float value, int expert) {
-    const uint32_t b = __float_as_uint(value + 0.0f);
-    const uint32_t order = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-    return (order >> 13) << 10 | (kMaxExperts - 1 - expert);
+  using type = int32_t;
+  static constexpr int32_t NONE = INT32_MIN;
+  typedef short pair __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ int32_t larger(int32_t a, int32_t b) { return a > b ? a : b; }
+  static __device__ __forceinline__ int32_t smaller(int32_t a, int32_t b) { return a > b ? b : a; }
+  // The keys of two neighbouring values, their bits in one word.
+  static __device__ __forceinline__ void of(uint32_t bits, int expert, int32_t* first, int32_t* second) {
+    const pair b = __builtin_bit_cast(pair, bits), sign = b >> (short)15;
+    const uint32_t order = __builtin_bit_cast(uint32_t, (pair)((b ^ (sign & (short)0x7FFF)) - sign));
+    *first = (int32_t)(order << 16 | (uint32_t)(kMaxExperts - 1 - expert));
+    *second = (int32_t)((order & 0xFFFF0000u) | (uint32_t)(kMaxExperts - 2 - expert));
   }
-  static __device__ __forceinline__ int expert(uint32_t key) {
-    // minus infinity, 0xFF800000, has the order 0x007FFFFF
-    return key >= ((0x007FFFFFu >> 13) + 1) << 10 ? kMaxExperts - 1 - (int)(key & (kMaxExperts - 1)) : -1;
+  static __device__ __forceinline__ int expert(int32_t key) {
+    constexpr int INF = std::is_same_v<T, bf16> ? 0x7F80 : 0x7C00;   // of minus infinity: -INF
+    return (key >> 16) > -INF ? kMaxExperts - 1 - (key & 0xFFFF) : -1;
   }
 };
 
@@ -231,7 +235,8 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
                                                     int32_t* __restrict__ experts, float* __restrict__ weights) {
   extern __shared__ float shared[];
   using R = Row<T, L, N>;
-  using Key = std::conditional_t<sizeof(T) == 2 && !BY_SCORE, ShortKey, WideKey>;
+  constexpr bool SHORT = sizeof(T) == 2 && !BY_SCORE;
+  using Key = std::conditional_t<SHORT, ShortKey<T>, WideKey>;
   using K = typename Key::type;
   constexpr int M = FEW && N > 8 ? 8 : N, SLOTS = FEW ? 1 : (kMaxTopK + L - 1) / L;
   const int j = threadIdx.x & (L - 1);
@@ -240,7 +245,8 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
   const T* x_row = logits + row * ld;
 
   float x[N], add[N], top = kNone;
-  R::load(x_row, r.experts, j, wide, x);
+  typename R::Vector in[N / R::V];
+  R::load(x_row, r.experts, j, wide, in, x);
   if constexpr (BY_SCORE)   // here, where nothing waits for it yet
 #pragma unroll
     for (int i = 0; i < N; ++i) add[i] = bias && R::element(i, j) < r.experts ? bias[R::element(i, j)] : 0.0f;
@@ -339,7 +345,19 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
 
   K k[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) k[i] = Key::of(x[i], R::element(i, j));
+  for (int i = 0; i < N; i += 2) {
+    if constexpr (SHORT) {
+      uint32_t bits;
+      __builtin_memcpy(&bits, &in[i / R::V].v[i % R::V], 4);
+      Key::of(bits, R::element(i, j), &k[i], &k[i + 1]);
+    } else {
+      k[i] = Key::of(x[i], R::element(i, j));
+      k[i + 1] = Key::of(x[i + 1], R::element(i + 1, j));
+    }
+  }
+  if (SHORT && r.groups > 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) k[i] = x[i] == kNone ? Key::NONE : k[i];
   largest_keys<Key, M>(k);
   int mine[SLOTS];  // lane j keeps the choices j, j + L, ...
 #pragma unroll
@@ -491,7 +509,8 @@ __global__ __launch_bounds__(256) void route_back_kernel(Router r, int64_t token
   const T* x_row = logits + row * ld;
   float* d = shared + threadIdx.x / L * (L * N + 1);
   float x[N], top = kNone;
-  R::load(x_row, r.experts, j, wide, x);
+  typename R::Vector in[N / R::V];
+  R::load(x_row, r.experts, j, wide, in, x);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     d[R::element(i, j)] = 0.0f;
@@ -546,8 +565,8 @@ __global__ __launch_bounds__(256) void route_back_kernel(Router r, int64_t token
 // Fewer lanes per row exchange less per row, as long as a lane holds at most
 // 16 values and the rows still make 4,096 waves (4 for each of the 1,024
 // SIMDs).  131,072 rows of 128 bfloat16 logits take 18 us in 8 lanes, 20 in
-// 16 and 51 in 64; 16,384 rows of 256 float32 ones in groups 15 us in 16 lanes
-// and 20 in 64.
+// 16 and 49 in 64; 16,384 rows of 256 float32 ones in groups 14 us in 16 lanes
+// and 18 in 64.
 template <class F>
 void with_shape(int64_t tokens, int experts, F&& f) {
   int lanes = 64;
