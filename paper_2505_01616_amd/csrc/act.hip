@@ -231,9 +231,56 @@ struct Cut {
   int step;          // slots of one pass through shared memory
   int64_t longest;
   int64_t items, partials, joins;   // at most
-  bool planned;      // whether the parts are laid out by plan_kernel
+  // Who lays out the parts: no one (whole sums, in the experts' order), every
+  // wave that needs one by itself, or plan_kernel in a list.
+  enum Plan { WHOLE, BY_WAVE, LISTED } plan;
   int64_t bytes;     // workspace
 };
+
+// The parts of an expert's sum, and the slots of each.
+__device__ __forceinline__ void cut_sum(const Cut& cut, uint32_t n, uint32_t* parts, uint32_t* each) {
+  const uint32_t longest = (uint32_t)cut.longest;
+  *parts = n > longest ? (n + longest - 1) / longest : 1;
+  *each = ((n + *parts - 1) / *parts + cut.step - 1) / cut.step * cut.step;
+  if (*parts > 1) *parts = (n + *each - 1) / *each;
+}
+
+// Part number `want` (JOINS: the want-th expert that is cut) in the order of
+// plan_kernel, by a wave, a lane per expert: for few experts less than the
+// launch that would write a list.
+template <bool JOINS>
+__device__ __forceinline__ void find_part(const Grad& g, const Cut& cut, const int32_t* offsets, int want, Item* part,
+                                          Join* joined) {
+  const int e = threadIdx.x & 63;
+  Item it{-1, 0, 0, -1};
+  uint32_t parts = 0, each = 0;
+  if (e < g.experts) {
+    it = segment(offsets, e, g.slots);
+    cut_sum(cut, (uint32_t)(it.to - it.from), &parts, &each);
+  }
+  int item = 0, partial = 0, join = 0;
+  for (int h = 0; h < g.experts; ++h) {
+    const int other = __builtin_amdgcn_readlane((int)each, h), count = __builtin_amdgcn_readlane((int)parts, h);
+    const bool before = other > (int)each || (other == (int)each && h < e);
+    item += before ? count : 0;
+    partial += before && count > 1 ? count : 0;
+    join += before && count > 1 ? 1 : 0;
+  }
+  const bool fits = item + (int64_t)parts <= cut.items && (parts == 1 || partial + (int64_t)parts <= cut.partials);
+  const uint64_t found = __ballot(e < g.experts && fits &&
+                                  (JOINS ? parts > 1 && join == want : want >= item && want < item + (int)parts));
+  const int lane = found ? __builtin_ctzll(found) : 0;
+  auto of = [&](int v) { return __builtin_amdgcn_readlane(v, lane); };
+  if constexpr (JOINS) {
+    const Join all{of(e), of(partial), of((int)parts), 0};
+    *joined = found ? all : Join{-1, 0, 0, 0};
+  } else {
+    const int count = of((int)parts), slots = of((int)each), p = want - of(item), first = of(it.from), last = of(it.to);
+    const int64_t from = first + (int64_t)p * slots, to = min((int64_t)last, from + slots);
+    const int number = of(partial) + p, expert = of(e);
+    *part = !found ? Item{-1, 0, 0, -1} : count > 1 ? Item{expert, (int)from, (int)to, number} : Item{expert, first, last, -1};
+  }
+}
 
 // Orders the experts' sums by length, longest first, and cuts the long ones:
 // workgroups start in this order, so the last to end are short (a sum over
@@ -250,10 +297,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, const int32
   uint32_t parts = 0, each = 0;
   if (e < g.experts) {
     it = segment(offsets, e, g.slots);
-    const uint32_t n = it.to - it.from, longest = (uint32_t)cut.longest;
-    parts = n > longest ? (n + longest - 1) / longest : 1;
-    each = ((n + parts - 1) / parts + cut.step - 1) / cut.step * cut.step;
-    if (parts > 1) parts = (n + each - 1) / each;
+    cut_sum(cut, (uint32_t)(it.to - it.from), &parts, &each);
     it.partial = (int)each;
   }
   length[e] = e < g.experts ? (int)each : -1;
@@ -319,10 +363,15 @@ __global__ __launch_bounds__(1024) void plan_kernel(Grad g, Cut cut, const int32
 // dW of the experts whose sums are in parts.  Four threads take every fourth
 // part of four elements; the order of the sum depends on the parts alone.
 template <class O>
-__global__ __launch_bounds__(256) void join_kernel(Grad g, const Join* __restrict__ joins,
+__global__ __launch_bounds__(256) void join_kernel(Grad g, Cut cut, const int32_t* __restrict__ offsets,
+                                                   const Join* __restrict__ joins,
                                                    const float* __restrict__ partials, O* __restrict__ dw) {
   __shared__ float sums[4][64][4];
-  const Join j = joins[blockIdx.y];
+  Join j;
+  if (cut.plan == Cut::LISTED)
+    j = joins[blockIdx.y];
+  else
+    find_part<true>(g, cut, offsets, blockIdx.y, nullptr, &j);
   if (j.parts == 0) return;
   const int64_t size = (int64_t)g.n * g.cols;
   const float* from = partials + j.first * size;
@@ -369,7 +418,7 @@ __global__ __launch_bounds__(256) void join_kernel(Grad g, const Join* __restric
 }
 
 template <class T, class O, int BN, int BC, int WN, int WC, int KB>
-__global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* __restrict__ items,
+__global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, const Item* __restrict__ items,
                                                             const T* __restrict__ dy, const int8_t* __restrict__ q,
                                                             const int8_t* __restrict__ exponents,
                                                             const int32_t* __restrict__ map,
@@ -388,7 +437,13 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, const Item* 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tiles_n = (g.n + BN - 1) / BN;
   const int n0 = (int)(blockIdx.x % tiles_n) * BN, c0 = (int)(blockIdx.x / tiles_n) * BC;
-  Item it = items ? items[blockIdx.y] : segment(offsets, blockIdx.y, g.slots);
+  Item it;
+  if (cut.plan == Cut::WHOLE)
+    it = segment(offsets, blockIdx.y, g.slots);
+  else if (cut.plan == Cut::LISTED)
+    it = items[blockIdx.y];
+  else
+    find_part<false>(g, cut, offsets, blockIdx.y, &it, nullptr);
   if (it.expert < 0) return;
   if (g.rows == 0) it.to = it.from;   // no row to read: all count as zeros
 
@@ -631,10 +686,12 @@ Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols, int32_t ty
   c.longest = ceil_div(slots * tiles, 256);
   if (c.longest < 256) c.longest = 256;
   if (c.longest > kMaxSlots) c.longest = kMaxSlots;   // no sum is longer
-  // laying the parts out and joining them takes two more launches, about as
-  // long as 1,024 slots of one tile
-  c.planned = slots > 1024;
-  if (!c.planned) return c;
+  // joining the parts takes a launch more, about as long as 1,024 slots of one
+  // tile, and a list of them another, which many experts or tiles are worth:
+  // 131,072 slots of 4 experts, 64 x 64 from float16, take 23 us without a list
+  // and 26.5 with one, 9,003 slots of 16 experts of 48 tiles 64 and 60.5
+  c.plan = slots <= 1024 ? Cut::WHOLE : experts <= 8 && experts * tiles <= 512 ? Cut::BY_WAVE : Cut::LISTED;
+  if (c.plan == Cut::WHOLE) return c;
   c.items = experts + slots / c.longest;
   c.joins = slots / c.longest < experts ? slots / c.longest : experts;
   c.partials = 2 * (slots / c.longest);
@@ -737,18 +794,18 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
           using O = decltype(o);
           constexpr int LONG = Terms<T>::value == 1 ? 64 : 32;
           hipStream_t s = static_cast<hipStream_t>(hip_stream);
-          Item* items = cut.planned ? static_cast<Item*>(d_work) : nullptr;
+          Item* items = static_cast<Item*>(d_work);
           Join* joins = reinterpret_cast<Join*>(items + cut.items);
           float* partials = reinterpret_cast<float*>(joins + cut.joins);
-          if (cut.planned)
+          if (cut.plan == Cut::LISTED)
             hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(experts, 64) * 64), 0, s, g, cut, d_offsets, items, joins);
           auto run = [&](auto kernel, int threads) {
             const int lds = 2 * 2 * cut.step * (Terms<T>::value + 1) * (cut.tile + 32);
             (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
             hipLaunchKernelGGL(kernel,
                                dim3((unsigned)(ceil_div(n, cut.tile) * ceil_div(cols, cut.tile)),
-                                    (unsigned)(cut.planned ? cut.items : experts)),
-                               dim3(threads), lds, s, g, items, static_cast<const T*>(d_dy), d_q, d_exponents,
+                                    (unsigned)(cut.plan == Cut::WHOLE ? experts : cut.items)),
+                               dim3(threads), lds, s, g, cut, items, static_cast<const T*>(d_dy), d_q, d_exponents,
                                d_row_of_slot ? d_row_of_slot : d_offsets, d_offsets, static_cast<O*>(d_dw), partials);
           };
           if (cut.tile == 256)
@@ -760,7 +817,7 @@ extern "C" netsim_status netsim_act_weight_grad(int32_t device, int32_t experts,
             // nothing to do cost 4 us at 14,000 of them
             const int64_t groups = ceil_div((int64_t)n * cols, 256), most = cut.joins < 32 ? 4096 / cut.joins : 128;
             hipLaunchKernelGGL(join_kernel<O>, dim3((unsigned)(groups < most ? groups : most), (unsigned)cut.joins),
-                               dim3(256), 0, s, g, joins, partials, static_cast<O*>(d_dw));
+                               dim3(256), 0, s, g, cut, d_offsets, joins, partials, static_cast<O*>(d_dw));
           }
         });
       });
