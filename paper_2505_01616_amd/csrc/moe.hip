@@ -79,8 +79,10 @@ __device__ __forceinline__ float exp_of(float x) {
   const float hi = x * LOG2E;
   const float low = __builtin_fmaf(x, LOG2E_LOW, __builtin_fmaf(x, LOG2E, -hi));
   const float p = __builtin_amdgcn_exp2f(hi);
-  // beyond the range hi alone decides (0 or infinity); low may not be finite there
-  return fabsf(hi) < 150.0f ? __builtin_fmaf(p, low * LN2, p) : p;
+  // From 128 on p is infinite, which a low of 0 or less would turn into a NaN;
+  // below -128 it is 0 or nearly so.  Neither takes a correction, and low may
+  // not be finite there.
+  return fabsf(hi) < 128.0f ? __builtin_fmaf(p, low * LN2, p) : p;
 }
 // exp(x) for x <= 0 with the product rounded: off by |x| half steps more.
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
