@@ -592,6 +592,8 @@ void with_shape(int64_t tokens, int experts, F&& f) {
     values(std::integral_constant<int, 64>{});
 }
 
+constexpr int64_t kRowsOfLaunch = 1 << 25;   // of up to 64 threads each
+
 // Whether vectors of V elements of every row are aligned and whole.
 template <class T>
 bool whole_vectors(const void* p, int64_t ld, int experts, int vector) {
@@ -983,11 +985,14 @@ extern "C" netsim_status netsim_route(int32_t device, const netsim_router* route
           using T = decltype(t);
           constexpr int L = decltype(l)::value, N = decltype(n)::value;
           const size_t lds = r.groups > 1 ? 256 / L * sizeof(float) * (L * N + 1 + 2 * r.groups) : 0;
+          const T* in = static_cast<const T*>(d_logits);
+          const bool wide = whole_vectors<T>(in, ld_logits, r.experts, Row<T, L, N>::V);
           auto run = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), lds,
-                               static_cast<hipStream_t>(hip_stream), r, tokens, static_cast<const T*>(d_logits),
-                               ld_logits, whole_vectors<T>(d_logits, ld_logits, r.experts, Row<T, L, N>::V), d_bias,
-                               d_experts, d_weights);
+            in_launches(tokens, kRowsOfLaunch, [&](int64_t first, int64_t rows) {
+              hipLaunchKernelGGL(kernel, dim3((unsigned)ceil_div(rows, 256 / L)), dim3(256), lds,
+                                 static_cast<hipStream_t>(hip_stream), r, rows, in + first * ld_logits, ld_logits, wide,
+                                 d_bias, d_experts + first * r.top_k, d_weights + first * r.top_k);
+            });
           };
           // without a bias and sums of scores the logits give the same order
           const bool by_score = d_bias || r.best > 1;
@@ -1029,18 +1034,25 @@ extern "C" netsim_status netsim_route_backward(int32_t device, const netsim_rout
         if (r.softmax && !r.renorm) {
           with_shape(tokens, r.experts, [&](auto l, auto n) {
             constexpr int L = decltype(l)::value, N = decltype(n)::value, V = Row<T, L, N>::V;
-            hipLaunchKernelGGL((route_back_kernel<T, L, N>), dim3((unsigned)ceil_div(tokens, 256 / L)), dim3(256), 0, s,
-                               r, tokens, in, ld_logits, whole_vectors<T>(in, ld_logits, r.experts, V), d_experts,
-                               d_dweights, out, ld_dlogits, whole_vectors<T>(out, ld_dlogits, r.experts, V));
+            const bool wide = whole_vectors<T>(in, ld_logits, r.experts, V);
+            const bool wide_out = whole_vectors<T>(out, ld_dlogits, r.experts, V);
+            in_launches(tokens, kRowsOfLaunch, [&](int64_t first, int64_t rows) {
+              hipLaunchKernelGGL((route_back_kernel<T, L, N>), dim3((unsigned)ceil_div(rows, 256 / L)), dim3(256), 0, s, r,
+                                 rows, in + first * ld_logits, ld_logits, wide, d_experts + first * r.top_k,
+                                 d_dweights + first * r.top_k, out + first * ld_dlogits, ld_dlogits, wide_out);
+            });
           });
           return;
         }
         auto run = [&](auto lanes) {
           constexpr int K = decltype(lanes)::value, V = 16 / sizeof(T);
           const size_t lds = 256 / K * sizeof(float) * (ceil_div(r.experts, V) * V);
-          hipLaunchKernelGGL((route_back_chosen_kernel<T, K>), dim3((unsigned)ceil_div(tokens, 256 / K)), dim3(256), lds,
-                             s, r, tokens, in, ld_logits, d_experts, d_dweights, out, ld_dlogits,
-                             whole_vectors<T>(out, ld_dlogits, r.experts, V));
+          const bool wide = whole_vectors<T>(out, ld_dlogits, r.experts, V);
+          in_launches(tokens, kRowsOfLaunch, [&](int64_t first, int64_t rows) {
+            hipLaunchKernelGGL((route_back_chosen_kernel<T, K>), dim3((unsigned)ceil_div(rows, 256 / K)), dim3(256), lds, s,
+                               r, rows, in + first * ld_logits, ld_logits, d_experts + first * r.top_k,
+                               d_dweights + first * r.top_k, out + first * ld_dlogits, ld_dlogits, wide);
+          });
         };
         // the rows of a workgroup have to fit its shared memory (64 KB)
         if (r.top_k <= 8 && r.experts <= 512)

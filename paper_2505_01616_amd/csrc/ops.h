@@ -73,6 +73,13 @@ netsim_status launch(const char* what, int32_t device, F&& go) {
   return e == hipSuccess ? NETSIM_OK : fail(NETSIM_E_DEVICE, what, hipGetErrorString(e));
 }
 
+// A grid of 2^32 threads or more is cut short by the runtime, without an error:
+// work over `count` items goes in launches of at most `most`.
+template <class F>
+void in_launches(int64_t count, int64_t most, F&& go) {
+  for (int64_t first = 0; first < count; first += most) go(first, count - first < most ? count - first : most);
+}
+
 // Calls f with a value of the element type `type` names.
 template <class F>
 void with_type(int32_t type, F&& f) {
