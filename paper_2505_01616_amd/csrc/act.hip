@@ -663,6 +663,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, con
 }
 
 constexpr int kMaxCols = 1 << 20;
+constexpr int64_t kBlocksOfLaunch = 1 << 30;   // two threads each; a row has at most 2^15
 constexpr int64_t kMaxSlots = 0x7fffffff - 4096;   // a step past the end stays in 32 bits
 
 // How a call's sums are cut, from its sizes alone.
@@ -718,12 +719,14 @@ extern "C" netsim_status netsim_act_save(int32_t device, int64_t rows, int32_t c
     const int blocks = (int)ceil_div(cols, kBlock);
     if (rows > ((int64_t)1 << 37) / blocks) return fail(NETSIM_E_INVALID, what, "more than 2^37 blocks of 32 columns");
     return launch(what, device, [&] {
-      const int64_t groups = ceil_div(rows * blocks, 128);
       with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(save_kernel<T>, dim3((unsigned)groups), dim3(256), 0,
-                           static_cast<hipStream_t>(hip_stream), rows, cols, blocks, static_cast<const T*>(d_x), ld_x,
-                           d_q, d_exponents);
+        in_launches(rows, kBlocksOfLaunch / blocks, [&](int64_t first, int64_t n) {
+          hipLaunchKernelGGL(save_kernel<T>, dim3((unsigned)ceil_div(n * blocks, 128)), dim3(256), 0,
+                             static_cast<hipStream_t>(hip_stream), n, cols, blocks,
+                             static_cast<const T*>(d_x) + first * ld_x, ld_x, d_q + first * blocks * kBlock,
+                             d_exponents + first * blocks);
+        });
       });
     });
   });
@@ -744,12 +747,13 @@ extern "C" netsim_status netsim_act_restore(int32_t device, int64_t rows, int32_
     const int blocks = (int)ceil_div(cols, kBlock);
     if (rows > ((int64_t)1 << 37) / blocks) return fail(NETSIM_E_INVALID, what, "more than 2^37 blocks of 32 columns");
     return launch(what, device, [&] {
-      const int64_t groups = ceil_div(rows * blocks, 128);
       with_type(type, [&](auto t) {
         using T = decltype(t);
-        hipLaunchKernelGGL(restore_kernel<T>, dim3((unsigned)groups), dim3(256), 0,
-                           static_cast<hipStream_t>(hip_stream), rows, cols, blocks, d_q, d_exponents,
-                           static_cast<T*>(d_x), ld_x);
+        in_launches(rows, kBlocksOfLaunch / blocks, [&](int64_t first, int64_t n) {
+          hipLaunchKernelGGL(restore_kernel<T>, dim3((unsigned)ceil_div(n * blocks, 128)), dim3(256), 0,
+                             static_cast<hipStream_t>(hip_stream), n, cols, blocks, d_q + first * blocks * kBlock,
+                             d_exponents + first * blocks, static_cast<T*>(d_x) + first * ld_x, ld_x);
+        });
       });
     });
   });

@@ -61,3 +61,20 @@ def test_route_backward_of_more_rows_than_a_grid(gpu, scores):  # noqa: F811
     for c in range(8):
         same &= got[:, c] == ordinary[c]
     assert int((~same).sum()) == len(rows)
+
+
+def test_save_of_more_blocks_than_a_grid(gpu):  # noqa: F811
+    """2^31 blocks and a few more: rows of one column."""
+    torch, moe = gpu
+    rows = 2 ** 31 + 5
+    x = allocate(torch, lambda: torch.zeros((rows, 1), dtype=torch.bfloat16, device="cuda"))
+    x += 1.0
+    at = [0, 2 ** 30 - 1, 2 ** 30, 2 ** 31 - 1, 2 ** 31, rows - 1]
+    for n, i in enumerate(at):
+        x[i, 0] = 3.0 + n
+    saved = allocate(torch, lambda: moe.save(x))
+    q, e = plain.save(host(x[at]))
+    np.testing.assert_array_equal(saved.q[at].cpu().numpy(), q)
+    np.testing.assert_array_equal(saved.exponents[at].cpu().numpy(), e)
+    back = allocate(torch, lambda: moe.restore(saved, torch.bfloat16))
+    assert bool((back == x).all())
