@@ -740,7 +740,7 @@ netsim_status netsim_act_restore(int32_t device, int64_t rows, int32_t cols, con
  * dy takes part with all its bits (float16 and float32 as two and three
  * bfloat16 terms, magnitudes below 2^-126 not kept exactly), x as restored,
  * the sums in 32 bits, rounded once to out_type.  A slot whose row is out of
- * range counts as a row of zeros.  experts: 1 .. 1024; n, cols: 1 .. 2^20;
+ * range is left out, whatever its dy holds.  experts: 1 .. 1024; n, cols: 1 .. 2^20;
  * slots < 2^31-4096.  d_work: netsim_act_weight_grad_work_bytes(...) bytes
  * (-1 for refused sizes), aligned to 16.
  */

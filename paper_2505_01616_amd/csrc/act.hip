@@ -431,6 +431,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, con
   constexpr int CY = BN / 8, NY = KB * CY / THREADS, CX = BC / 16, NX = KB * CX / THREADS;
   constexpr int FN = BN / WN / 32, FC = BC / WC / 32;
   static_assert(THREADS % CY == 0 && THREADS % CX == 0 && NY * THREADS == KB * CY && NX * THREADS == KB * CX, "");
+  static_assert(CY == 2 * CX && NY == 2 * NX, "a wave's slots of dy are those of its saved rows");
   constexpr float MOST = sizeof(T) == 2 ? 65504.0f : 3.402823466e38f;
   extern __shared__ __align__(16) bf16 shared[];
 
@@ -445,10 +446,13 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, con
   else
     find_part<false>(g, cut, offsets, blockIdx.y, &it, nullptr);
   if (it.expert < 0) return;
-  if (g.rows == 0) it.to = it.from;   // no row to read: all count as zeros
+  if (g.rows == 0) it.to = it.from;   // no row to read: every slot is left out
 
-  // this thread's part of a tile of dy and of saved rows
-  const int y_chunk = tid % CY, y_row = tid / CY, x_chunk = tid % CX, x_row = tid / CX;
+  // This thread's part of a tile of dy and of saved rows.  A wave brings in
+  // dy of the slots whose saved rows it brings in, half of them at a time.
+  const int y_chunk = tid % CY, x_chunk = tid % CX, x_row = tid / CX;
+  const int y_row = wave * (64 / CX) + lane / CY;
+  auto y_step = [](int i) { return (i & 1) * (64 / CY) + (i >> 1) * (THREADS / CX); };
   const int y_left = g.n - (n0 + y_chunk * 8);
   const bool x_in = c0 + x_chunk * 16 < g.blocks * kBlock;
   // columns beyond the row reach no output: a chunk wholly beyond reads the
@@ -474,11 +478,11 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, con
     }
   };
   auto load_y = [&](int s0, int i, bool plain) {
-    const T* from = y_at + (int64_t)(s0 - it.from + i * (THREADS / CY)) * g.ld;
+    const T* from = y_at + (int64_t)(s0 - it.from + y_step(i)) * g.ld;
     if (plain)
       y[i] = load_eight(from);
     else
-      y[i] = load_some(from, s0 + y_row + i * (THREADS / CY) < it.to ? y_left : 0);
+      y[i] = load_some(from, s0 + y_row + y_step(i) < it.to ? y_left : 0);
   };
   auto load_x = [&](int s0, int i) {
     // no conditions that branch: the products on both sides stay one block
@@ -489,7 +493,15 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, con
     e[i] = (uint8_t)exponents[block];
   };
   auto store_y = [&](bf16* stage, int i) {
-    const int k = y_row + i * (THREADS / CY);
+    const int k = y_row + y_step(i);
+    // A slot without a row is left out of dy as well: an infinity or a NaN
+    // times the row's zeros would be a NaN.  The lanes that hold the slot's
+    // row say whether there is one; their bits are 32 (i & 1) + CX (lane / CY)
+    // and on.
+    const uint64_t rows_held = __ballot(held[i >> 1]);
+    const int keep = __builtin_amdgcn_sbfe((int)(rows_held >> (32 * (i & 1))), CX * (lane / CY), 1);   // 0 or -1
+#pragma unroll
+    for (int j = 0; j < Eight<T>::WORDS; ++j) y[i].w[j] &= (uint32_t)keep;
     if constexpr (TERMS == 1) {
       *reinterpret_cast<uint4*>(stage + k * PY + y_chunk * 8) = make_uint4(y[i].w[0], y[i].w[1], y[i].w[2], y[i].w[3]);
     } else {
