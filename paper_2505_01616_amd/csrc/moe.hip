@@ -393,13 +393,13 @@ __global__ __launch_bounds__(256) void route_kernel(Router r, int64_t tokens, co
     sum += w[s];
   }
   if (r.renorm) z = sum_over<L>(sum);
-  const float factor = z > 0.0f ? r.scale / z : 0.0f;
 #pragma unroll
   for (int s = 0; s < SLOTS; ++s)
     if (at < tokens && s * L + j < r.top_k) {
       const int64_t to = row * r.top_k + s * L + j;
       experts[to] = row_bad ? -1 : mine[s];
-      weights[to] = row_bad ? NAN : w[s] * factor;
+      // divided first: scale / z may be infinite where the weight is not
+      weights[to] = row_bad ? NAN : z > 0.0f ? w[s] / z * r.scale : 0.0f;
     }
 }
 

@@ -122,3 +122,16 @@ def test_softmax_routing_of_every_logit(gpu, kind, with_bias, renorm):  # noqa: 
     far = x.max(1, keepdims=True) - x.min(1, keepdims=True)
     bound = (2 * far + 40) * U * want_w + 2 * TINY
     assert (np.abs(host(w) - want_w)[keep] <= bound[keep]).all()
+
+
+@pytest.mark.parametrize("scores,level", [("sigmoid", -75.0), ("sigmoid", -86.0), ("softmax", -75.0)])
+@pytest.mark.parametrize("scale", [16.0, 1e8, 3e38])
+def test_weights_of_small_scores_with_large_factors(gpu, scores, level, scale):  # noqa: F811
+    """scale / (sum of the chosen scores) is beyond float32, the weights are
+    not."""
+    torch, moe = gpu
+    r = moe.Router(16, 4, scores, scale=scale)
+    x = np.random.default_rng(2).uniform(level - 1, level + 0.5, (64, 16)).astype(np.float32).astype(np.float64)
+    x[1] = level
+    x[2, 1:] = -np.inf
+    check_route(torch, moe, r, "f32", x, None)
