@@ -616,8 +616,8 @@ struct Plan {
   int experts, top_k, ranks;
   int64_t tokens, per_rank;   // tokens of a source rank
   int chunk_tokens;           // tokens of a chunk
-  int64_t rank_chunks;        // chunks of a source rank
-  int64_t chunks;
+  int64_t rank_chunks;        // chunks of a source rank; the last that holds tokens may have fewer
+  int64_t chunks;             // of the ranks that hold tokens: the first ones
   bool once;
   bool small;                 // one workgroup does it all
 };
@@ -754,8 +754,9 @@ __global__ __launch_bounds__(1024) void dispatch_scan_kernel(Plan p, int32_t* __
     if (pair >= p.ranks * p.ranks) return;
     const int from = pair / p.ranks, to = pair % p.ranks;
     int64_t rows = 0;
+    const int64_t mine = min(p.rank_chunks, p.chunks - from * p.rank_chunks);   // none or below: no tokens
 #pragma unroll 8
-    for (int64_t c = 0; c < p.rank_chunks; ++c) rows += sent[(from * p.rank_chunks + c) * p.ranks + to];
+    for (int64_t c = 0; c < mine; ++c) rows += sent[(from * p.rank_chunks + c) * p.ranks + to];
     traffic[pair] = (double)rows * row_bytes;
     return;
   }
@@ -943,7 +944,8 @@ Plan make_plan(int32_t experts, int32_t top_k, int64_t tokens, int32_t ranks, in
   p.once = once;
   p.chunk_tokens = kChunk / top_k;
   p.rank_chunks = ceil_div(p.per_rank, p.chunk_tokens);
-  p.chunks = p.rank_chunks * ranks;
+  const int64_t whole = (tokens - 1) / p.per_rank;   // ranks before the last that holds tokens
+  p.chunks = whole * p.rank_chunks + ceil_div(tokens - whole * p.per_rank, p.chunk_tokens);
   p.small = tokens * top_k <= kSmallChoices && 16 * experts + ranks * ranks <= kSmallInts;
   return p;
 }
