@@ -1073,7 +1073,8 @@ extern "C" int64_t netsim_dispatch_work_bytes(int32_t experts, int32_t top_k, in
   if (bad_dispatch(experts, top_k, tokens, ranks, tokens_per_rank)) return -1;
   if (tokens == 0) return 0;
   const Plan p = make_plan(experts, top_k, tokens, ranks, tokens_per_rank, false);
-  return 4 * (p.chunks * (p.experts + p.ranks) + p.experts);
+  // one workgroup works in its own memory: a word, so that there is an array
+  return p.small ? 4 : 4 * (p.chunks * (p.experts + p.ranks) + p.experts);
 }
 
 extern "C" netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_t top_k, int64_t tokens,

@@ -139,11 +139,15 @@ def dispatch(experts: torch.Tensor, num_experts: int, ranks: int = 1, tokens_per
     per = tokens_per_rank if tokens_per_rank is not None else max(1, -(-tokens // max(1, ranks)))
     work = max(0, ns.netsim_dispatch_work_bytes(num_experts, top_k, tokens, ranks, per))
     index, stream = _at(device)
-    # the whole numbers and the workspace are one allocation: each more would
-    # cost a tenth of a small call
-    whole = torch.empty(max(0, num_experts) + 1 + 2 * tokens * top_k + work // 4, dtype=torch.int32, device=device)
+    # the whole numbers are one allocation: each more would cost a tenth of a
+    # small call.  So is a small call's workspace, which is a word; a larger
+    # one is free again after the call, whatever the caller keeps.
+    inside = work // 4 if work <= 4 else 0
+    whole = torch.empty(max(0, num_experts) + 1 + 2 * tokens * top_k + inside, dtype=torch.int32, device=device)
     offsets, token_of_slot, slot_of_choice, space = whole.split_with_sizes(
-        (max(0, num_experts) + 1, tokens * top_k, tokens * top_k, work // 4))
+        (max(0, num_experts) + 1, tokens * top_k, tokens * top_k, inside))
+    if work > 4:
+        space = torch.empty(work // 4, dtype=torch.int32, device=device)
     out = Dispatch(offsets, token_of_slot, slot_of_choice.view(tokens, top_k),
                    torch.empty((max(0, ranks), max(0, ranks)), dtype=torch.float64, device=device))
     ns.netsim_dispatch(index, num_experts, top_k, tokens, experts.data_ptr(), ranks, per, row_bytes,

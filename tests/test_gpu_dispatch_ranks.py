@@ -24,3 +24,14 @@ def test_ranks_without_tokens(gpu, tokens, k, experts, ranks, per, once):  # noq
     want = plain.dispatch(e, experts, ranks, per, 1056.0, once)
     for name, g, w in zip(got._fields, got, want):
         np.testing.assert_array_equal(g.cpu().numpy(), w, err_msg=name)
+
+
+@pytest.mark.parametrize("tokens,k,experts,ranks", [(48, 2, 8, 8), (1000, 8, 256, 64), (20000, 8, 256, 64), (3000, 4, 1024, 1024)])
+def test_results_keep_no_workspace(gpu, tokens, k, experts, ranks):  # noqa: F811
+    """What a result keeps alive are the results (and one word at most)."""
+    torch, moe = gpu
+    e = torch.randint(0, experts, (tokens, k), dtype=torch.int32, device="cuda")
+    d = moe.dispatch(e, experts, ranks=ranks, row_bytes=8.0)
+    whole = sum(t.numel() * 4 for t in (d.offsets, d.token_of_slot, d.slot_of_choice))
+    for t in (d.offsets, d.token_of_slot, d.slot_of_choice):
+        assert t.untyped_storage().nbytes() <= whole + 4
