@@ -12,6 +12,10 @@ kernels, on torch's current stream of the tensors' device, and returns
 without waiting.  Tensors of another stream have to be ready on it, as for
 any torch operation.  Rows may be parts of wider tensors; the last dimension
 is contiguous.  Failures raise ``NetsimError``, wrong tensors ``ValueError``.
+
+The weights of ``route`` carry their gradient to the logits (once; the bias
+has none).  The results of the other calls carry none: they are whole numbers,
+made from whole numbers, or gradients themselves.
 """
 
 from __future__ import annotations
@@ -93,9 +97,7 @@ def _at(device):
     return device.index, _raw_stream(device.index)
 
 
-def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = None):
-    """logits [tokens, experts] -> (experts int32, weights float32), both
-    [tokens, top_k]; -1 and 0 where a row has no further expert."""
+def _route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor]):
     ld = _rows("logits", logits, _TYPES)
     tokens, n = logits.shape
     if n != router.experts:
@@ -109,6 +111,32 @@ def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = N
     ns.netsim_route(index, router.struct, tokens, _TYPES[logits.dtype], logits.data_ptr(), ld,
                     None if bias is None else bias.data_ptr(), experts.data_ptr(), weights.data_ptr(), stream)
     return experts, weights
+
+
+class _Routed(torch.autograd.Function):
+    """route's weights as a function of its logits, the choice held."""
+
+    @staticmethod
+    def forward(ctx, logits, router, bias):
+        experts, weights = _route(router, logits, bias)
+        ctx.router = router
+        ctx.save_for_backward(logits, experts)
+        ctx.mark_non_differentiable(experts)
+        return experts, weights
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, _, dweights):
+        logits, experts = ctx.saved_tensors
+        return route_backward(ctx.router, logits, experts, dweights.contiguous()), None, None
+
+
+def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = None):
+    """logits [tokens, experts] -> (experts int32, weights float32), both
+    [tokens, top_k]; -1 and 0 where a row has no further expert."""
+    if logits.requires_grad and torch.is_grad_enabled():
+        return _Routed.apply(logits, router, bias)
+    return _route(router, logits, bias)
 
 
 def route_backward(router: Router, logits: torch.Tensor, experts: torch.Tensor, dweights: torch.Tensor) -> torch.Tensor:
