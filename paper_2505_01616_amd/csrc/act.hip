@@ -690,8 +690,10 @@ Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols, int32_t ty
   const int64_t tiles = ceil_div(n, c.tile) * ceil_div(cols, c.tile);   // of one expert
   // Steps of 64 slots keep a compute unit's shared memory to one workgroup,
   // those of 32 leave room for two or three smaller ones, which takes many
-  // tiles to be of use: 2,048 tiles of 128 are 10% faster by 32 slots, 128 of
-  // them 13% slower.
+  // tiles to be of use.  16,384 slots in tiles of 128: with 512 tiles (8 experts
+  // of 64) 69 us by 64 slots and 74 by 32, with 1,024 68 and 67, with 1,536 74 and
+  // 68, with 4,096 119 and 115; 128 to 512 of 16 an expert 35 either way.  2,048
+  // slots: up to 512 tiles 4% slower by 64, from 1,024 on 4 to 12%.
   c.step = terms == 1 && (c.tile == 256 || tiles * experts < 1024) ? 64 : 32;
   // the slots that each of the 256 compute units would have of one tile if
   // all were busy to the end; parts of a few steps cost more in partial sums
@@ -700,10 +702,12 @@ Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t cols, int32_t ty
   if (c.longest < 256) c.longest = 256;
   if (c.longest > kMaxSlots) c.longest = kMaxSlots;   // no sum is longer
   // joining the parts takes a launch more, about as long as 1,024 slots of one
-  // tile, and a list of them another, which many experts or tiles are worth:
-  // 131,072 slots of 4 experts, 64 x 64 from float16, take 23 us without a list
-  // and 26.5 with one, 9,003 slots of 16 experts of 48 tiles 64 and 60.5
-  c.plan = slots <= 1024 ? Cut::WHOLE : experts <= 8 && experts * tiles <= 512 ? Cut::BY_WAVE : Cut::LISTED;
+  // tile, and a list of them another, which every wave's own search outweighs
+  // with many experts or tiles.  16,384 slots, without a list and with one: 1, 4
+  // and 8 experts of one tile 15.5 us and 18, 16 of them 16.6 and 18.2, 32 of
+  // them 21.5 and 18.8; 1 expert of 16 tiles 28.7 and 30.6, 4 of them 34.9 and
+  // 35.1, 8 of them 33.8 and 32.9, 8 of 64 tiles 70.6 and 69.4.
+  c.plan = slots <= 1024 ? Cut::WHOLE : experts * tiles <= 64 && experts <= 16 ? Cut::BY_WAVE : Cut::LISTED;
   if (c.plan == Cut::WHOLE) return c;
   c.items = experts + slots / c.longest;
   c.joins = slots / c.longest < experts ? slots / c.longest : experts;
