@@ -662,11 +662,14 @@ typedef struct {
  *   d_weights[tokens x top_k]: their weights (float32).
  * A logit of minus infinity takes an expert out of the row (a c of minus
  * infinity too); where fewer than top_k are left, the last experts are -1
- * with weight 0, a row without any is all -1 and 0.  Chosen scores whose sum
- * underflows to 0 have weights 0 when renormalised, and no gradient.  Finite logits, the
- * type's lowest value too, are values as any other.  A row whose scores are
- * not defined (a NaN; plus infinity under softmax) has experts -1 and NaN
- * weights.
+ * with weight 0, a row without any is all -1 and 0.  Finite logits, the type's
+ * lowest value too, are values as any other.  A row whose scores are not
+ * defined (a NaN; plus infinity under softmax) has experts -1 and NaN weights.
+ * Scores are computed in 32 bits: a weight is off by less than
+ * (2 d + 40) 2^-24 of itself, d the largest distance between two logits of the
+ * row (sigmoid: the largest magnitude of one), and scores below 2^-126 may
+ * count as 0.  Chosen scores whose sum is 0 then have weights 0 when
+ * renormalised under sigmoid, and no gradient.
  */
 netsim_status netsim_route(int32_t device, const netsim_router* router, int64_t tokens, int32_t type,
                            const void* d_logits, int64_t ld_logits, const float* d_bias,
@@ -715,9 +718,9 @@ netsim_status netsim_dispatch(int32_t device, int32_t experts, int32_t top_k, in
  * exponents e, one per 32 columns: x is q 2^e with e = floor(log2 of the
  * block's largest magnitude) - 6, at least -126, q = x 2^-e rounded to
  * nearest even and held to +-127.  So |x - q 2^e| <= 2^e, 2^(e-1) where q
- * was not held: at most 1/64 of the block's largest magnitude, and restoring
- * never overflows.  A block with an infinity or a NaN has e = -128 and
- * restores as NaN.
+ * was not held: at most 1/64 of the block's largest magnitude, or 2^-127 where
+ * that is below 2^-120.  Restoring to the type that was saved never overflows.
+ * A block with an infinity or a NaN has e = -128 and restores as NaN.
  *   d_x[rows x ld_x], d_q[rows x 32*blocks] (aligned to 16),
  *   d_exponents[rows x blocks]; cols: 1 .. 2^20; rows * blocks <= 2^37.
  */
