@@ -84,9 +84,16 @@ __device__ __forceinline__ float exp_of(float x) {
   // not be finite there.
   return fabsf(hi) < 128.0f ? __builtin_fmaf(p, low * LN2, p) : p;
 }
-// exp(x) for x <= 0 with the product rounded: off by |x| half steps more.
+// exp(x) for x <= 0 with the product rounded: off by |x| half steps more.  For
+// softmax's sum alone, where what is far away counts little: 1,023 of 1,024
+// logits 5 below the largest, the worst case, leave weights off by 4.1 units
+// in the last place (2.2 with exp_of, which takes 262,144 rows of 128 from 27.7
+// to 30.0 us); in ordinary rows both leave the 7.6 that float32 logits'
+// differences are rounded by.
 __device__ __forceinline__ float exp_near(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
-__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }   // to 1 unit more
+// To 1.8 units in the last place; 1.5 with the quotient refined, which takes
+// 16,384 rows of 256 from 13.6 to 14.1 us.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
 
 struct Router {
   int experts, top_k, groups, kept, best;
