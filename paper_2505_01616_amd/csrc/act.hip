@@ -637,7 +637,7 @@ __global__ __launch_bounds__(64 * WN * WC) void grad_kernel(Grad g, Cut cut, con
 
   // The tile leaves through shared memory, so that rows are written as whole
   // lines.  64 experts of 8 slots each, 2,048 x 2,048 in bfloat16 (537 MB):
-  // 116 us, and 193 us when every lane wrote the four columns that it holds.
+  // 118 us, and 193 us when every lane wrote the four columns that it holds.
   auto write = [&](auto* out) {
     using D = std::remove_reference_t<decltype(*out)>;
     constexpr int V = 16 / sizeof(D), PITCH = BC + V;

@@ -146,7 +146,7 @@ struct Row {
 // six choices: 27 us (2.9 TB/s), 507 vector instructions per eight rows, 16 of
 // them exponentials at a quarter of the rate: 31,000 cycles of each SIMD.
 // 16,384 rows of 256 float32 logits, sigmoid scores, a bias and groups: 14 us,
-// 1,254 instructions per four rows, 9 us of it, with four waves a SIMD to hide
+// 1,279 instructions per four rows, 9 us of it, with four waves a SIMD to hide
 // the groups' passes through shared memory (131,072 rows: 70 us).
 
 // A 32-bit value in a 64-bit float leaves its low 29 bits free.
@@ -617,8 +617,9 @@ bool whole_vectors(const void* p, int64_t ld, int experts, int vector) {
 //
 // Bound by the length of each wave's chain of ballots and counters, not by
 // bytes (12.6 MB for 1,048,576 choices of 256 experts from 64 ranks): 6.8 us
-// counting, 4 us adding up, 9.9 us placing.  Chunks of 1,024 choices make 1,024
-// waves there.  48 choices in one launch: 3.8 us.
+// counting, 5.4 us adding up, 9.9 us placing.  Chunks of 1,024 choices make 1,024
+// waves there, one for each SIMD, so nothing hides a wave's chain.  48 choices in
+// one launch: 4.2 us.
 struct Plan {
   int experts, top_k, ranks;
   int64_t tokens, per_rank;   // tokens of a source rank
@@ -629,7 +630,7 @@ struct Plan {
   bool small;                 // one workgroup does it all
 };
 // One launch is shorter to enqueue than three: 8,192 choices of 256 experts
-// take 14.5 us a call in one workgroup and 19 in three launches, 16,384 take 22
+// take 13 us a call in one workgroup and 19 in three launches, 16,384 take 22
 // and 19.
 constexpr int kSmallChoices = 8192, kSmallInts = 16000;   // 64 KB of shared memory
 
