@@ -756,6 +756,129 @@ netsim_status netsim_act_weight_grad(int32_t device, int32_t experts, int64_t sl
                                      int32_t out_type, void* d_dw, void* d_work, int64_t work_bytes,
                                      void* hip_stream);
 
+/*
+ * The products of experts with rows by slot.  w: [experts x n x cols],
+ * contiguous.  Slot s of expert e (d_offsets as netsim_dispatch gives them;
+ * NULL: one expert, which has all slots) has the row x of d_x[rows x ld_x]
+ * that d_row_of_slot[s] names (NULL: row s; rows is then slots), and
+ *   product:  y_s = x w_e^T                           (n values)
+ *   gated:    h_s = act(g) u, g = x w_gate_e^T, u = x w_up_e^T
+ * elementwise, act(g) = g / (1 + exp(-g)) (NETSIM_SILU) or g times the normal
+ * distribution's function of g (NETSIM_GELU).  x, the weights and the result
+ * [slots x ld_y] have one type of 16 bits; sums and act are computed in 32 and
+ * rounded once.  A slot of no expert or without a row (its number out of
+ * range) has a result of zeros.
+ * experts: 1 .. 1024; n, cols: 1 .. 2^20; slots < 2^31-4096.
+ */
+enum { NETSIM_SILU = 0, NETSIM_GELU = 1 };
+netsim_status netsim_experts_product(int32_t device, int32_t experts, int64_t slots, int32_t n,
+                                     int32_t cols, int32_t type, int64_t rows, const void* d_x,
+                                     int64_t ld_x, const int32_t* d_row_of_slot,
+                                     const int32_t* d_offsets, const void* d_w, void* d_y,
+                                     int64_t ld_y, void* hip_stream);
+netsim_status netsim_experts_gated(int32_t device, int32_t experts, int64_t slots, int32_t n,
+                                   int32_t cols, int32_t type, int32_t activation, int64_t rows,
+                                   const void* d_x, int64_t ld_x, const int32_t* d_row_of_slot,
+                                   const int32_t* d_offsets, const void* d_w_gate,
+                                   const void* d_w_up, void* d_h, int64_t ld_h, void* hip_stream);
+
+/*
+ * Their backward passes.  From the result's gradient d_dy (d_dh)
+ * [slots x ld_dy]:
+ *   d_dx: the rows' gradient, contiguous (NULL: none).  Without
+ *     d_row_of_slot that of every slot; with it that of every row, [rows x
+ *     cols], the sum over the row's slots d_slots_of_row[rows x slots_each]
+ *     (as netsim_dispatch's d_slot_of_choice: the slots that d_row_of_slot
+ *     gives the row, -1 for none) in the list's order;
+ *   d_dw, or d_dw_gate and d_dw_up: the weights' [experts x n x cols], zero
+ *     for an expert without slots (NULL: none).
+ * gated's g and u are computed again; their gradients are rounded to the
+ * inputs' type before they enter the products.  Sums in 32 bits, rounded once.
+ * A slot of no expert or without a row is left out, whatever its gradient
+ * holds.  d_work: netsim_experts_backward_work_bytes(...) bytes (-1 for
+ * refused sizes), aligned to 16; matrices: 1 for product, 2 for gated;
+ * has_offsets, has_rows: whether d_offsets and d_row_of_slot are given.
+ */
+int64_t netsim_experts_backward_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                           int32_t matrices, int32_t has_offsets, int32_t has_rows);
+netsim_status netsim_experts_product_backward(
+    int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols, int32_t type,
+    int64_t rows, const void* d_x, int64_t ld_x, const int32_t* d_row_of_slot,
+    const int32_t* d_offsets, const void* d_w, const void* d_dy, int64_t ld_dy,
+    const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx, void* d_dw, void* d_work,
+    int64_t work_bytes, void* hip_stream);
+netsim_status netsim_experts_gated_backward(
+    int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols, int32_t type,
+    int32_t activation, int64_t rows, const void* d_x, int64_t ld_x, const int32_t* d_row_of_slot,
+    const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up, const void* d_dh,
+    int64_t ld_dh, const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx, void* d_dw_gate,
+    void* d_dw_up, void* d_work, int64_t work_bytes, void* hip_stream);
+
+/*
+ * Rows in whole numbers of 8 bits with a scale for each: x ~ q s, s = m / 127
+ * with m the row's largest magnitude, at least 2^-100, and q = x (127 / m)
+ * rounded to nearest even.  A row with an infinity or a NaN has q = 0 and a
+ * scale that is a NaN.
+ *   d_x[rows x ld_x], d_q[rows x 16 ((cols+15)/16)] (zeros beyond cols,
+ *   aligned to 16), d_scales[rows]; cols: 1 .. 2^17.
+ */
+netsim_status netsim_rows_quantise(int32_t device, int64_t rows, int32_t cols, int32_t type,
+                                   const void* d_x, int64_t ld_x, int8_t* d_q, float* d_scales,
+                                   void* hip_stream);
+
+/*
+ * The experts' product with rows and weights in 8 bits, d_q, d_scales of
+ * `rows` rows and d_wq, d_w_scales of experts x n rows as
+ * netsim_rows_quantise gives them:
+ *   y_s[i] = (sum over c of q[c] wq_e[i][c]) s ws_e[i],
+ * the sum in whole numbers, times the row's scale, times the channel's, each
+ * rounded to 32 bits, and the result [slots x ld_y] to out_type.  Slots, rows
+ * and offsets as in netsim_experts_product.
+ */
+netsim_status netsim_experts_product8(int32_t device, int32_t experts, int64_t slots, int32_t n,
+                                      int32_t cols, int64_t rows, const int8_t* d_q,
+                                      const float* d_scales, const int32_t* d_row_of_slot,
+                                      const int32_t* d_offsets, const int8_t* d_wq,
+                                      const float* d_w_scales, int32_t out_type, void* d_y,
+                                      int64_t ld_y, void* hip_stream);
+
+/*
+ * An AdamW step (number `step`, from 1 on) over many tensors, in place:
+ *   g = grad * grad_scale
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = (1 - lr weight_decay) p
+ *       - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in 32 bits, every product and sum rounded on its own; factors are rounded
+ * to 32 bits once.  With bits = 32 d_m and d_v are float arrays.  With
+ * bits = 8 they hold m and sqrt(v) as 8-bit floats (4 exponent bits, 3 of
+ * mantissa, without infinities; 256 ((size+255)/256) of them, zeros beyond the
+ * tensor, aligned to 8), each the value times 448 / t of its block of 256
+ * elements, rounded to nearest even, t the block's largest magnitude, and
+ * d_m_scales, d_v_scales[(size+255)/256] hold t / 448 (both 0 where t is below
+ * 2^-100; a root above zero does not round to zero).  A block that got an
+ * infinity or a NaN has a scale that is a NaN.
+ * d_p may have 16 bits, with a copy in 32 (d_master, or NULL), which is then
+ * what is updated and d_p its rounding.  Arrays are contiguous and must not
+ * overlap.  The list is on the host and read before the call returns; a graph
+ * captures its addresses and the call's numbers.  d_counter (or NULL): 16 bytes
+ * on the device, aligned to 8, whose first 8 are the number of steps so far
+ * (int64).  The call then counts there, on its stream, instead of taking `step`,
+ * so that a replayed graph counts on; the other 8 bytes are the call's own.
+ */
+typedef struct {
+  void* d_p;
+  const void* d_g;
+  void *d_m, *d_v;
+  float *d_m_scales, *d_v_scales;   /* bits = 8                                */
+  float* d_master;                  /* or NULL                                 */
+  int64_t size;
+  int32_t p_type, g_type;
+} netsim_adamw_tensor;
+netsim_status netsim_adamw(int32_t device, int32_t tensors, const netsim_adamw_tensor* list,
+                           int32_t bits, int64_t step, void* d_counter, double lr, double beta1,
+                           double beta2, double eps, double weight_decay, double grad_scale,
+                           void* hip_stream);
+
 /* Message of the last failure on h (or of the calling thread when h is NULL). */
 const char* netsim_last_error(const netsim_t* h);
 

@@ -1,0 +1,274 @@
+// An AdamW step over many tensors at once, with moments in 32 or in 8 bits.
+//
+//   g = grad * grad_scale              r = sqrt(v)
+//   m = b1 m + (1 - b1) g              d = m / (r / sqrt(1 - b2^t) + eps)
+//   v = b2 v + (1 - b2) g^2            p = (1 - lr decay) p - lr / (1 - b1^t) d
+//
+// One pass over the data, bound by memory: a bfloat16 parameter with a 32-bit
+// copy takes 28 bytes, one with moments in 8 bits 10.  In 32 bits every
+// product and sum rounds on its own, quotients and roots to nearest.
+//
+// Moments in 8 bits: m and r (not v: the root halves the range) as floats of
+// 4 exponent and 3 mantissa bits, 256 elements of a tensor sharing a 32-bit
+// scale that makes the block's largest magnitude the type's largest, 448.  So
+// the scale follows the largest exactly, and a moment that falls by less than
+// a step of its own still falls with it.  A root above zero stays above zero:
+// m / r of a root rounded to zero would be a step without bound.
+#include <math.h>
+
+#include "values.h"
+
+namespace netsim_ops {
+namespace {
+
+constexpr int kScaled = 256;                      // elements that share a scale
+constexpr float kLeast = 7.888609052210118e-31f;  // 2^-100: a block whose largest is below is saved as zeros
+constexpr int kTensors = 40;                      // of a launch
+constexpr int kChunk = 4096;                      // elements a workgroup takes at a time
+
+struct One {
+  void* p;
+  const void* g;
+  void *m, *v;
+  float *m_scales, *v_scales, *master;
+  int64_t n;
+  int64_t chunk;    // the first of the launch's chunks that is this tensor's
+  int32_t p_type, g_type;
+};
+struct Many {
+  One one[kTensors];
+  int32_t count;
+  int64_t chunks;
+};
+struct Factors {
+  float b1, b2, c1, c2;   // c: 1 - b
+  float keep, rate, root, eps, grad_scale;
+};
+// A step's number on the device, and what follows from it.
+struct Counter {
+  int64_t step;
+  float rate, root;
+};
+__host__ __device__ inline void corrections(int64_t step, double lr, double b1, double b2, float* rate, float* root) {
+  *rate = (float)(lr / (1 - pow(b1, (double)step)));
+  *root = (float)(1 / sqrt(1 - pow(b2, (double)step)));
+}
+__global__ void count_kernel(Counter* c, double lr, double b1, double b2) {
+  c->step += 1;
+  corrections(c->step, lr, b1, b2, &c->rate, &c->root);
+}
+
+template <class T>
+__device__ __forceinline__ void load8(const void* base, int64_t at, int left, float (&v)[8]) {
+  const Eight<T> e = load_some(static_cast<const T*>(base) + at, left);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = value_of(e, j);
+}
+// The type is the same for the workgroup.
+__device__ __forceinline__ void load8(int32_t type, const void* base, int64_t at, int left, float (&v)[8]) {
+  if (type == NETSIM_F32)
+    load8<float>(base, at, left, v);
+  else if (type == NETSIM_BF16)
+    load8<bf16>(base, at, left, v);
+  else
+    load8<f16>(base, at, left, v);
+}
+__device__ __forceinline__ void store8(int32_t type, void* base, int64_t at, int left, const float (&v)[8]) {
+  if (type == NETSIM_F32)
+    store_some(static_cast<float*>(base) + at, v, left);
+  else if (type == NETSIM_BF16)
+    store_some(static_cast<bf16*>(base) + at, v, left);
+  else
+    store_some(static_cast<f16*>(base) + at, v, left);
+}
+
+__device__ __forceinline__ void widen(uint2 q, float scale, float (&v)[8]) {
+  const uint32_t w[2] = {q.x, q.y};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[h], true);
+    v[4 * h] = lo[0] * scale;
+    v[4 * h + 1] = lo[1] * scale;
+    v[4 * h + 2] = hi[0] * scale;
+    v[4 * h + 3] = hi[1] * scale;
+  }
+}
+
+// Eight values of a block that 32 lanes hold, in 8 bits; the block's scale.
+template <bool POSITIVE>
+__device__ __forceinline__ uint2 narrow(const float (&v)[8], float* scale) {
+  float top = 0.0f;
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    odd |= !isfinite(v[j]);
+    top = fmaxf(top, fabsf(v[j]));
+  }
+  if (odd) top = INFINITY;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const bool defined = top < INFINITY, zero = top < kLeast;
+  const float up = zero ? 0.0f : 448.0f / top;
+  *scale = !defined ? NAN : zero ? 0.0f : top / 448.0f;
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float s[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] = defined ? __builtin_amdgcn_fmed3f(v[4 * h + j] * up, -448.0f, 448.0f) : 0.0f;
+    int word = __builtin_amdgcn_cvt_pk_fp8_f32(s[0], s[1], 0, false);
+    word = __builtin_amdgcn_cvt_pk_fp8_f32(s[2], s[3], word, true);
+    if constexpr (POSITIVE)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (((uint32_t)word >> (8 * j) & 0xff) == 0 && v[4 * h + j] > 0.0f && !zero && defined) word |= 1 << (8 * j);
+    w[h] = (uint32_t)word;
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// The tensor that holds chunk c.
+__device__ __forceinline__ int tensor_of(const Many& many, int64_t c) {
+  int low = 0, high = many.count;
+  while (high - low > 1) {
+    const int mid = (low + high) / 2;
+    (many.one[mid].chunk <= c ? low : high) = mid;
+  }
+  return low;
+}
+
+// A lane takes eight elements in a row, so 32 lanes hold a block of 8-bit
+// moments.
+template <bool EIGHT>
+__global__ __launch_bounds__(256) void adamw_kernel(Many many, Factors f, const Counter* __restrict__ counter) {
+  if (counter) {
+    f.rate = counter->rate;
+    f.root = counter->root;
+  }
+  for (int64_t c = blockIdx.x; c < many.chunks; c += gridDim.x) {
+    const One& t = many.one[tensor_of(many, c)];
+    const int64_t first = (c - t.chunk) * kChunk;
+    for (int part = 0; part < kChunk / 2048; ++part) {
+      const int64_t at = first + part * 2048 + threadIdx.x * 8;
+      if (first + part * 2048 >= t.n) break;   // the same for the workgroup
+      const int left = (int)min(max(t.n - at, (int64_t)0), (int64_t)8);
+      float p[8], g[8], m[8], v[8], r[8];
+      load8(t.g_type, t.g, at, left, g);
+      if (t.master)
+        load8<float>(t.master, at, left, p);
+      else
+        load8(t.p_type, t.p, at, left, p);
+      const int64_t block = at / kScaled, blocks = (t.n + kScaled - 1) / kScaled;
+      if constexpr (EIGHT) {
+        uint2 qm = make_uint2(0, 0), qv = qm;
+        float sm = 0.0f, sv = 0.0f;
+        if (block < blocks) {
+          qm = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + at);
+          qv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + at);
+          sm = t.m_scales[block];
+          sv = t.v_scales[block];
+        }
+        widen(qm, sm, m);
+        widen(qv, sv, r);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = r[j] * r[j];
+      } else {
+        load8<float>(t.m, at, left, m);
+        load8<float>(t.v, at, left, v);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        g[j] *= f.grad_scale;
+        m[j] = m[j] * f.b1 + g[j] * f.c1;
+        v[j] = v[j] * f.b2 + g[j] * g[j] * f.c2;
+        r[j] = sqrtf(v[j]);
+        p[j] = p[j] * f.keep - m[j] / (r[j] * f.root + f.eps) * f.rate;
+      }
+      store8(t.p_type, t.p, at, left, p);
+      if (t.master) store_some(t.master + at, p, left);
+      if constexpr (EIGHT) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {   // beyond the tensor: zeros
+          m[j] = j < left ? m[j] : 0.0f;
+          r[j] = j < left ? r[j] : 0.0f;
+        }
+        float sm, sv;
+        const uint2 qm = narrow<false>(m, &sm), qv = narrow<true>(r, &sv);
+        if (block < blocks) {
+          *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.m) + at) = qm;
+          *reinterpret_cast<uint2*>(static_cast<uint8_t*>(t.v) + at) = qv;
+          if ((threadIdx.x & 31) == 0) {
+            t.m_scales[block] = sm;
+            t.v_scales[block] = sv;
+          }
+        }
+      } else {
+        store_some(static_cast<float*>(t.m) + at, m, left);
+        store_some(static_cast<float*>(t.v) + at, v, left);
+      }
+    }
+  }
+}
+
+}  // namespace
+}  // namespace netsim_ops
+
+using namespace netsim_ops;
+
+extern "C" netsim_status netsim_adamw(int32_t device, int32_t tensors, const netsim_adamw_tensor* list, int32_t bits, int64_t step,
+                                      void* d_counter, double lr, double beta1, double beta2, double eps, double weight_decay, double grad_scale,
+                                      void* hip_stream) {
+  const char* what = "adamw";
+  return entry(what, device, [&] {
+    if (tensors < 0 || (tensors > 0 && !list)) return fail(NETSIM_E_INVALID, what, "bad list of tensors");
+    if (bits != 8 && bits != 32) return fail(NETSIM_E_INVALID, what, "moments have 8 or 32 bits");
+    if (!d_counter && step < 1) return fail(NETSIM_E_INVALID, what, "the first step is 1");
+    if (!aligned(d_counter, 8)) return fail(NETSIM_E_INVALID, what, "d_counter is not aligned to 8 bytes");
+    if (!(beta1 >= 0 && beta1 < 1 && beta2 >= 0 && beta2 < 1)) return fail(NETSIM_E_INVALID, what, "betas must be 0 .. below 1");
+    if (!(eps > 0 && eps < INFINITY)) return fail(NETSIM_E_INVALID, what, "eps must be above 0");
+    if (!(lr >= 0 && lr < INFINITY && weight_decay >= 0 && weight_decay < INFINITY) || !std::isfinite(grad_scale))
+      return fail(NETSIM_E_INVALID, what, "lr, weight_decay and grad_scale must be finite, the first two not below 0");
+    bool any = d_counter != nullptr;
+    for (int32_t i = 0; i < tensors; ++i) {
+      const netsim_adamw_tensor& t = list[i];
+      if (t.size < 0 || t.size > (int64_t)1 << 40) return fail(NETSIM_E_INVALID, what, "bad size");
+      if (!type_ok(t.p_type) || !type_ok(t.g_type)) return fail(NETSIM_E_INVALID, what, "bad type");
+      if (t.size == 0) continue;
+      any = true;
+      if (!t.d_p || !t.d_g || !t.d_m || !t.d_v || (bits == 8 && (!t.d_m_scales || !t.d_v_scales)))
+        return fail(NETSIM_E_INVALID, what, "NULL array");
+      if (!aligned(t.d_p, type_size(t.p_type)) || !aligned(t.d_g, type_size(t.g_type)) || !aligned(t.d_m, bits == 8 ? 8 : 4) ||
+          !aligned(t.d_v, bits == 8 ? 8 : 4) || !aligned(t.d_m_scales, 4) || !aligned(t.d_v_scales, 4) || !aligned(t.d_master, 4))
+        return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or moments in 8 bits to 8 bytes");
+      if (t.d_master && t.p_type == NETSIM_F32) return fail(NETSIM_E_INVALID, what, "a copy in 32 bits is for parameters of 16");
+    }
+    if (!any) return (netsim_status)NETSIM_OK;
+    Factors f{(float)beta1, (float)beta2, (float)(1 - beta1), (float)(1 - beta2), (float)(1 - lr * weight_decay), 0.0f, 0.0f, (float)eps,
+              (float)grad_scale};
+    Counter* counter = static_cast<Counter*>(d_counter);
+    if (!counter) corrections(step, lr, beta1, beta2, &f.rate, &f.root);
+    return launch(what, device, [&] {
+      if (counter) hipLaunchKernelGGL(count_kernel, dim3(1), dim3(1), 0, static_cast<hipStream_t>(hip_stream), counter, lr, beta1, beta2);
+      Many many;
+      many.count = 0;
+      many.chunks = 0;
+      auto go = [&] {
+        if (many.count == 0) return;
+        const int64_t most = 2048;
+        const dim3 grid((unsigned)(many.chunks < most ? many.chunks : most));
+        hipLaunchKernelGGL(bits == 8 ? adamw_kernel<true> : adamw_kernel<false>, grid, dim3(256), 0, static_cast<hipStream_t>(hip_stream),
+                           many, f, counter);
+        many.count = 0;
+        many.chunks = 0;
+      };
+      for (int32_t i = 0; i < tensors; ++i) {
+        const netsim_adamw_tensor& t = list[i];
+        if (t.size == 0) continue;
+        many.one[many.count++] = One{t.d_p, t.d_g, t.d_m, t.d_v, t.d_m_scales, t.d_v_scales, t.d_master, t.size, many.chunks, t.p_type, t.g_type};
+        many.chunks += ceil_div(t.size, kChunk);
+        if (many.count == kTensors) go();
+      }
+      go();
+    });
+  });
+}

@@ -1,0 +1,207 @@
+// Rows in whole numbers of 8 bits with a scale for each, and the products of
+// experts with such rows and weights.
+//
+// A row x is q s with s = m / 127, m its largest magnitude (at least 2^-100)
+// and q = x (127 / m) rounded to nearest even.  The products' sums are whole
+// numbers of 32 bits, so their only roundings are those of the two scales:
+//   y_s[n] = (sum over c of q_x[c] q_w[n][c]) s_x s_w[n].
+#include <math.h>
+
+#include "parts.h"
+#include "tile.h"
+
+namespace netsim_ops {
+namespace {
+
+constexpr float kTiny = 7.888609052210118e-31f;   // 2^-100: 127 / m stays finite
+constexpr int kMaxEight = 1 << 17;                // 127 127 2^17 < 2^31
+
+inline int64_t padded(int64_t cols) { return ceil_div(cols, 16) * 16; }
+
+// A workgroup per row.
+template <class T>
+__global__ __launch_bounds__(256) void quantise_kernel(int cols, int pitch, const T* __restrict__ x, int64_t ld,
+                                                       int8_t* __restrict__ q, float* __restrict__ scales) {
+  constexpr int HELD = 4;   // chunks of eight values that stay in registers
+  __shared__ float tops[4];
+  const int64_t row = blockIdx.x;
+  const T* from = x + row * ld;
+  Eight<T> v[HELD];
+  float top = 0.0f;
+  bool odd = false;
+  auto look = [&](const Eight<T>& e) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float f = value_of(e, j);
+      odd |= !isfinite(f);
+      top = fmaxf(top, fabsf(f));
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int c = (i * 256 + threadIdx.x) * 8;
+    v[i] = load_some(from + c, cols - c);
+    look(v[i]);
+  }
+  for (int c = (HELD * 256 + threadIdx.x) * 8; c < cols; c += 2048) look(load_some(from + c, cols - c));
+  if (odd) top = INFINITY;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), kTiny);
+  const bool defined = top < INFINITY;
+  const float up = 127.0f / top;
+  if (threadIdx.x == 0) scales[row] = defined ? top / 127.0f : NAN;
+  auto put = [&](const Eight<T>& e, int c) {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int n = defined ? (int)rintf(value_of(e, j) * up) : 0;
+      w[j >> 2] |= (uint32_t)(uint8_t)(int8_t)n << (8 * (j & 3));
+    }
+    *reinterpret_cast<uint2*>(q + row * pitch + c) = make_uint2(w[0], w[1]);
+  };
+#pragma unroll
+  for (int i = 0; i < HELD; ++i) {
+    const int c = (i * 256 + threadIdx.x) * 8;
+    if (c < pitch) put(v[i], c);
+  }
+  for (int c = (HELD * 256 + threadIdx.x) * 8; c < pitch; c += 2048) put(load_some(from + c, cols - c), c);
+}
+
+struct Eights {
+  int experts, slots, n, pitch;
+  int64_t rows;
+  const int8_t* x;
+  const float* x_scales;
+  const int32_t *map, *offsets;
+  const int8_t* w;
+  const float* w_scales;
+  int64_t tiles;
+  int tiles_n;
+};
+
+__device__ __forceinline__ int64_t row_of(const Eights& p, int slot) {
+  const int64_t r = p.map ? p.map[slot] : slot;
+  return r >= 0 && r < p.rows ? r : -1;
+}
+
+template <class O, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
+  using M = Tile<int8_t, BM, BN, WM, WN>;
+  using A = RowTile<int8_t, BM, M::THREADS, true>;
+  using B = RowTile<int8_t, BN, M::THREADS, true>;
+  extern __shared__ __align__(16) char shared[];
+  const int64_t tile = tile_of_group(blockIdx.x);
+  if (tile >= p.tiles) return;
+  const int n0 = (int)(tile % p.tiles_n) * BN;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
+  if (rows.expert < -1) return;
+  const int count = rows.to - rows.from, lane = threadIdx.x & 63;
+
+  M m;
+  const int64_t first = (int64_t)max(rows.expert, 0) * p.n;
+  if (rows.expert >= 0 && p.rows > 0) {
+    A a;
+    B b;
+    a.open([&](int r) {
+      const int64_t at = row_of(p, rows.from + min(r, count - 1));
+      return p.x + (at < 0 ? 0 : at) * p.pitch;
+    });
+    b.open([&](int r) { return p.w + (first + min(n0 + r, p.n - 1)) * p.pitch; });
+    m.template run<A, B>(
+        shared, (p.pitch + A::STEP - 1) / A::STEP,
+        [&](Place stage, int s) {
+          a.load(stage, s * A::STEP, p.pitch);
+          b.load(stage + BM * kStepBytes, s * A::STEP, p.pitch);
+        },
+        [](Place) {});
+  }
+  float x_scale[M::FM], w_scale[M::FN][16];
+  bool held[M::FM];
+#pragma unroll
+  for (int i = 0; i < M::FM; ++i) {
+    const int r = M::row0() + i * 32 + (lane & 31);
+    const int64_t at = rows.expert >= 0 && r < count ? row_of(p, rows.from + r) : -1;
+    held[i] = at >= 0;
+    x_scale[i] = held[i] ? p.x_scales[at] : 0.0f;
+  }
+#pragma unroll
+  for (int j = 0; j < M::FN; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      w_scale[j][r] = p.w_scales[first + min(n0 + M::col0() + j * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), p.n - 1)];
+  M::template write<BN, M::FN>(shared, out + (int64_t)rows.from * ld_out + n0, ld_out, count, p.n - n0,
+                               [&](int j) { return M::col0() + j * 32; },
+                               [&](int i, int j, int r) { return held[i] ? (float)m.sum[i][j][r] * x_scale[i] * w_scale[j][r] : 0.0f; });
+}
+
+}  // namespace
+}  // namespace netsim_ops
+
+using namespace netsim_ops;
+
+extern "C" netsim_status netsim_rows_quantise(int32_t device, int64_t rows, int32_t cols, int32_t type, const void* d_x,
+                                              int64_t ld_x, int8_t* d_q, float* d_scales, void* hip_stream) {
+  const char* what = "rows_quantise";
+  return entry(what, device, [&] {
+    if (!type_ok(type)) return fail(NETSIM_E_INVALID, what, "bad type");
+    if (rows < 0 || cols < 1 || cols > kMaxEight) return fail(NETSIM_E_INVALID, what, "bad rows or cols");
+    if (ld_x < cols) return fail(NETSIM_E_INVALID, what, "ld_x is below cols");
+    if (rows == 0) return (netsim_status)NETSIM_OK;
+    if (!d_x || !d_q || !d_scales) return fail(NETSIM_E_INVALID, what, "NULL array");
+    if (!aligned(d_x, type_size(type)) || !aligned(d_q, 16) || !aligned(d_scales, 4))
+      return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or d_q to 16 bytes");
+    const int pitch = (int)padded(cols);
+    if (rows > ((int64_t)1 << 40) / pitch) return fail(NETSIM_E_INVALID, what, "more than 2^40 values");
+    return launch(what, device, [&] {
+      with_type(type, [&](auto t) {
+        using T = decltype(t);
+        in_launches(rows, 1 << 22, [&](int64_t first, int64_t n) {
+          hipLaunchKernelGGL(quantise_kernel<T>, dim3((unsigned)n), dim3(256), 0, static_cast<hipStream_t>(hip_stream), cols, pitch,
+                             static_cast<const T*>(d_x) + first * ld_x, ld_x, d_q + first * pitch, d_scales + first);
+        });
+      });
+    });
+  });
+}
+
+extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                                 int64_t rows, const int8_t* d_q, const float* d_scales,
+                                                 const int32_t* d_row_of_slot, const int32_t* d_offsets, const int8_t* d_wq,
+                                                 const float* d_w_scales, int32_t out_type, void* d_y, int64_t ld_y,
+                                                 void* hip_stream) {
+  const char* what = "experts_product8";
+  return entry(what, device, [&] {
+    if (!type_ok(out_type)) return fail(NETSIM_E_INVALID, what, "bad type");
+    if (experts < 1 || experts > 1024 || slots < 0 || slots > kMaxSlots || n < 1 || n > kMaxCols || cols < 1 || cols > kMaxEight)
+      return fail(NETSIM_E_INVALID, what, "experts must be 1 .. 1024, n 1 .. 2^20, cols 1 .. 2^17, slots 0 .. 2^31-4097");
+    if (rows < 0) return fail(NETSIM_E_INVALID, what, "rows is below 0");
+    if (!d_row_of_slot && rows != slots) return fail(NETSIM_E_INVALID, what, "without a list of rows there must be one for every slot");
+    if (!d_offsets && experts != 1) return fail(NETSIM_E_INVALID, what, "several experts need offsets");
+    if (ld_y < n) return fail(NETSIM_E_INVALID, what, "ld_y is below n");
+    if (slots == 0) return (netsim_status)NETSIM_OK;
+    if ((rows > 0 && (!d_q || !d_scales)) || !d_wq || !d_w_scales || !d_y) return fail(NETSIM_E_INVALID, what, "NULL array");
+    if (!aligned(d_q, 16) || !aligned(d_wq, 16) || !aligned(d_scales, 4) || !aligned(d_w_scales, 4) || !aligned(d_row_of_slot, 4) ||
+        !aligned(d_offsets, 4) || !aligned(d_y, type_size(out_type)))
+      return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or whole numbers to 16 bytes");
+    return launch(what, device, [&] {
+      with_type(out_type, [&](auto o) {
+        using O = decltype(o);
+        auto run = [&](auto kernel, int bm, int bn, int threads, int lds) {
+          Eights p{experts, (int)slots, n, (int)padded(cols), rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales, 0, 0};
+          p.tiles_n = (int)ceil_div(n, bn);
+          p.tiles = p.tiles_n * most_rows_tiles(experts, slots, bm, d_offsets);
+          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+          hipLaunchKernelGGL(kernel, dim3((unsigned)groups_of_tiles(p.tiles)), dim3(threads), lds, static_cast<hipStream_t>(hip_stream),
+                             p, static_cast<O*>(d_y), ld_y);
+        };
+        if (slots / experts >= 256)
+          run(eight_kernel<O, 256, 256, 2, 4>, 256, 256, 512, Tile<int8_t, 256, 256, 2, 4>::LDS);
+        else
+          run(eight_kernel<O, 128, 128, 2, 2>, 128, 128, 256, Tile<int8_t, 128, 128, 2, 2>::LDS);
+      });
+    });
+  });
+}

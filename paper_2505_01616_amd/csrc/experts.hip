@@ -1,0 +1,586 @@
+// The products of experts with rows by slot, and their gradients.
+//
+//   product:  y_s = x W_e^T                    (x: the row of slot s, e its expert)
+//   gated:    h_s = act(g) u, g = x Wg_e^T, u = x Wu_e^T
+//
+// gated's backward pass computes g and u again, from which
+//   dg = dh u act'(g), du = dh act(g)          (rounded to the inputs' type)
+// and then, as product's does from dy, the rows' gradient dg Wg + du Wu and
+// the weights', the sums of dg x and du x over an expert's slots.  All of it
+// is products by tiles (tile.h); what differs is which index of an operand is
+// the summed one, and what becomes of the sums.
+#include <math.h>
+
+#include "parts.h"
+#include "tile.h"
+
+namespace netsim_ops {
+namespace {
+
+// What a call's kernels are given.  n and k: rows and columns of an expert's
+// matrix.
+template <class T>
+struct Products {
+  int experts, slots, n, k;
+  int64_t rows, ld;         // of x
+  const T* x;
+  const int32_t* map;       // slots' rows; NULL: a slot's row has its number
+  const int32_t* offsets;   // NULL: one expert has all slots
+  const T* w[2];
+  int64_t tiles;            // of a launch
+  int tiles_n;
+};
+
+// The row of a slot, -1 for none.
+template <class T>
+__device__ __forceinline__ int64_t row_of(const Products<T>& p, int slot) {
+  const int64_t r = p.map ? p.map[slot] : slot;
+  return r >= 0 && r < p.rows ? r : -1;
+}
+
+// act(g) and its derivative.
+struct Slope {
+  float act, slope;
+};
+struct Silu {
+  static __device__ __forceinline__ Slope at(float g) {
+    const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504f));
+    return {g * p, p * (1.0f + g * (1.0f - p))};
+  }
+};
+// The normal distribution's function from erfc(z) = t exp(q(t) - z^2), t =
+// 2 / (2 + z), q the polynomial of degree 7 that is nearest log(erfc(z)
+// exp(z^2) / t) at Chebyshev's points of 0 <= z <= 14: off by 3e-6 of erfc up
+// to z = 4.5, by 8e-6 beyond, where results have at most 12 bits.
+struct Gelu {
+  static __device__ __forceinline__ Slope at(float g) {
+    constexpr float Q[8] = {-1.26544062f, 0.997983451f, 0.397944044f, -0.0533622151f, 0.376357389f, -1.03015518f, 0.768512808f, -0.191840475f};
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.35355339f * fabsf(g)), e = g * g * -0.5f;
+    float q = Q[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) q = fmaf(q, t, Q[i]);
+    const float half = 0.5f * t * __builtin_amdgcn_exp2f((q + e) * 1.44269504f), p = g < 0.0f ? half : 1.0f - half;
+    return {g * p, p + g * __builtin_amdgcn_exp2f(e * 1.44269504f) * 0.39894228f};
+  }
+};
+template <class F>
+__device__ __forceinline__ void with_activation(int kind, F&& f) {
+  if (kind == NETSIM_SILU)
+    f(Silu{});
+  else
+    f(Gelu{});
+}
+
+enum Out { PRODUCT, GATED, GATED_BACK };
+
+// Four values of a row in shared memory, from a multiple of eight bytes on.
+template <class T>
+__device__ __forceinline__ Eight<T> quad(const T* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return Eight<T>{{w.x, w.y, 0, 0}};
+}
+
+// Rows by slot.  PRODUCT: out = y.  GATED: out = h; a tile's columns are 32 of
+// g and 32 of u in turn, so that a lane holds both of an element.  GATED_BACK:
+// out = dg, out2 = du, both [slots x ld_out].
+template <class T, int OUT, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN) void rows_kernel(Products<T> p, int activation, const T* __restrict__ dy,
+                                                            int64_t ld_dy, T* __restrict__ out, T* __restrict__ out2,
+                                                            int64_t ld_out) {
+  using M = Tile<T, BM, BN, WM, WN>;
+  using A = RowTile<T, BM, M::THREADS, DIRECT>;
+  using B = RowTile<T, BN, M::THREADS, DIRECT>;
+  constexpr int COLS = OUT == PRODUCT ? BN : BN / 2, JN = OUT == PRODUCT ? M::FN : M::FN / 2;
+  extern __shared__ __align__(16) char shared[];
+  const int64_t tile = tile_of_group(blockIdx.x);
+  if (tile >= p.tiles) return;
+  const int n0 = (int)(tile % p.tiles_n) * COLS;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
+  if (rows.expert < -1) return;
+  const int count = rows.to - rows.from, lane = threadIdx.x & 63;
+
+  M m;
+  bool held[M::FM];   // whether there is a row for this lane's slots
+#pragma unroll
+  for (int i = 0; i < M::FM; ++i) {
+    const int r = M::row0() + i * 32 + (lane & 31);
+    held[i] = rows.expert >= 0 && r < count && row_of(p, rows.from + r) >= 0;
+  }
+  if (rows.expert >= 0 && p.rows > 0) {
+    A a;
+    B b;
+    a.open([&](int r) {
+      const int64_t at = row_of(p, rows.from + min(r, count - 1));
+      return p.x + (at < 0 ? 0 : at) * p.ld;
+    });
+    const int64_t first = (int64_t)rows.expert * p.n;
+    b.open([&](int r) {
+      if constexpr (OUT == PRODUCT) return p.w[0] + (first + min(n0 + r, p.n - 1)) * p.k;
+      constexpr int W = BN / WN;   // columns of a wave: half of them g's
+      const int n = n0 + r / W * (W / 2) + r % (W / 2);
+      return p.w[r % W / (W / 2)] + (first + min(n, p.n - 1)) * p.k;
+    });
+    m.template run<A, B>(
+        shared, (p.k + A::STEP - 1) / A::STEP,
+        [&](Place stage, int s) {
+          a.load(stage, s * A::STEP, p.k);
+          b.load(stage + BM * kStepBytes, s * A::STEP, p.k);
+        },
+        [&](Place stage) {
+          a.store(stage);
+          b.store(stage + BM * kStepBytes);
+        });
+  }
+  auto col = [&](int j) { return M::col0() / (M::FN / JN) + j * 32; };
+  T* to = out + (int64_t)rows.from * ld_out + n0;
+  if constexpr (OUT == PRODUCT) {
+    M::template write<COLS, JN>(shared, to, ld_out, count, p.n - n0, col,
+                                [&](int i, int j, int r) { return held[i] ? m.sum[i][j][r] : 0.0f; });
+  } else if constexpr (OUT == GATED) {
+    with_activation(activation, [&](auto act) {
+      M::template write<COLS, JN>(shared, to, ld_out, count, p.n - n0, col, [&](int i, int j, int r) {
+        return held[i] ? act.at(m.sum[i][j][r]).act * m.sum[i][j + JN][r] : 0.0f;
+      });
+    });
+  } else {
+    // the tile of dh, in whole lines through shared memory as well
+    constexpr int PITCH = COLS + 8;
+    static_assert(BM * PITCH * sizeof(T) <= M::LDS, "");
+    T* tile_dy = reinterpret_cast<T*>(shared);
+    for (int t = threadIdx.x; t < BM * COLS / 8; t += M::THREADS) {
+      const int r = t / (COLS / 8), c = t % (COLS / 8) * 8;
+      *reinterpret_cast<uint4*>(tile_dy + r * PITCH + c) =
+          chunk_of(dy + (int64_t)(rows.from + r) * ld_dy + n0 + c, r < count ? p.n - n0 - c : 0);
+    }
+    __syncthreads();
+    with_activation(activation, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < M::FM; ++i)
+#pragma unroll
+        for (int j = 0; j < JN; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const Eight<T> d = quad(tile_dy + (M::row0() + i * 32 + (lane & 31)) * PITCH + col(j) + 2 * r + 4 * (lane >> 5));
+#pragma unroll
+            for (int h = r; h < r + 4; ++h) {
+              const float v = value_of(d, h - r), u = m.sum[i][j + JN][h];
+              const Slope s = act.at(m.sum[i][j][h]);
+              m.sum[i][j][h] = held[i] ? v * u * s.slope : 0.0f;
+              m.sum[i][j + JN][h] = held[i] ? v * s.act : 0.0f;
+            }
+            // one after the other: together they need more registers than there are
+            __builtin_amdgcn_sched_barrier(0);
+          }
+    });
+    M::template write<COLS, JN>(shared, to, ld_out, count, p.n - n0, col, [&](int i, int j, int r) { return m.sum[i][j][r]; });
+    M::template write<COLS, JN>(shared, out2 + (int64_t)rows.from * ld_out + n0, ld_out, count, p.n - n0, col,
+                                [&](int i, int j, int r) { return m.sum[i][j + JN][r]; });
+  }
+}
+
+// Rows' gradients by slot: the sum over `pairs` of d W, d [slots x ld_d] of n
+// values a row.
+template <class T, class O, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN) void input_kernel(Products<T> p, int pairs, const T* __restrict__ d0,
+                                                             const T* __restrict__ d1, int64_t ld_d,
+                                                             O* __restrict__ dx) {
+  using M = Tile<T, BM, BN, WM, WN>;
+  using A = RowTile<T, BM, M::THREADS, DIRECT>;
+  using B = ColTile<T, BN, M::THREADS, DIRECT>;
+  extern __shared__ __align__(16) char shared[];
+  const int64_t tile = tile_of_group(blockIdx.x);
+  if (tile >= p.tiles) return;
+  const int c0 = (int)(tile % p.tiles_n) * BN;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
+  if (rows.expert < -1) return;
+  const int count = rows.to - rows.from;
+
+  M m;
+  if (rows.expert >= 0) {
+    A a;
+    B b;
+    a.open([&](int r) { return d0 + (int64_t)(rows.from + min(r, count - 1)) * ld_d; });
+    const T* w0 = p.w[0] + (int64_t)rows.expert * p.n * p.k;
+    b.open(w0, p.k, c0, p.k);
+    const int steps = (p.n + A::STEP - 1) / A::STEP;
+    m.template run<A, B>(
+        shared, steps * pairs,
+        [&](Place stage, int s) {
+          const bool second = s >= steps;
+          const int k0 = (second ? s - steps : s) * A::STEP;
+          a.load(stage, k0, p.n, second ? d1 - d0 : 0);
+          b.load(stage + BM * kStepBytes, [&](int i) { return k0 + b.row(i) < p.n ? k0 + b.row(i) : -1; },
+                 second ? p.w[1] - p.w[0] : 0);
+        },
+        [&](Place stage) {
+          a.store(stage);
+          b.store(stage + BM * kStepBytes);
+        });
+  }
+  M::template write<BN, M::FN>(shared, dx + (int64_t)rows.from * p.k + c0, p.k, count, p.k - c0,
+                               [&](int j) { return M::col0() + j * 32; },
+                               [&](int i, int j, int r) { return m.sum[i][j][r]; });
+}
+
+// dx[row] = the sum over the row's slots of their gradients, in the order of
+// the list.
+template <class T>
+__global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int cols, int each, int slots,
+                                                     const int32_t* __restrict__ slots_of_row,
+                                                     const float* __restrict__ by_slot, T* __restrict__ dx) {
+  const int64_t row = blockIdx.x;
+  const int32_t* list = slots_of_row + row * each;
+  for (int c = threadIdx.x * 4; c < cols; c += 1024) {
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < each; ++j) {
+      const int s = list[j];
+      if (s < 0 || s >= slots) continue;
+      const float* from = by_slot + (int64_t)s * cols + c;
+      for (int h = 0; h < 4; ++h)
+        if (c + h < cols) sum[h] += from[h];
+    }
+    for (int h = 0; h < 4; ++h)
+      if (c + h < cols) dx[row * cols + c + h] = (T)sum[h];
+  }
+}
+
+// The weights' gradients: dW[e][n][c] = the sum over e's slots of d[s][n]
+// x[row(s)][c].  Both factors have the summed index as their slow one.
+// blockIdx.z: the matrix.
+template <class T, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__(64 * WM * WN) void weight_kernel(Products<T> p, Sums g, Cut cut, const Item* __restrict__ items,
+                                                              const T* __restrict__ d0, const T* __restrict__ d1,
+                                                              int64_t ld_d, T* __restrict__ dw0, T* __restrict__ dw1,
+                                                              float* __restrict__ partials) {
+  using M = Tile<T, BM, BN, WM, WN>;
+  using A = ColTile<T, BM, M::THREADS, DIRECT>;
+  using B = ColTile<T, BN, M::THREADS, DIRECT>;
+  extern __shared__ __align__(16) char shared[];
+  const int tiles_n = (g.n + BM - 1) / BM;
+  const int n0 = (int)(blockIdx.x % tiles_n) * BM, c0 = (int)(blockIdx.x / tiles_n) * BN;
+  Item it;
+  if (cut.plan == Cut::WHOLE)
+    it = segment(p.offsets, blockIdx.y, g.slots);
+  else if (cut.plan == Cut::LISTED)
+    it = items[blockIdx.y];
+  else
+    find_part<false>(g, cut, p.offsets, blockIdx.y, &it, nullptr);
+  if (it.expert < 0) return;
+  if (p.rows == 0) it.to = it.from;
+
+  M m;
+  A a;
+  B b;
+  a.open(blockIdx.z ? d1 : d0, ld_d, n0, g.n);
+  b.open(p.x, p.ld, c0, g.cols);
+  m.template run<A, B>(
+      shared, (it.to - it.from + A::STEP - 1) / A::STEP,
+      [&](Place stage, int s) {
+        const int first = it.from + s * A::STEP;
+        // a slot without a row takes no part, whatever its d holds
+        a.load(stage, [&](int i) { const int k = first + a.row(i); return k < it.to && row_of(p, k) >= 0 ? k : -1; });
+        b.load(stage + BM * kStepBytes, [&](int i) -> int64_t { const int k = first + b.row(i); return k < it.to ? row_of(p, k) : -1; });
+      },
+      [&](Place stage) {
+        a.store(stage);
+        b.store(stage + BM * kStepBytes);
+      });
+  auto col = [&](int j) { return M::col0() + j * 32; };
+  auto value = [&](int i, int j, int r) { return m.sum[i][j][r]; };
+  const int64_t size = (int64_t)g.n * g.cols, at = (int64_t)n0 * g.cols + c0;
+  if (it.partial < 0)
+    M::template write<BN, M::FN>(shared, (blockIdx.z ? dw1 : dw0) + it.expert * size + at, g.cols, g.n - n0, g.cols - c0, col, value);
+  else
+    M::template write<BN, M::FN>(shared, partials + (blockIdx.z * cut.partials + it.partial) * size + at, g.cols, g.n - n0,
+                                 g.cols - c0, col, value);
+}
+
+// A tile's shape.
+template <class T, int BM_, int BN_, int WM_, int WN_, bool DIRECT_>
+struct Shape {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr bool DIRECT = DIRECT_;
+  using M = Tile<T, BM, BN, WM, WN>;
+};
+// Calls f with the shape for `size` (256 or 128).  Rows that are no whole
+// chunks pass through registers, which leaves too few for the larger tile.
+template <class T, class F>
+void with_tile(int size, bool direct, F&& f) {
+  if (!direct)
+    f(Shape<T, 128, 128, 2, 2, false>{});
+  else if (size == 256)
+    f(Shape<T, 256, 256, 2, 4, true>{});
+  else
+    f(Shape<T, 128, 128, 2, 2, true>{});
+}
+template <class F>
+void with_bool(bool b, F&& f) {
+  if (b)
+    f(std::true_type{});
+  else
+    f(std::false_type{});
+}
+template <class F>
+void with_16_bits(int32_t type, F&& f) {
+  if (type == NETSIM_BF16)
+    f(bf16{});
+  else
+    f(f16{});
+}
+
+constexpr int64_t kMaxGroups = 1 << 22;   // of a launch: 2^31 threads
+
+// What a call was given, checked.
+struct Call {
+  int32_t device, experts;
+  int64_t slots;
+  int32_t n, k, type;
+  int64_t rows;
+  const void* x;
+  int64_t ld;
+  const int32_t *map, *offsets;
+  const void* w[2];
+  int matrices;
+
+  template <class T>
+  Products<T> products() const {
+    return Products<T>{experts, (int)slots, n, k, rows, ld, static_cast<const T*>(x), map, offsets,
+                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0};
+  }
+  // Whether x's rows, and the weights', are whole chunks of 16 bytes.
+  bool x_direct() const { return ld % 8 == 0 && k % 8 == 0 && aligned(x, 16); }
+  bool w_direct() const { return k % 8 == 0 && aligned(w[0], 16) && aligned(w[1], 16); }
+};
+
+constexpr const char* kSizes = "experts must be 1 .. 1024, the matrices' rows and columns 1 .. 2^20, slots 0 .. 2^31-4097";
+bool sizes_ok(int32_t experts, int64_t slots, int32_t n, int32_t k) {
+  return experts >= 1 && experts <= 1024 && slots >= 0 && slots <= kMaxSlots && n >= 1 && n <= kMaxCols && k >= 1 && k <= kMaxCols;
+}
+
+netsim_status check(const char* what, const Call& c) {
+  if (c.type != NETSIM_BF16 && c.type != NETSIM_F16) return fail(NETSIM_E_INVALID, what, "the type must be of 16 bits");
+  if (!sizes_ok(c.experts, c.slots, c.n, c.k)) return fail(NETSIM_E_INVALID, what, kSizes);
+  if (c.rows < 0) return fail(NETSIM_E_INVALID, what, "rows is below 0");
+  if (c.ld < c.k) return fail(NETSIM_E_INVALID, what, "ld_x is below the row's length");
+  if (!c.map && c.rows != c.slots) return fail(NETSIM_E_INVALID, what, "without a list of rows there must be one for every slot");
+  if (!c.offsets && c.experts != 1) return fail(NETSIM_E_INVALID, what, "several experts need offsets");
+  if ((c.rows > 0 && !c.x) || !c.w[0] || !c.w[1]) return fail(NETSIM_E_INVALID, what, "NULL array");
+  if (!aligned(c.x, 2) || !aligned(c.w[0], 2) || !aligned(c.w[1], 2) || !aligned(c.map, 4) || !aligned(c.offsets, 4))
+    return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type");
+  return NETSIM_OK;
+}
+
+int tile_of(int64_t slots, int64_t experts, int64_t n, int64_t k) {
+  (void)n;
+  (void)k;
+  return slots / experts >= 256 ? 256 : 128;
+}
+
+template <class K, class... Args>
+void go(K kernel, dim3 grid, int threads, int lds, hipStream_t s, Args... args) {
+  (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
+}
+
+// Rows by slot (rows_kernel).
+template <int OUT>
+void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, void* out, void* out2, int64_t ld_out, hipStream_t s) {
+  with_16_bits(c.type, [&](auto t) {
+    using T = decltype(t);
+    with_tile<T>(tile_of(c.slots, c.experts, c.n, c.k), c.x_direct() && c.w_direct(), [&](auto shape) {
+      using S = decltype(shape);
+      auto p = c.products<T>();
+      p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? S::BN : S::BN / 2);
+      p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::BM, c.offsets);
+      go(rows_kernel<T, OUT, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3((unsigned)groups_of_tiles(p.tiles)), S::M::THREADS,
+         S::M::LDS, s, p, activation, static_cast<const T*>(dy), ld_dy, static_cast<T*>(out), static_cast<T*>(out2), ld_out);
+    });
+  });
+}
+
+// Workspace of a backward pass, each array from a multiple of 256 bytes on.
+struct Space {
+  int64_t d[2] = {0, 0}, by_slot = 0, list = 0, partials = 0, bytes = 0;
+  int64_t ld_d = 0;
+
+  int64_t take(int64_t size) {
+    const int64_t at = bytes;
+    bytes += ceil_div(size, 256) * 256;
+    return at;
+  }
+};
+
+// How the weights' sums are cut (parts.h).
+Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t k, bool offsets) {
+  Cut c{};
+  c.tile = tile_of(slots, experts, n, k);
+  c.step = 64;
+  c.plan = Cut::WHOLE;
+  return c;
+}
+
+Space space_of(const Cut& cut, int matrices, int64_t slots, int64_t n, int64_t k, bool list) {
+  Space s;
+  s.ld_d = ceil_div(n, 8) * 8;
+  if (matrices == 2)
+    for (int64_t& d : s.d) d = s.take(slots * s.ld_d * 2);
+  if (list) s.by_slot = s.take(slots * k * 4);
+  s.list = s.take(16 * (cut.items + cut.joins));
+  s.partials = s.take(4 * matrices * cut.partials * n * k);
+  return s;
+}
+
+// The gradients of x (NULL: none) and the weights (NULL: none) from d, whose
+// rows are the slots'.
+void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work, const void* d0, const void* d1, int64_t ld_d,
+                   const int32_t* slots_of_row, int32_t each, void* dx, void* dw0, void* dw1, hipStream_t s) {
+  const bool d_direct = ld_d % 8 == 0 && c.n % 8 == 0 && aligned(d0, 16) && aligned(d1, 16);
+  with_16_bits(c.type, [&](auto t) {
+    using T = decltype(t);
+    if (dx && c.slots > 0)
+      with_tile<T>(tile_of(c.slots, c.experts, c.n, c.k), d_direct && c.w_direct(), [&](auto shape) {
+        with_bool(c.map != nullptr, [&](auto mapped) {
+          using S = decltype(shape);
+          using O = std::conditional_t<decltype(mapped)::value, float, T>;
+          auto p = c.products<T>();
+          p.tiles_n = (int)ceil_div(c.k, S::BN);
+          p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::BM, c.offsets);
+          go(input_kernel<T, O, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3((unsigned)groups_of_tiles(p.tiles)), S::M::THREADS,
+             S::M::LDS, s, p, c.matrices, static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
+             static_cast<O*>(decltype(mapped)::value ? static_cast<void*>(work + space.by_slot) : dx));
+        });
+      });
+    if (dx && c.map && c.rows > 0)
+      in_launches(c.rows, kMaxGroups, [&](int64_t first, int64_t n) {
+        hipLaunchKernelGGL(gather_kernel<T>, dim3((unsigned)n), dim3(256), 0, s, n, c.k, each, (int)c.slots,
+                           slots_of_row + first * each, reinterpret_cast<const float*>(work + space.by_slot),
+                           static_cast<T*>(dx) + first * c.k);
+      });
+    if (dw0)
+      with_tile<T>(cut.tile, d_direct && c.x_direct(), [&](auto shape) {
+        using S = decltype(shape);
+        const Sums g{c.experts, c.n, c.k, (int)c.slots, c.k % 4 == 0 && aligned(dw0, 8) && (c.matrices < 2 || aligned(dw1, 8))};
+        Item* items = reinterpret_cast<Item*>(work + space.list);
+        Join* joins = reinterpret_cast<Join*>(items + cut.items);
+        float* partials = reinterpret_cast<float*>(work + space.partials);
+        if (cut.plan == Cut::LISTED)
+          hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(c.experts, 64) * 64), 0, s, g, cut, c.offsets, items, joins);
+        go(weight_kernel<T, S::BM, S::BN, S::WM, S::WN, S::DIRECT>,
+           dim3((unsigned)(ceil_div(c.n, S::BM) * ceil_div(c.k, S::BN)), (unsigned)(cut.plan == Cut::WHOLE ? c.experts : cut.items),
+                c.matrices),
+           S::M::THREADS, S::M::LDS, s, c.products<T>(), g, cut, items, static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
+           static_cast<T*>(dw0), static_cast<T*>(dw1), partials);
+        if (cut.joins > 0)
+          for (int i = 0; i < c.matrices; ++i)
+            hipLaunchKernelGGL(join_kernel<T>, dim3(256, (unsigned)cut.joins), dim3(256), 0, s, g, cut, c.offsets, joins,
+                               partials + i * cut.partials * (int64_t)c.n * c.k, static_cast<T*>(i ? dw1 : dw0));
+      });
+  });
+}
+
+// The checks that both backward passes share; the workspace they need.
+netsim_status check_back(const char* what, const Call& c, const void* dy, int64_t ld_dy, const int32_t* slots_of_row, int32_t each,
+                         const void* dx, const void* dw0, const void* dw1, const void* work, int64_t work_bytes, const Space& space) {
+  if (netsim_status bad = check(what, c)) return bad;
+  if (ld_dy < c.n) return fail(NETSIM_E_INVALID, what, "the gradient's row pitch is below n");
+  if (c.slots > 0 && !dy) return fail(NETSIM_E_INVALID, what, "NULL array");
+  if (!dw0 != !dw1) return fail(NETSIM_E_INVALID, what, "both matrices' gradients or neither");
+  if (dx && c.map && (each < 1 || (c.rows > 0 && !slots_of_row)))
+    return fail(NETSIM_E_INVALID, what, "the gradient of rows in a list needs the slots of every row");
+  if (!aligned(dy, 2) || !aligned(dx, 2) || !aligned(dw0, 2) || !aligned(dw1, 2) || !aligned(slots_of_row, 4) || !aligned(work, 16))
+    return fail(NETSIM_E_INVALID, what, "an array is not aligned to its type, or d_work to 16 bytes");
+  if (work_bytes < space.bytes || (space.bytes > 0 && !work)) return fail(NETSIM_E_INVALID, what, "the workspace is too small");
+  return NETSIM_OK;
+}
+
+}  // namespace
+}  // namespace netsim_ops
+
+using namespace netsim_ops;
+
+extern "C" netsim_status netsim_experts_product(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                                int32_t type, int64_t rows, const void* d_x, int64_t ld_x,
+                                                const int32_t* d_row_of_slot, const int32_t* d_offsets, const void* d_w,
+                                                void* d_y, int64_t ld_y, void* hip_stream) {
+  const char* what = "experts_product";
+  return entry(what, device, [&] {
+    const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w, d_w}, 1};
+    if (netsim_status bad = check(what, c)) return bad;
+    if (ld_y < n) return fail(NETSIM_E_INVALID, what, "ld_y is below n");
+    if (slots == 0) return (netsim_status)NETSIM_OK;
+    if (!d_y) return fail(NETSIM_E_INVALID, what, "NULL array");
+    if (!aligned(d_y, 2)) return fail(NETSIM_E_INVALID, what, "d_y is not aligned to its type");
+    return launch(what, device, [&] { enqueue_rows<PRODUCT>(c, 0, nullptr, 0, d_y, nullptr, ld_y, static_cast<hipStream_t>(hip_stream)); });
+  });
+}
+
+extern "C" netsim_status netsim_experts_gated(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                              int32_t type, int32_t activation, int64_t rows, const void* d_x, int64_t ld_x,
+                                              const int32_t* d_row_of_slot, const int32_t* d_offsets, const void* d_w_gate,
+                                              const void* d_w_up, void* d_h, int64_t ld_h, void* hip_stream) {
+  const char* what = "experts_gated";
+  return entry(what, device, [&] {
+    const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w_gate, d_w_up}, 2};
+    if (netsim_status bad = check(what, c)) return bad;
+    if (activation != NETSIM_SILU && activation != NETSIM_GELU) return fail(NETSIM_E_INVALID, what, "bad activation");
+    if (ld_h < n) return fail(NETSIM_E_INVALID, what, "ld_h is below n");
+    if (slots == 0) return (netsim_status)NETSIM_OK;
+    if (!d_h) return fail(NETSIM_E_INVALID, what, "NULL array");
+    if (!aligned(d_h, 2)) return fail(NETSIM_E_INVALID, what, "d_h is not aligned to its type");
+    return launch(what, device, [&] { enqueue_rows<GATED>(c, activation, nullptr, 0, d_h, nullptr, ld_h, static_cast<hipStream_t>(hip_stream)); });
+  });
+}
+
+extern "C" int64_t netsim_experts_backward_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                                      int32_t matrices, int32_t has_offsets, int32_t has_rows) {
+  if (!sizes_ok(experts, slots, n, cols) || matrices < 1 || matrices > 2) return -1;
+  return space_of(make_cut(experts, slots, n, cols, has_offsets), matrices, slots, n, cols, has_rows).bytes;
+}
+
+extern "C" netsim_status netsim_experts_product_backward(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                                         int32_t type, int64_t rows, const void* d_x, int64_t ld_x,
+                                                         const int32_t* d_row_of_slot, const int32_t* d_offsets,
+                                                         const void* d_w, const void* d_dy, int64_t ld_dy,
+                                                         const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx,
+                                                         void* d_dw, void* d_work, int64_t work_bytes, void* hip_stream) {
+  const char* what = "experts_product_backward";
+  return entry(what, device, [&] {
+    const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w, d_w}, 1};
+    if (!sizes_ok(experts, slots, n, cols)) return fail(NETSIM_E_INVALID, what, kSizes);
+    const Cut cut = make_cut(experts, slots, n, cols, d_offsets);
+    const Space space = space_of(cut, 1, slots, n, cols, d_row_of_slot);
+    if (netsim_status bad = check_back(what, c, d_dy, ld_dy, d_slots_of_row, slots_each, d_dx, d_dw, d_dw, d_work, work_bytes, space))
+      return bad;
+    return launch(what, device, [&] {
+      enqueue_grads(c, cut, space, static_cast<char*>(d_work), d_dy, d_dy, ld_dy, d_slots_of_row, slots_each, d_dx, d_dw, nullptr,
+                    static_cast<hipStream_t>(hip_stream));
+    });
+  });
+}
+
+extern "C" netsim_status netsim_experts_gated_backward(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
+                                                       int32_t type, int32_t activation, int64_t rows, const void* d_x,
+                                                       int64_t ld_x, const int32_t* d_row_of_slot, const int32_t* d_offsets,
+                                                       const void* d_w_gate, const void* d_w_up, const void* d_dh, int64_t ld_dh,
+                                                       const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx,
+                                                       void* d_dw_gate, void* d_dw_up, void* d_work, int64_t work_bytes,
+                                                       void* hip_stream) {
+  const char* what = "experts_gated_backward";
+  return entry(what, device, [&] {
+    const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w_gate, d_w_up}, 2};
+    if (!sizes_ok(experts, slots, n, cols)) return fail(NETSIM_E_INVALID, what, kSizes);
+    if (activation != NETSIM_SILU && activation != NETSIM_GELU) return fail(NETSIM_E_INVALID, what, "bad activation");
+    const Cut cut = make_cut(experts, slots, n, cols, d_offsets);
+    const Space space = space_of(cut, 2, slots, n, cols, d_row_of_slot);
+    if (netsim_status bad =
+            check_back(what, c, d_dh, ld_dh, d_slots_of_row, slots_each, d_dx, d_dw_gate, d_dw_up, d_work, work_bytes, space))
+      return bad;
+    return launch(what, device, [&] {
+      hipStream_t s = static_cast<hipStream_t>(hip_stream);
+      char* work = static_cast<char*>(d_work);
+      if (slots > 0) enqueue_rows<GATED_BACK>(c, activation, d_dh, ld_dh, work + space.d[0], work + space.d[1], space.ld_d, s);
+      enqueue_grads(c, cut, space, work, work + space.d[0], work + space.d[1], space.ld_d, d_slots_of_row, slots_each, d_dx, d_dw_gate,
+                    d_dw_up, s);
+    });
+  });
+}

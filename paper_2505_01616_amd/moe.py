@@ -1,6 +1,7 @@
 """Operators of an expert-parallel layer on torch tensors (the
-``netsim_route``, ``netsim_dispatch`` and ``netsim_act_*`` calls of
-include/netsim.h, which holds their definitions).
+``netsim_route``, ``netsim_dispatch``, ``netsim_act_*``, ``netsim_experts_*``,
+``netsim_rows_quantise`` and ``netsim_adamw`` calls of include/netsim.h, which
+holds their definitions).
 
 What they compute is what a simulation of such a layer is given: the experts
 that the tokens choose, the bytes every rank then sends to every other one
@@ -14,15 +15,18 @@ any torch operation.  Rows may be parts of wider tensors; the last dimension
 is contiguous.  Failures raise ``NetsimError``, wrong tensors ``ValueError``.
 
 The weights of ``route`` carry their gradient to the logits (once; the bias
-has none).  The results of the other calls carry none: they are whole numbers,
+has none), the results of ``gated`` and ``product`` theirs to rows and weights
+(once).  The results of the other calls carry none: they are whole numbers,
 made from whole numbers, or gradients themselves.
 """
 
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import NamedTuple, Optional
+from operator import attrgetter
+from typing import NamedTuple, Optional, Sequence
 
+import numpy as np
 import torch
 
 from . import netsim as ns
@@ -241,3 +245,304 @@ def weight_grad(saved: Saved, dy: torch.Tensor, offsets: torch.Tensor, row_of_sl
                               offsets.data_ptr(), _TYPES[out_dtype], out.data_ptr(),
                               None if space is None else space.data_ptr(), work, stream)
     return out
+
+
+# ------------------------------------------------------- products of experts
+_HALVES = (torch.bfloat16, torch.float16)
+_ACTIVATIONS = {"silu": ns.SILU, "gelu": ns.GELU}
+
+
+def _list(name: str, t: Optional[torch.Tensor], device, dims: int = 1):
+    """Checks a list of whole numbers (or None); its address, which for a list
+    of none is never followed but must not be NULL."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.dim() != dims or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: a contiguous int32 tensor of {dims} dimension(s) on {device} is wanted")
+    return t.data_ptr() or 16
+
+
+class _Products:
+    """The arguments that the products and their backward passes share."""
+
+    def __init__(self, x, weights, offsets, row_of_slot, slots_of_row):
+        self.ld = _rows("x", x, _HALVES)
+        device, w = x.device, weights[0]
+        if w.dim() != 3:
+            raise ValueError("weights: [experts, n, cols] is wanted ([n, cols] for one expert)")
+        self.rows, self.cols = x.shape
+        self.experts, self.n, _ = w.shape
+        for t in weights:
+            _flat("weights", t, x.dtype, (self.experts, self.n, self.cols), device)
+        if offsets is not None and offsets.numel() != self.experts + 1:
+            raise ValueError("offsets: one more than experts are wanted")
+        if offsets is None and self.experts != 1:
+            raise ValueError("offsets: several experts need them")
+        self.offsets, self.map = _list("offsets", offsets, device), _list("row_of_slot", row_of_slot, device)
+        self.slots = self.rows if row_of_slot is None else row_of_slot.numel()
+        self.list, self.each = _list("slots_of_row", slots_of_row, device, 2), 0
+        if slots_of_row is not None:
+            if slots_of_row.shape[0] != self.rows:
+                raise ValueError("slots_of_row: [rows of x, slots of each] is wanted")
+            self.each = slots_of_row.shape[1]
+        self.index, self.stream = _at(device)
+        self.type = _TYPES[x.dtype]
+
+    def result(self, x):
+        return torch.empty((self.slots, self.n), dtype=x.dtype, device=x.device)
+
+    def workspace(self, matrices: int, device):
+        size = max(0, ns.netsim_experts_backward_work_bytes(self.experts, self.slots, self.n, self.cols, matrices,
+                                                            self.offsets is not None, self.map is not None))
+        return torch.empty(size, dtype=torch.uint8, device=device) if size else None, size
+
+
+def _matrices(weights):
+    """Weights as [experts, n, cols]."""
+    return [w.unsqueeze(0) if w.dim() == 2 else w for w in weights]
+
+
+def _products(x, weights, offsets, row_of_slot, slots_of_row, activation):
+    p = _Products(x, weights, offsets, row_of_slot, slots_of_row)
+    y = p.result(x)
+    head, tail = (p.index, p.experts, p.slots, p.n, p.cols, p.type), (p.rows, x.data_ptr(), p.ld, p.map, p.offsets)
+    if activation is None:
+        ns.netsim_experts_product(*head, *tail, weights[0].data_ptr(), y.data_ptr(), p.n, p.stream)
+    else:
+        ns.netsim_experts_gated(*head, activation, *tail, weights[0].data_ptr(), weights[1].data_ptr(), y.data_ptr(), p.n,
+                                p.stream)
+    return y
+
+
+class _Multiplied(torch.autograd.Function):
+    """gated (activation: its number) or product (None) as a function of x
+    and the weights."""
+
+    @staticmethod
+    def forward(ctx, x, offsets, row_of_slot, slots_of_row, activation, *weights):
+        if ctx.needs_input_grad[0] and row_of_slot is not None and slots_of_row is None:
+            raise ValueError("slots_of_row: the gradient of rows in a list needs the slots of every row")
+        ctx.activation = activation
+        ctx.save_for_backward(x, offsets, row_of_slot, slots_of_row, *weights)
+        return _products(x, weights, offsets, row_of_slot, slots_of_row, activation)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, offsets, row_of_slot, slots_of_row, *weights = ctx.saved_tensors
+        if dy.stride(1) != 1 or dy.shape[0] > 1 and dy.stride(0) < dy.shape[1]:
+            dy = dy.contiguous()
+        p = _Products(x, weights, offsets, row_of_slot, slots_of_row)
+        dx = torch.empty((p.rows, p.cols), dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
+        wanted = any(ctx.needs_input_grad[5:])
+        dw = [torch.empty_like(w) if wanted else None for w in weights]
+        space, size = p.workspace(len(weights), x.device)
+        address = [None if t is None else t.data_ptr() for t in (dx, *dw, space)]
+        head, tail = (p.index, p.experts, p.slots, p.n, p.cols, p.type), (p.rows, x.data_ptr(), p.ld, p.map, p.offsets)
+        tail += (*(w.data_ptr() for w in weights), dy.data_ptr(), dy.stride(0) if dy.shape[0] > 1 else p.n, p.list, p.each,
+                 *address, size, p.stream)
+        if ctx.activation is None:
+            ns.netsim_experts_product_backward(*head, *tail)
+        else:
+            ns.netsim_experts_gated_backward(*head, ctx.activation, *tail)
+        return dx, None, None, None, None, *dw
+
+
+def _multiply(x, weights, offsets, row_of_slot, slots_of_row, activation):
+    weights = _matrices(weights)
+    if torch.is_grad_enabled() and (x.requires_grad or any(w.requires_grad for w in weights)):
+        return _Multiplied.apply(x, offsets, row_of_slot, slots_of_row, activation, *weights)
+    return _products(x, weights, offsets, row_of_slot, slots_of_row, activation)
+
+
+def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+          row_of_slot: Optional[torch.Tensor] = None, slots_of_row: Optional[torch.Tensor] = None,
+          activation: str = "silu") -> torch.Tensor:
+    """act(x w_gate^T) * (x w_up^T) by slot, [slots, n], in one kernel.
+    activation: 'silu' or 'gelu'.
+
+    x [rows, cols] and the weights [experts, n, cols] of one type, bfloat16 or
+    float16; an expert has the slots that `offsets` gives it (None: one expert
+    has all; its weights may be [n, cols]), a slot the row row_of_slot[slot]
+    (None: the row of its number).  slots_of_row [rows, slots of each], the
+    other way round (-1 for none), is what the gradient of rows in such a list
+    needs.  With a Dispatch: plan.offsets, plan.token_of_slot and
+    plan.slot_of_choice.  Slots of no expert or without a row are zeros, and
+    left out of the gradients."""
+    if activation not in _ACTIVATIONS:
+        raise ValueError("activation: 'silu' or 'gelu'")
+    return _multiply(x, (w_gate, w_up), offsets, row_of_slot, slots_of_row, _ACTIVATIONS[activation])
+
+
+def product(x: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+            row_of_slot: Optional[torch.Tensor] = None, slots_of_row: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x w^T by slot, [slots, n]; arguments as gated's."""
+    return _multiply(x, (w,), offsets, row_of_slot, slots_of_row, None)
+
+
+# --------------------------------------------------------- products in 8 bits
+class Rows8(NamedTuple):
+    """Rows in whole numbers of 8 bits with a scale for each: row ~ q scale."""
+
+    q: torch.Tensor                 # int8 [..., cols up to a multiple of 16]
+    scales: torch.Tensor            # float32 [...]
+    cols: int
+
+
+def quantise(x: torch.Tensor) -> Rows8:
+    """Rows [rows, cols], or weights [experts, n, cols] (contiguous), in whole
+    numbers of 8 bits."""
+    if x.dim() == 3 and x.is_contiguous():
+        q, scales, cols = quantise(x.view(-1, x.shape[2]))
+        return Rows8(q.view(*x.shape[:2], -1), scales.view(x.shape[:2]), cols)
+    ld = _rows("x", x, _TYPES)
+    rows, cols = x.shape
+    index, stream = _at(x.device)
+    q = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=x.device)
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    ns.netsim_rows_quantise(index, rows, cols, _TYPES[x.dtype], x.data_ptr(), ld, q.data_ptr(), scales.data_ptr(), stream)
+    return Rows8(q, scales, cols)
+
+
+def product8(x: Rows8, w: Rows8, offsets: Optional[torch.Tensor] = None, row_of_slot: Optional[torch.Tensor] = None,
+             out_dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """x w^T by slot, [slots, n], from rows and weights in 8 bits: sums of
+    whole numbers times the row's scale and the channel's.  Slots as in
+    gated."""
+    if x.q.dim() != 2 or w.q.dim() not in (2, 3) or not x.q.is_cuda or x.cols != w.cols or out_dtype not in _TYPES:
+        raise ValueError("quantised rows, weights [experts, n, cols] of as many columns on a GPU, and a float32, bfloat16 or "
+                         "float16 result are wanted")
+    wq, w_scales = (w.q, w.scales) if w.q.dim() == 3 else (w.q.unsqueeze(0), w.scales.unsqueeze(0))
+    device, rows, (experts, n, _) = x.q.device, x.q.shape[0], wq.shape
+    pitch = -(-x.cols // 16) * 16
+    _flat("x.q", x.q, torch.int8, (rows, pitch), device)
+    _flat("x.scales", x.scales, torch.float32, (rows,), device)
+    _flat("w.q", wq, torch.int8, (experts, n, pitch), device)
+    _flat("w.scales", w_scales, torch.float32, (experts, n), device)
+    if offsets is not None and offsets.numel() != experts + 1:
+        raise ValueError("offsets: one more than experts are wanted")
+    at, rows_at = _list("offsets", offsets, device), _list("row_of_slot", row_of_slot, device)
+    slots = rows if row_of_slot is None else row_of_slot.numel()
+    index, stream = _at(device)
+    y = torch.empty((slots, n), dtype=out_dtype, device=device)
+    ns.netsim_experts_product8(index, experts, slots, n, x.cols, rows, x.q.data_ptr(), x.scales.data_ptr(), rows_at, at,
+                               wq.data_ptr(), w_scales.data_ptr(), _TYPES[out_dtype], y.data_ptr(), n, stream)
+    return y
+
+
+# ------------------------------------------------------------------- the step
+SCALED = 256    # elements of a tensor whose 8-bit moments share a scale
+_TENSOR = np.dtype([(n, np.uintp) for n in ("p", "g", "m", "v", "m_scales", "v_scales", "master")]
+                   + [("size", np.int64), ("p_type", np.int32), ("g_type", np.int32)])
+_address, _contiguous, _device = torch.Tensor.data_ptr, torch.Tensor.is_contiguous, torch.Tensor.get_device
+_shape, _dtype = attrgetter("shape"), attrgetter("dtype")
+
+
+class Moments(NamedTuple):
+    """A tensor's first and second moment: float32 [size] both, or in 8 bits
+    float8_e4m3fn [SCALED * blocks] with their scales, the second as its root."""
+
+    m: torch.Tensor
+    v: torch.Tensor
+    m_scales: Optional[torch.Tensor] = None     # float32 [blocks]
+    v_scales: Optional[torch.Tensor] = None
+
+
+class AdamW:
+    """AdamW over a list of tensors, one call a step (netsim_adamw).
+
+    params: contiguous tensors of float32, bfloat16 or float16 on one GPU,
+    updated in place.  bits: of the moments, 32 or 8.  masters: True, or the
+    copies in 32 bits that parameters of 16 then have (what is updated; the
+    parameter is its rounding).  moments, steps: where to go on from; zeros and
+    0 otherwise.  counted: the steps' number is kept on the GPU (`counter`), so
+    that a captured step counts on with every replay; lr and grad_scale are
+    then those of the capture."""
+
+    def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: float = 0.01, bits: int = 32, masters=False, moments: Optional[Sequence[Moments]] = None,
+                 steps: int = 0, counted: bool = False):
+        self.params = list(params)
+        self.lr, self.betas, self.eps, self.weight_decay = float(lr), (float(betas[0]), float(betas[1])), float(eps), float(weight_decay)
+        self.bits, self.steps = int(bits), int(steps)
+        if self.bits not in (8, 32) or self.steps < 0:
+            raise ValueError("bits: 8 or 32; steps: not below 0")
+        for p in self.params:
+            if not p.is_cuda or p.dtype not in _TYPES or not p.is_contiguous() or p.device != self.params[0].device:
+                raise ValueError("params: contiguous float32, bfloat16 or float16 tensors on one GPU are wanted")
+        device = self.params[0].device if self.params else None
+        if masters is True:
+            masters = [None if p.dtype == torch.float32 else p.detach().float() for p in self.params]
+        self.masters = list(masters) if masters else [None] * len(self.params)
+        self.moments = list(moments) if moments is not None else [self._zeros(p) for p in self.params]
+        if len(self.masters) != len(self.params) or len(self.moments) != len(self.params):
+            raise ValueError("masters, moments: one for every parameter are wanted")
+        self._entries = np.zeros(len(self.params), dtype=_TENSOR)
+        for p, copy, state, e in zip(self.params, self.masters, self.moments, self._entries):
+            n, blocks = p.numel(), -(-p.numel() // SCALED)
+            if copy is not None:
+                if p.dtype == torch.float32 or copy.numel() != n:
+                    raise ValueError("masters: of as many elements as their parameters, which have 16 bits")
+                _flat("masters", copy, torch.float32, copy.shape, device)
+                e["master"] = copy.data_ptr()
+            for name, t in zip(("m", "v"), state[:2]):
+                if self.bits == 32:
+                    if t.numel() != n:
+                        raise ValueError("moments: as many elements as their parameters are wanted")
+                    _flat("moments", t, torch.float32, t.shape, device)
+                else:
+                    _flat("moments", t, torch.float8_e4m3fn, (blocks * SCALED,), device)
+                e[name] = t.data_ptr()
+            if self.bits == 8:
+                for name, t in zip(("m_scales", "v_scales"), state[2:]):
+                    if t is None:
+                        raise ValueError("moments: those in 8 bits have scales")
+                    _flat(name, t, torch.float32, (blocks,), device)
+                    e[name] = t.data_ptr()
+            e["size"], e["p_type"] = n, _TYPES[p.dtype]
+        self._shapes, self._types = list(map(_shape, self.params)), list(map(_dtype, self.params))
+        self._devices = list(map(_device, self.params))
+        self.counter = None
+        if counted and self.params:
+            self.counter = torch.tensor([self.steps, 0], dtype=torch.int64, device=device)
+
+    def _zeros(self, p):
+        if self.bits == 32:
+            return Moments(*(torch.zeros(p.numel(), dtype=torch.float32, device=p.device) for _ in range(2)))
+        blocks = -(-p.numel() // SCALED)
+        return Moments(*(torch.zeros(blocks * SCALED, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
+                         for _ in range(2)),
+                       *(torch.zeros(blocks, dtype=torch.float32, device=p.device) for _ in range(2)))
+
+    def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, lr: Optional[float] = None,
+             grad_scale: float = 1.0) -> None:
+        """One step with `grads` (None: the parameters' .grad), times
+        grad_scale.  A parameter whose gradient is None stays as it is."""
+        params, entries = self.params, self._entries
+        shapes, devices, types = self._shapes, self._devices, self._types
+        if grads is None:
+            grads = [p.grad for p in params]
+        if len(grads) != len(params):
+            raise ValueError("grads: one for every parameter is wanted")
+        if any(g is None for g in grads):
+            at = [i for i, g in enumerate(grads) if g is not None]
+            entries, params, grads = entries[at], [params[i] for i in at], [grads[i] for i in at]
+            shapes, devices, types = ([v[i] for i in at] for v in (shapes, devices, types))
+        kinds = list(map(_dtype, grads))
+        if (list(map(_shape, grads)) != shapes or list(map(_device, grads)) != devices or not all(map(_contiguous, grads))
+                or not all(k in _TYPES for k in set(kinds))):
+            raise ValueError("grads: contiguous float32, bfloat16 or float16 tensors of the parameters' shapes, on their GPU, "
+                             "are wanted")
+        if (list(map(_shape, params)) != shapes or list(map(_device, params)) != devices or list(map(_dtype, params)) != types
+                or not all(map(_contiguous, params))):
+            raise ValueError("params: shapes, types and GPU must stay as they were, and tensors contiguous")
+        if params:
+            entries["p"] = list(map(_address, params))
+            entries["g"] = list(map(_address, grads))
+            entries["g_type"] = [_TYPES[k] for k in kinds]
+            index, stream = _at(params[0].device)
+            ns.netsim_adamw(index, len(params), entries.ctypes.data, self.bits, self.steps + 1,
+                            None if self.counter is None else self.counter.data_ptr(), self.lr if lr is None else float(lr),
+                            *self.betas, self.eps, self.weight_decay, float(grad_scale), stream)
+            torch.autograd.graph.increment_version(params)
+        self.steps += 1

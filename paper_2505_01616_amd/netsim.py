@@ -30,6 +30,7 @@ EXEC_AUTO, EXEC_GRID, EXEC_BLOCK, EXEC_CLUSTER, EXEC_EXACT = 0, 1, 2, 3, 4
 
 F32, BF16, F16 = 0, 1, 2
 SCORES_SOFTMAX, SCORES_SIGMOID = 0, 1
+SILU, GELU = 0, 1
 
 STATUS_NAMES = {OK: "NETSIM_OK", E_INVALID: "NETSIM_E_INVALID", E_NOMEM: "NETSIM_E_NOMEM",
                 E_DEVICE: "NETSIM_E_DEVICE", E_STATE: "NETSIM_E_STATE", E_LIMIT: "NETSIM_E_LIMIT"}
@@ -82,6 +83,12 @@ class netsim_router(ctypes.Structure):
                 ("renormalise", ctypes.c_int32), ("groups", ctypes.c_int32),
                 ("groups_kept", ctypes.c_int32), ("group_best", ctypes.c_int32),
                 ("scale", ctypes.c_float)]
+
+
+class netsim_adamw_tensor(ctypes.Structure):
+    _fields_ = [("d_p", ctypes.c_void_p), ("d_g", ctypes.c_void_p), ("d_m", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("d_m_scales", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p), ("d_master", ctypes.c_void_p),
+                ("size", ctypes.c_int64), ("p_type", ctypes.c_int32), ("g_type", ctypes.c_int32)]
 
 
 class NetsimError(RuntimeError):
@@ -146,6 +153,16 @@ _SIGS = {
     "netsim_act_weight_grad_work_bytes": (_I64, [_I32, _I64, _I32, _I32, _I32]),
     "netsim_act_weight_grad": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _P, _I64, _I64, _P, _P, _P, _P,
                                       _I32, _P, _P, _I64, _P]),
+    "netsim_experts_product": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P]),
+    "netsim_experts_gated": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64, _P]),
+    "netsim_experts_backward_work_bytes": (_I64, [_I32, _I64, _I32, _I32, _I32, _I32, _I32]),
+    "netsim_experts_product_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P,
+                                               _I32, _P, _P, _P, _I64, _P]),
+    "netsim_experts_gated_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64,
+                                             _P, _I32, _P, _P, _P, _P, _I64, _P]),
+    "netsim_rows_quantise": (_I32, [_I32, _I64, _I32, _I32, _P, _I64, _P, _P, _P]),
+    "netsim_experts_product8": (_I32, [_I32, _I32, _I64, _I32, _I32, _I64, _P, _P, _P, _P, _P, _P, _I32, _P, _I64, _P]),
+    "netsim_adamw": (_I32, [_I32, _I32, _P, _I32, _I64, _P, _D, _D, _D, _D, _D, _D, _P]),
     "netsim_last_error": (ctypes.c_char_p, [_H]),
     "netsim_destroy": (None, [_H]),
 }
@@ -530,6 +547,56 @@ def netsim_act_weight_grad(device, experts, slots, n, cols, type, d_dy, ld_dy, r
     _check(None, load_library().netsim_act_weight_grad(device, experts, slots, n, cols, type, d_dy, ld_dy, rows, d_q,
                                                        d_exponents, d_row_of_slot, d_offsets, out_type, d_dw, d_work,
                                                        work_bytes, _stream(stream)))
+
+
+def netsim_experts_product(device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, d_w, d_y, ld_y,
+                           stream=None):
+    _check(None, load_library().netsim_experts_product(device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot,
+                                                       d_offsets, d_w, d_y, ld_y, _stream(stream)))
+
+
+def netsim_experts_gated(device, experts, slots, n, cols, type, activation, rows, d_x, ld_x, d_row_of_slot, d_offsets,
+                         d_w_gate, d_w_up, d_h, ld_h, stream=None):
+    _check(None, load_library().netsim_experts_gated(device, experts, slots, n, cols, type, activation, rows, d_x, ld_x,
+                                                     d_row_of_slot, d_offsets, d_w_gate, d_w_up, d_h, ld_h,
+                                                     _stream(stream)))
+
+
+def netsim_experts_backward_work_bytes(experts, slots, n, cols, matrices, has_offsets, has_rows) -> int:
+    return load_library().netsim_experts_backward_work_bytes(experts, slots, n, cols, matrices, has_offsets, has_rows)
+
+
+def netsim_experts_product_backward(device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, d_w,
+                                    d_dy, ld_dy, d_slots_of_row, slots_each, d_dx, d_dw, d_work, work_bytes, stream=None):
+    _check(None, load_library().netsim_experts_product_backward(device, experts, slots, n, cols, type, rows, d_x, ld_x,
+                                                                d_row_of_slot, d_offsets, d_w, d_dy, ld_dy, d_slots_of_row,
+                                                                slots_each, d_dx, d_dw, d_work, work_bytes,
+                                                                _stream(stream)))
+
+
+def netsim_experts_gated_backward(device, experts, slots, n, cols, type, activation, rows, d_x, ld_x, d_row_of_slot,
+                                  d_offsets, d_w_gate, d_w_up, d_dh, ld_dh, d_slots_of_row, slots_each, d_dx, d_dw_gate,
+                                  d_dw_up, d_work, work_bytes, stream=None):
+    _check(None, load_library().netsim_experts_gated_backward(device, experts, slots, n, cols, type, activation, rows, d_x,
+                                                              ld_x, d_row_of_slot, d_offsets, d_w_gate, d_w_up, d_dh, ld_dh,
+                                                              d_slots_of_row, slots_each, d_dx, d_dw_gate, d_dw_up, d_work,
+                                                              work_bytes, _stream(stream)))
+
+
+def netsim_rows_quantise(device, rows, cols, type, d_x, ld_x, d_q, d_scales, stream=None):
+    _check(None, load_library().netsim_rows_quantise(device, rows, cols, type, d_x, ld_x, d_q, d_scales, _stream(stream)))
+
+
+def netsim_experts_product8(device, experts, slots, n, cols, rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales,
+                            out_type, d_y, ld_y, stream=None):
+    _check(None, load_library().netsim_experts_product8(device, experts, slots, n, cols, rows, d_q, d_scales, d_row_of_slot,
+                                                        d_offsets, d_wq, d_w_scales, out_type, d_y, ld_y, _stream(stream)))
+
+
+def netsim_adamw(device, tensors, list, bits, step, d_counter, lr, beta1, beta2, eps, weight_decay, grad_scale, stream=None):
+    """list: address of an array of netsim_adamw_tensor on the host."""
+    _check(None, load_library().netsim_adamw(device, tensors, list, bits, step, d_counter, lr, beta1, beta2, eps,
+                                             weight_decay, grad_scale, _stream(stream)))
 
 
 def netsim_last_error(h=None) -> str:
