@@ -7,6 +7,7 @@
 //   y_s[n] = (sum over c of q_x[c] q_w[n][c]) s_x s_w[n].
 #include <math.h>
 
+#include "few.h"
 #include "parts.h"
 #include "tile.h"
 
@@ -78,7 +79,7 @@ struct Eights {
   const int32_t *map, *offsets;
   const int8_t* w;
   const float* w_scales;
-  int64_t tiles;
+  int64_t tiles, first;   // all tiles, and where a launch begins
   int tiles_n;
 };
 
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(64 * WM * WN) void eight_kernel(Eights p, O* __rest
   using A = RowTile<int8_t, BM, M::THREADS, true>;
   using B = RowTile<int8_t, BN, M::THREADS, true>;
   extern __shared__ __align__(16) char shared[];
-  const int64_t tile = tile_of_group(blockIdx.x);
+  const int64_t tile = p.first + tile_of_group(blockIdx.x);
   if (tile >= p.tiles) return;
   const int n0 = (int)(tile % p.tiles_n) * BN;
   const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
@@ -137,6 +138,38 @@ __global__ __launch_bounds__(64 * WM * WN) void eight_kernel(Eights p, O* __rest
                                [&](int i, int j, int r) { return held[i] ? (float)m.sum[i][j][r] * x_scale[i] * w_scale[j][r] : 0.0f; });
 }
 
+// For few rows of each expert.
+template <class O>
+__global__ __launch_bounds__(kFewThreads) void few_eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
+  constexpr int COLS = 2 * kFewCols;
+  extern __shared__ __align__(16) char shared[];
+  auto* sums = reinterpret_cast<i32x4*>(shared);
+  const int64_t tile = p.first + blockIdx.x;
+  if (tile >= p.tiles) return;
+  const int n0 = (int)(tile % p.tiles_n) * COLS;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, kFewRows, (int)(tile / p.tiles_n));
+  if (rows.expert < -1) return;
+  const int count = rows.to - rows.from, lane = threadIdx.x & 63;
+  const int64_t first = (int64_t)max(rows.expert, 0) * p.n;
+  with_few(count, [&](auto tiles) {
+    constexpr int MT = decltype(tiles)::value;
+    const bool any = rows.expert >= 0 && p.rows > 0;
+    if (any)
+      few_sums<int8_t, MT, true>(sums, [&](int m) {
+        const int64_t at = row_of(p, rows.from + min(m, count - 1));
+        return p.x + (at < 0 ? 0 : at) * p.pitch;
+      }, p.w + (first + min(n0 + (lane & 15), p.n - 1)) * p.pitch, p.w + (first + min(n0 + 16 + (lane & 15), p.n - 1)) * p.pitch, p.pitch);
+    __syncthreads();
+    for (int t = threadIdx.x; t < MT * 16 * COLS; t += kFewThreads) {
+      const int m = t / COLS, n = t % COLS;
+      if (m >= count || n0 + n >= p.n) continue;
+      const int64_t at = any ? row_of(p, rows.from + m) : -1;
+      const float v = at >= 0 ? (float)few_sum<int8_t, MT>(sums, n / 16, m, n % 16) * p.x_scales[at] * p.w_scales[first + n0 + n] : 0.0f;
+      out[(int64_t)(rows.from + m) * ld_out + n0 + n] = (O)v;
+    }
+  });
+}
+
 }  // namespace
 }  // namespace netsim_ops
 
@@ -158,7 +191,7 @@ extern "C" netsim_status netsim_rows_quantise(int32_t device, int64_t rows, int3
     return launch(what, device, [&] {
       with_type(type, [&](auto t) {
         using T = decltype(t);
-        in_launches(rows, 1 << 22, [&](int64_t first, int64_t n) {
+        in_launches(rows, kMaxGroups, [&](int64_t first, int64_t n) {
           hipLaunchKernelGGL(quantise_kernel<T>, dim3((unsigned)n), dim3(256), 0, static_cast<hipStream_t>(hip_stream), cols, pitch,
                              static_cast<const T*>(d_x) + first * ld_x, ld_x, d_q + first * pitch, d_scales + first);
         });
@@ -190,14 +223,18 @@ extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts
       with_type(out_type, [&](auto o) {
         using O = decltype(o);
         auto run = [&](auto kernel, int bm, int bn, int threads, int lds) {
-          Eights p{experts, (int)slots, n, (int)padded(cols), rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales, 0, 0};
+          Eights p{experts, (int)slots, n, (int)padded(cols), rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales, 0, 0, 0};
           p.tiles_n = (int)ceil_div(n, bn);
           p.tiles = p.tiles_n * most_rows_tiles(experts, slots, bm, d_offsets);
           (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-          hipLaunchKernelGGL(kernel, dim3((unsigned)groups_of_tiles(p.tiles)), dim3(threads), lds, static_cast<hipStream_t>(hip_stream),
-                             p, static_cast<O*>(d_y), ld_y);
+          over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
+            p.first = first;
+            hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), lds, static_cast<hipStream_t>(hip_stream), p, static_cast<O*>(d_y), ld_y);
+          });
         };
-        if (slots / experts >= 256)
+        if (slots <= 24 * (int64_t)experts)
+          run(few_eight_kernel<O>, kFewRows, 2 * kFewCols, kFewThreads, kFewShared);
+        else if (slots / experts >= 256)
           run(eight_kernel<O, 256, 256, 2, 4>, 256, 256, 512, Tile<int8_t, 256, 256, 2, 4>::LDS);
         else
           run(eight_kernel<O, 128, 128, 2, 2>, 128, 128, 256, Tile<int8_t, 128, 128, 2, 2>::LDS);

@@ -11,6 +11,7 @@
 // the summed one, and what becomes of the sums.
 #include <math.h>
 
+#include "few.h"
 #include "parts.h"
 #include "tile.h"
 
@@ -27,7 +28,7 @@ struct Products {
   const int32_t* map;       // slots' rows; NULL: a slot's row has its number
   const int32_t* offsets;   // NULL: one expert has all slots
   const T* w[2];
-  int64_t tiles;            // of a launch
+  int64_t tiles, first;     // all tiles, and where a launch begins
   int tiles_n;
 };
 
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(64 * WM * WN) void rows_kernel(Products<T> p, int a
   using B = RowTile<T, BN, M::THREADS, DIRECT>;
   constexpr int COLS = OUT == PRODUCT ? BN : BN / 2, JN = OUT == PRODUCT ? M::FN : M::FN / 2;
   extern __shared__ __align__(16) char shared[];
-  const int64_t tile = tile_of_group(blockIdx.x);
+  const int64_t tile = p.first + tile_of_group(blockIdx.x);
   if (tile >= p.tiles) return;
   const int n0 = (int)(tile % p.tiles_n) * COLS;
   const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
@@ -178,6 +179,49 @@ __global__ __launch_bounds__(64 * WM * WN) void rows_kernel(Products<T> p, int a
   }
 }
 
+// PRODUCT and GATED for few rows of each expert.
+template <class T, int OUT, bool DIRECT>
+__global__ __launch_bounds__(kFewThreads) void few_kernel(Products<T> p, int activation, T* __restrict__ out, int64_t ld_out) {
+  constexpr int COLS = OUT == PRODUCT ? 2 * kFewCols : kFewCols;
+  extern __shared__ __align__(16) char shared[];
+  auto* sums = reinterpret_cast<f32x4*>(shared);
+  const int64_t tile = p.first + blockIdx.x;
+  if (tile >= p.tiles) return;
+  const int n0 = (int)(tile % p.tiles_n) * COLS;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, kFewRows, (int)(tile / p.tiles_n));
+  if (rows.expert < -1) return;
+  const int count = rows.to - rows.from, lane = threadIdx.x & 63;
+  with_few(count, [&](auto tiles) {
+    constexpr int MT = decltype(tiles)::value;
+    const bool any = rows.expert >= 0 && p.rows > 0;
+    if (any) {
+      const int64_t first = (int64_t)rows.expert * p.n;
+      const T* w0 = p.w[0] + (first + min(n0 + (lane & 15), p.n - 1)) * p.k;
+      const T* w1 = OUT == PRODUCT ? p.w[0] + (first + min(n0 + 16 + (lane & 15), p.n - 1)) * p.k
+                                   : p.w[1] + (first + min(n0 + (lane & 15), p.n - 1)) * p.k;
+      few_sums<T, MT, DIRECT>(sums, [&](int m) {
+        const int64_t at = row_of(p, rows.from + min(m, count - 1));
+        return p.x + (at < 0 ? 0 : at) * p.ld;
+      }, w0, w1, p.k);
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < MT * 16 * COLS; t += kFewThreads) {
+      const int m = t / COLS, n = t % COLS;
+      if (m >= count || n0 + n >= p.n) continue;
+      float v = 0.0f;
+      if (any && row_of(p, rows.from + m) >= 0) {
+        if constexpr (OUT == PRODUCT) {
+          v = few_sum<T, MT>(sums, n / 16, m, n % 16);
+        } else {
+          const float g = few_sum<T, MT>(sums, 0, m, n), u = few_sum<T, MT>(sums, 1, m, n);
+          with_activation(activation, [&](auto act) { v = act.at(g).act * u; });
+        }
+      }
+      out[(int64_t)(rows.from + m) * ld_out + n0 + n] = (T)v;
+    }
+  });
+}
+
 // Rows' gradients by slot: the sum over `pairs` of d W, d [slots x ld_d] of n
 // values a row.
 template <class T, class O, int BM, int BN, int WM, int WN, bool DIRECT>
@@ -188,7 +232,7 @@ __global__ __launch_bounds__(64 * WM * WN) void input_kernel(Products<T> p, int 
   using A = RowTile<T, BM, M::THREADS, DIRECT>;
   using B = ColTile<T, BN, M::THREADS, DIRECT>;
   extern __shared__ __align__(16) char shared[];
-  const int64_t tile = tile_of_group(blockIdx.x);
+  const int64_t tile = p.first + tile_of_group(blockIdx.x);
   if (tile >= p.tiles) return;
   const int c0 = (int)(tile % p.tiles_n) * BN;
   const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
@@ -223,25 +267,24 @@ __global__ __launch_bounds__(64 * WM * WN) void input_kernel(Products<T> p, int 
 }
 
 // dx[row] = the sum over the row's slots of their gradients, in the order of
-// the list.
+// the list.  A lane takes eight columns.
 template <class T>
-__global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int cols, int each, int slots,
+__global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int cols, int each, int slots, int units,
                                                      const int32_t* __restrict__ slots_of_row,
                                                      const float* __restrict__ by_slot, T* __restrict__ dx) {
-  const int64_t row = blockIdx.x;
+  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x, row = unit / units;
+  const int c = (int)(unit - row * units) * 8, left = cols - c;
+  if (row >= rows) return;
   const int32_t* list = slots_of_row + row * each;
-  for (int c = threadIdx.x * 4; c < cols; c += 1024) {
-    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int j = 0; j < each; ++j) {
-      const int s = list[j];
-      if (s < 0 || s >= slots) continue;
-      const float* from = by_slot + (int64_t)s * cols + c;
-      for (int h = 0; h < 4; ++h)
-        if (c + h < cols) sum[h] += from[h];
-    }
-    for (int h = 0; h < 4; ++h)
-      if (c + h < cols) dx[row * cols + c + h] = (T)sum[h];
+  float sum[8] = {};
+#pragma unroll 4
+  for (int j = 0; j < each; ++j) {
+    const int s = list[j];
+    const Eight<float> v = load_some(by_slot + (int64_t)max(s, 0) * cols + c, s >= 0 && s < slots ? left : 0);
+#pragma unroll
+    for (int h = 0; h < 8; ++h) sum[h] += value_of(v, h);
   }
+  store_some(dx + row * cols + c, sum, left);
 }
 
 // The weights' gradients: dW[e][n][c] = the sum over e's slots of d[s][n]
@@ -273,13 +316,29 @@ __global__ __launch_bounds__(64 * WM * WN) void weight_kernel(Products<T> p, Sum
   B b;
   a.open(blockIdx.z ? d1 : d0, ld_d, n0, g.n);
   b.open(p.x, p.ld, c0, g.cols);
+  // The slots' rows, read a step ahead: what a and b bring in of a step are the
+  // same slots.  A slot without a row takes no part, whatever its d holds.
+  static_assert(A::N == B::N && A::EACH == B::EACH, "");
+  const int64_t rows = min(p.rows, (int64_t)0x7fffffff);
+  int row[A::N];
+  auto look = [&](int first) {
+#pragma unroll
+    for (int i = 0; i < A::N; ++i) {
+      const int k = first + a.row(i);
+      row[i] = p.map ? p.map[min(k, it.to - 1)] : k;
+    }
+  };
+  if (it.from < it.to) look(it.from);
   m.template run<A, B>(
       shared, (it.to - it.from + A::STEP - 1) / A::STEP,
       [&](Place stage, int s) {
         const int first = it.from + s * A::STEP;
-        // a slot without a row takes no part, whatever its d holds
-        a.load(stage, [&](int i) { const int k = first + a.row(i); return k < it.to && row_of(p, k) >= 0 ? k : -1; });
-        b.load(stage + BM * kStepBytes, [&](int i) -> int64_t { const int k = first + b.row(i); return k < it.to ? row_of(p, k) : -1; });
+        bool held[A::N];
+#pragma unroll
+        for (int i = 0; i < A::N; ++i) held[i] = first + a.row(i) < it.to && row[i] >= 0 && row[i] < rows;
+        a.load(stage, [&](int i) { return held[i] ? first + a.row(i) : -1; });
+        b.load(stage + BM * kStepBytes, [&](int i) { return held[i] ? row[i] : -1; });
+        look(first + A::STEP);
       },
       [&](Place stage) {
         a.store(stage);
@@ -328,8 +387,6 @@ void with_16_bits(int32_t type, F&& f) {
     f(f16{});
 }
 
-constexpr int64_t kMaxGroups = 1 << 22;   // of a launch: 2^31 threads
-
 // What a call was given, checked.
 struct Call {
   int32_t device, experts;
@@ -345,7 +402,7 @@ struct Call {
   template <class T>
   Products<T> products() const {
     return Products<T>{experts, (int)slots, n, k, rows, ld, static_cast<const T*>(x), map, offsets,
-                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0};
+                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0, 0};
   }
   // Whether x's rows, and the weights', are whole chunks of 16 bytes.
   bool x_direct() const { return ld % 8 == 0 && k % 8 == 0 && aligned(x, 16); }
@@ -382,18 +439,39 @@ void go(K kernel, dim3 grid, int threads, int lds, hipStream_t s, Args... args) 
   hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
 }
 
-// Rows by slot (rows_kernel).
+// Whether an expert has few rows: few_kernel reads the weights faster, tiles
+// read the rows less often.
+bool few(int64_t slots, int64_t experts) { return slots <= 24 * experts; }
+
+// Rows by slot (rows_kernel, few_kernel).
 template <int OUT>
 void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, void* out, void* out2, int64_t ld_out, hipStream_t s) {
   with_16_bits(c.type, [&](auto t) {
     using T = decltype(t);
+    if constexpr (OUT != GATED_BACK)
+      if (few(c.slots, c.experts)) {
+        auto p = c.products<T>();
+        p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? 2 * kFewCols : kFewCols);
+        p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, kFewRows, c.offsets);
+        with_bool(c.x_direct() && c.w_direct(), [&](auto direct) {
+          over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
+            p.first = first;
+            go(few_kernel<T, OUT, decltype(direct)::value>, dim3(groups), kFewThreads, kFewShared, s, p, activation,
+               static_cast<T*>(out), ld_out);
+          });
+        });
+        return;
+      }
     with_tile<T>(tile_of(c.slots, c.experts, c.n, c.k), c.x_direct() && c.w_direct(), [&](auto shape) {
       using S = decltype(shape);
       auto p = c.products<T>();
       p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? S::BN : S::BN / 2);
       p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::BM, c.offsets);
-      go(rows_kernel<T, OUT, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3((unsigned)groups_of_tiles(p.tiles)), S::M::THREADS,
-         S::M::LDS, s, p, activation, static_cast<const T*>(dy), ld_dy, static_cast<T*>(out), static_cast<T*>(out2), ld_out);
+      over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
+        p.first = first;
+        go(rows_kernel<T, OUT, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, activation,
+           static_cast<const T*>(dy), ld_dy, static_cast<T*>(out), static_cast<T*>(out2), ld_out);
+      });
     });
   });
 }
@@ -410,12 +488,21 @@ struct Space {
   }
 };
 
-// How the weights' sums are cut (parts.h).
-Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t k, bool offsets) {
+// How the weights' sums are cut (parts.h): into parts as long as each of the
+// 256 compute units would have slots of one tile if all were busy to the end.
+Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t k, int matrices) {
   Cut c{};
   c.tile = tile_of(slots, experts, n, k);
   c.step = 64;
-  c.plan = Cut::WHOLE;
+  const int64_t tiles = matrices * ceil_div(n, c.tile) * ceil_div(k, c.tile);
+  c.longest = ceil_div(slots * tiles, 256);
+  if (c.longest < 256) c.longest = 256;
+  if (c.longest > kMaxSlots) c.longest = kMaxSlots;
+  c.plan = slots <= 512 ? Cut::WHOLE : experts * tiles <= 64 && experts <= 16 ? Cut::BY_WAVE : Cut::LISTED;
+  if (c.plan == Cut::WHOLE) return c;
+  c.items = experts + slots / c.longest;
+  c.joins = slots / c.longest < experts ? slots / c.longest : experts;
+  c.partials = 2 * (slots / c.longest);
   return c;
 }
 
@@ -445,14 +532,18 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
           auto p = c.products<T>();
           p.tiles_n = (int)ceil_div(c.k, S::BN);
           p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::BM, c.offsets);
-          go(input_kernel<T, O, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3((unsigned)groups_of_tiles(p.tiles)), S::M::THREADS,
-             S::M::LDS, s, p, c.matrices, static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
-             static_cast<O*>(decltype(mapped)::value ? static_cast<void*>(work + space.by_slot) : dx));
+          over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
+            p.first = first;
+            go(input_kernel<T, O, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, c.matrices,
+               static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
+               static_cast<O*>(decltype(mapped)::value ? static_cast<void*>(work + space.by_slot) : dx));
+          });
         });
       });
     if (dx && c.map && c.rows > 0)
-      in_launches(c.rows, kMaxGroups, [&](int64_t first, int64_t n) {
-        hipLaunchKernelGGL(gather_kernel<T>, dim3((unsigned)n), dim3(256), 0, s, n, c.k, each, (int)c.slots,
+      in_launches(c.rows, (kMaxGroups << 8) / ceil_div(c.k, 8), [&](int64_t first, int64_t n) {
+        const int units = (int)ceil_div(c.k, 8);
+        hipLaunchKernelGGL(gather_kernel<T>, dim3((unsigned)ceil_div(n * units, 256)), dim3(256), 0, s, n, c.k, each, (int)c.slots, units,
                            slots_of_row + first * each, reinterpret_cast<const float*>(work + space.by_slot),
                            static_cast<T*>(dx) + first * c.k);
       });
@@ -534,7 +625,7 @@ extern "C" netsim_status netsim_experts_gated(int32_t device, int32_t experts, i
 extern "C" int64_t netsim_experts_backward_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
                                                       int32_t matrices, int32_t has_offsets, int32_t has_rows) {
   if (!sizes_ok(experts, slots, n, cols) || matrices < 1 || matrices > 2) return -1;
-  return space_of(make_cut(experts, slots, n, cols, has_offsets), matrices, slots, n, cols, has_rows).bytes;
+  return space_of(make_cut(experts, slots, n, cols, matrices), matrices, slots, n, cols, has_rows).bytes;
 }
 
 extern "C" netsim_status netsim_experts_product_backward(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
@@ -547,7 +638,7 @@ extern "C" netsim_status netsim_experts_product_backward(int32_t device, int32_t
   return entry(what, device, [&] {
     const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w, d_w}, 1};
     if (!sizes_ok(experts, slots, n, cols)) return fail(NETSIM_E_INVALID, what, kSizes);
-    const Cut cut = make_cut(experts, slots, n, cols, d_offsets);
+    const Cut cut = make_cut(experts, slots, n, cols, 1);
     const Space space = space_of(cut, 1, slots, n, cols, d_row_of_slot);
     if (netsim_status bad = check_back(what, c, d_dy, ld_dy, d_slots_of_row, slots_each, d_dx, d_dw, d_dw, d_work, work_bytes, space))
       return bad;
@@ -570,7 +661,7 @@ extern "C" netsim_status netsim_experts_gated_backward(int32_t device, int32_t e
     const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w_gate, d_w_up}, 2};
     if (!sizes_ok(experts, slots, n, cols)) return fail(NETSIM_E_INVALID, what, kSizes);
     if (activation != NETSIM_SILU && activation != NETSIM_GELU) return fail(NETSIM_E_INVALID, what, "bad activation");
-    const Cut cut = make_cut(experts, slots, n, cols, d_offsets);
+    const Cut cut = make_cut(experts, slots, n, cols, 2);
     const Space space = space_of(cut, 2, slots, n, cols, d_row_of_slot);
     if (netsim_status bad =
             check_back(what, c, d_dh, ld_dh, d_slots_of_row, slots_each, d_dx, d_dw_gate, d_dw_up, d_work, work_bytes, space))

@@ -1,0 +1,122 @@
+// Products of few rows with each expert's weights: what a generating layer
+// runs.  The weights are read once and nothing else counts, so they go straight
+// to registers in the matrix cores' order (16 rows of a matrix, 64 bytes of
+// each), many loads in flight, and the summed index is cut over the waves of a
+// workgroup, whose sums meet in shared memory.  A workgroup takes up to 64 rows
+// of one expert and 16 rows of each of two matrices (gated's), or 32 of one.
+#pragma once
+
+#include "tile.h"
+
+namespace netsim_ops {
+namespace {
+
+// Products of 16 x 16 over 64 bytes of the summed index; a lane gives 16 bytes
+// of row (lane & 15) from byte 16 (lane >> 4) on, and gets of column
+// (lane & 15) the rows 4 (lane >> 4) + r.
+using f32x4 = __attribute__((ext_vector_type(4))) float;
+template <class T>
+struct Small;
+template <>
+struct Small<bf16> {
+  using Sum = f32x4;
+  static __device__ __forceinline__ Sum add(uint4 a, uint4 b, Sum c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Small<f16> {
+  using Sum = f32x4;
+  static __device__ __forceinline__ Sum add(uint4 a, uint4 b, Sum c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Small<int8_t> {
+  using Sum = i32x4;
+  static __device__ __forceinline__ Sum add(uint4 a, uint4 b, Sum c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+  }
+};
+
+constexpr int kFewRows = 64, kFewCols = 16, kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+
+// 16 bytes of a row of which `left` elements are there.
+template <class T, bool DIRECT>
+__device__ __forceinline__ uint4 few_chunk(const T* p, int left) {
+  if constexpr (DIRECT)
+    return *(left > 0 ? reinterpret_cast<const uint4*>(p) : &zeros);
+  else
+    return chunk_of(p, left);
+}
+
+// The sums of up to 16 MT rows, rows k elements long: x(m): row m, w[0], w[1]:
+// this lane's rows of the matrices.  Every wave takes its part of the summed
+// index and leaves its sums in `shared`.
+template <class T, int MT, bool DIRECT, class X>
+__device__ __forceinline__ void few_sums(typename Small<T>::Sum* shared, X&& x, const T* w0, const T* w1, int k) {
+  constexpr int PER = 16 / sizeof(T), STEP = 4 * PER, U = MT == 1 ? 8 : MT == 2 ? 6 : 4;
+  const int lane = threadIdx.x & 63, wave = wave_of_group(), at = (lane >> 4) * PER;
+  const int steps = (k + STEP - 1) / STEP;
+  const int from = steps * wave / kFewWaves, to = steps * (wave + 1) / kFewWaves;
+  typename Small<T>::Sum sum[2][MT] = {};
+  const T* rows[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) rows[m] = x(m * 16 + (lane & 15)) + at;
+  w0 += at;
+  w1 += at;
+  auto some = [&](int s0, auto number) {
+    constexpr int N = decltype(number)::value;
+    uint4 a[N][2], b[N][MT];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int c = (s0 + u) * STEP, left = k - c - at;
+      a[u][0] = few_chunk<T, DIRECT>(w0 + c, left);
+      a[u][1] = few_chunk<T, DIRECT>(w1 + c, left);
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) b[u][m] = few_chunk<T, DIRECT>(rows[m] + (s0 + u) * STEP, k - (s0 + u) * STEP - at);
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        sum[0][m] = Small<T>::add(a[u][0], b[u][m], sum[0][m]);
+        sum[1][m] = Small<T>::add(a[u][1], b[u][m], sum[1][m]);
+      }
+  };
+  int s = from;
+  for (; s + U <= to; s += U) some(s, std::integral_constant<int, U>{});
+  for (; s < to; ++s) some(s, std::integral_constant<int, 1>{});
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) shared[((wave * 2 + p) * MT + m) * 64 + lane] = sum[p][m];
+}
+
+// The workgroup's sum over its waves: matrix p, row m, column n.
+template <class T, int MT>
+__device__ __forceinline__ auto few_sum(const typename Small<T>::Sum* shared, int p, int m, int n) {
+  using V = std::conditional_t<sizeof(T) == 1, int, float>;
+  const V* at = reinterpret_cast<const V*>(shared) + ((p * MT + m / 16) * 64 + m % 16 + 16 * (n / 4)) * 4 + n % 4;
+  V sum = 0;
+#pragma unroll
+  for (int w = 0; w < kFewWaves; ++w) sum += at[w * 2 * MT * 256];
+  return sum;
+}
+
+// Calls f with the number of 16-row tiles that `count` rows take.
+template <class F>
+__device__ __forceinline__ void with_few(int count, F&& f) {
+  if (count <= 16)
+    f(std::integral_constant<int, 1>{});
+  else if (count <= 32)
+    f(std::integral_constant<int, 2>{});
+  else
+    f(std::integral_constant<int, 4>{});
+}
+constexpr int kFewShared = kFewWaves * 2 * 4 * 64 * 16;
+
+}  // namespace
+}  // namespace netsim_ops

@@ -294,41 +294,46 @@ struct Rows {
   int expert, from, to;
 };
 
+// Inclusive sums over the lanes of a wave.
+__device__ __forceinline__ int lanes_up(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, true);    // 1 lane down a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, true);    // 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, true);    // 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, true);    // 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // lane 15 of the row before, rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // lane 31, rows 2 and 3
+  return v;
+}
+
 // Tile number `want` when every expert's slots are cut into tiles of `size`:
-// the slots before the first expert's, the experts', those behind the last
-// one's.  offsets NULL: one expert has all slots.
+// the experts' slots, then those before the first one's and those behind the
+// last one's.  offsets NULL: one expert has all slots.
 __device__ __forceinline__ Rows find_rows(const int32_t* offsets, int experts, int slots, int size, int want) {
-  if (!offsets) {
-    const int64_t from = (int64_t)want * size;
-    return from < slots ? Rows{0, (int)from, (int)min(from + size, (int64_t)slots)} : Rows{-2, 0, 0};
-  }
+  auto part = [&](int expert, int from, int to, int nth) {
+    const int64_t start = from + (int64_t)nth * size;
+    return start < to ? Rows{expert, (int)start, (int)min(start + size, (int64_t)to)} : Rows{-2, 0, 0};
+  };
+  if (!offsets) return part(0, 0, slots, want);
   const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int first = 0; first < experts + 2; first += 64) {
-    const int i = first + lane;
+  for (int first = 0; first < experts; first += 64) {
+    const int e = first + lane;
     int a = 0, b = 0;
-    if (i < experts + 2) {
-      a = i == 0 ? 0 : min(max(offsets[i - 1], 0), slots);
-      b = i <= experts ? min(max(offsets[i], a), slots) : slots;
+    if (e < experts) {
+      a = min(max(offsets[e], 0), slots);
+      b = min(max(offsets[e + 1], a), slots);
     }
-    const int tiles = (int)(((int64_t)b - a + size - 1) / size);
-    int up = tiles;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int w = __shfl_up(up, o, 64);
-      if (lane >= o) up += w;
-    }
-    const uint64_t found = __ballot(want >= before + up - tiles && want < before + up);
+    const int tiles = (int)(((int64_t)b - a + size - 1) / size), up = lanes_up(tiles);
+    const uint64_t found = __ballot(want >= up - tiles && want < up);
     if (found) {
       const int at = __builtin_ctzll(found);
-      const int from = __builtin_amdgcn_readlane(a, at), to = __builtin_amdgcn_readlane(b, at);
-      const int nth = want - before - __builtin_amdgcn_readlane(up - tiles, at), e = first + at - 1;
-      const int start = from + nth * size;
-      return Rows{e < experts ? e : -1, start, min(to - start, size) + start};
+      return part(first + at, __builtin_amdgcn_readlane(a, at), __builtin_amdgcn_readlane(b, at),
+                  want - __builtin_amdgcn_readlane(up - tiles, at));
     }
-    before += __builtin_amdgcn_readlane(up, 63);
+    want -= __builtin_amdgcn_readlane(up, 63);
   }
-  return Rows{-2, 0, 0};
+  const int head = min(max(offsets[0], 0), slots), tail = min(max(offsets[experts], 0), slots);
+  const int tiles = (int)(((int64_t)head + size - 1) / size);
+  return want < tiles ? part(-1, 0, head, want) : part(-1, tail, slots, want - tiles);
 }
 
 // How many such tiles there may be.
@@ -344,7 +349,15 @@ __device__ __forceinline__ int64_t tile_of_group(uint32_t group) {
   const uint32_t die = group % kDies, nth = group / kDies;
   return ((int64_t)(nth / kNear) * kDies + die) * kNear + nth % kNear;
 }
-inline int64_t groups_of_tiles(int64_t tiles) { return ceil_div(tiles, kDies * kNear) * kDies * kNear; }
+constexpr int64_t kMaxGroups = 1 << 22;   // of a launch: at most 2^31 threads, whole rounds of dies
+
+// Launches that together have a workgroup for each of `tiles` tiles: go(first,
+// groups), for groups numbered by tile_of_group from `first` on.
+template <class F>
+void over_tiles(int64_t tiles, F&& go) {
+  const int64_t groups = ceil_div(tiles, kDies * kNear) * kDies * kNear;
+  in_launches(groups, kMaxGroups, [&](int64_t first, int64_t n) { go(first, (unsigned)n); });
+}
 
 }  // namespace
 }  // namespace netsim_ops
