@@ -81,6 +81,7 @@ struct Eights {
   const float* w_scales;
   int64_t tiles, first;   // all tiles, and where a launch begins
   int tiles_n;
+  bool near_x, near_w;    // x, an expert's matrix: fewer than 2^32 bytes
 };
 
 __device__ __forceinline__ int64_t row_of(const Eights& p, int slot) {
@@ -88,16 +89,17 @@ __device__ __forceinline__ int64_t row_of(const Eights& p, int slot) {
   return r >= 0 && r < p.rows ? r : -1;
 }
 
-template <class O, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
-  using M = Tile<int8_t, BM, BN, WM, WN>;
-  using A = RowTile<int8_t, BM, M::THREADS, true>;
-  using B = RowTile<int8_t, BN, M::THREADS, true>;
+template <class O, int SIZE>
+__global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
+  using M = Tile<int8_t, SIZE>;
+  using A = RowTile<int8_t, SIZE, M::THREADS, true>;
+  using B = A;
   extern __shared__ __align__(16) char shared[];
   const int64_t tile = p.first + tile_of_group(blockIdx.x);
   if (tile >= p.tiles) return;
-  const int n0 = (int)(tile % p.tiles_n) * BN;
-  const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
+  const At at = at_of_tile(tile, (int)(p.tiles / p.tiles_n), p.tiles_n);
+  const int n0 = at.col * SIZE;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, SIZE, at.row);
   if (rows.expert < -1) return;
   const int count = rows.to - rows.from, lane = threadIdx.x & 63;
 
@@ -106,34 +108,38 @@ __global__ __launch_bounds__(64 * WM * WN) void eight_kernel(Eights p, O* __rest
   if (rows.expert >= 0 && p.rows > 0) {
     A a;
     B b;
-    a.open([&](int r) {
+    a.open(p.x, p.near_x, [&](int r) {
       const int64_t at = row_of(p, rows.from + min(r, count - 1));
-      return p.x + (at < 0 ? 0 : at) * p.pitch;
+      return (at < 0 ? 0 : at) * p.pitch;
     });
-    b.open([&](int r) { return p.w + (first + min(n0 + r, p.n - 1)) * p.pitch; });
+    b.open(p.w + first * p.pitch, p.near_w, [&](int r) { return (int64_t)min(n0 + r, p.n - 1) * p.pitch; });
     m.template run<A, B>(
         shared, (p.pitch + A::STEP - 1) / A::STEP,
-        [&](Place stage, int s) {
-          a.load(stage, s * A::STEP, p.pitch);
-          b.load(stage + BM * kStepBytes, s * A::STEP, p.pitch);
+        [&](int s) { return a.quick(s * A::STEP, p.pitch) & b.near; },
+        [&](int n, Place stage, int s, auto quick) {
+          constexpr bool QUICK = decltype(quick)::value;
+          if (n < A::N)
+            a.template load<QUICK>(n, stage, s * A::STEP, p.pitch);
+          else
+            b.template load<QUICK>(n - A::N, stage + M::HALF, s * A::STEP, p.pitch);
         },
         [](Place) {});
   }
-  float x_scale[M::FM], w_scale[M::FN][16];
-  bool held[M::FM];
+  float x_scale[M::F], w_scale[M::F][16];
+  bool held[M::F];
 #pragma unroll
-  for (int i = 0; i < M::FM; ++i) {
+  for (int i = 0; i < M::F; ++i) {
     const int r = M::row0() + i * 32 + (lane & 31);
     const int64_t at = rows.expert >= 0 && r < count ? row_of(p, rows.from + r) : -1;
     held[i] = at >= 0;
     x_scale[i] = held[i] ? p.x_scales[at] : 0.0f;
   }
 #pragma unroll
-  for (int j = 0; j < M::FN; ++j)
+  for (int j = 0; j < M::F; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r)
       w_scale[j][r] = p.w_scales[first + min(n0 + M::col0() + j * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3), p.n - 1)];
-  M::template write<BN, M::FN>(shared, out + (int64_t)rows.from * ld_out + n0, ld_out, count, p.n - n0,
+  M::template write<SIZE, M::F>(shared, out + (int64_t)rows.from * ld_out + n0, ld_out, count, p.n - n0,
                                [&](int j) { return M::col0() + j * 32; },
                                [&](int i, int j, int r) { return held[i] ? (float)m.sum[i][j][r] * x_scale[i] * w_scale[j][r] : 0.0f; });
 }
@@ -223,7 +229,8 @@ extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts
       with_type(out_type, [&](auto o) {
         using O = decltype(o);
         auto run = [&](auto kernel, int bm, int bn, int threads, int lds) {
-          Eights p{experts, (int)slots, n, (int)padded(cols), rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales, 0, 0, 0};
+          Eights p{experts, (int)slots, n, (int)padded(cols), rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales, 0, 0, 0,
+                   rows * padded(cols) <= (int64_t)1 << 32, n * padded(cols) <= (int64_t)1 << 32};
           p.tiles_n = (int)ceil_div(n, bn);
           p.tiles = p.tiles_n * most_rows_tiles(experts, slots, bm, d_offsets);
           (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -235,9 +242,9 @@ extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts
         if (slots <= 24 * (int64_t)experts)
           run(few_eight_kernel<O>, kFewRows, 2 * kFewCols, kFewThreads, kFewShared);
         else if (slots / experts >= 256)
-          run(eight_kernel<O, 256, 256, 2, 4>, 256, 256, 512, Tile<int8_t, 256, 256, 2, 4>::LDS);
+          run(eight_kernel<O, 256>, 256, 256, 256, Tile<int8_t, 256>::LDS);
         else
-          run(eight_kernel<O, 128, 128, 2, 2>, 128, 128, 256, Tile<int8_t, 128, 128, 2, 2>::LDS);
+          run(eight_kernel<O, 128>, 128, 128, 256, Tile<int8_t, 128>::LDS);
       });
     });
   });

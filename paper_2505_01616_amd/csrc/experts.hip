@@ -30,6 +30,7 @@ struct Products {
   const T* w[2];
   int64_t tiles, first;     // all tiles, and where a launch begins
   int tiles_n;
+  bool near_x, near_w;      // x, an expert's matrix: fewer than 2^32 bytes
 };
 
 // The row of a slot, -1 for none.
@@ -84,55 +85,62 @@ __device__ __forceinline__ Eight<T> quad(const T* p) {
 // Rows by slot.  PRODUCT: out = y.  GATED: out = h; a tile's columns are 32 of
 // g and 32 of u in turn, so that a lane holds both of an element.  GATED_BACK:
 // out = dg, out2 = du, both [slots x ld_out].
-template <class T, int OUT, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void rows_kernel(Products<T> p, int activation, const T* __restrict__ dy,
+template <class T, int OUT, int SIZE, bool DIRECT>
+__global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products<T> p, int activation, const T* __restrict__ dy,
                                                             int64_t ld_dy, T* __restrict__ out, T* __restrict__ out2,
                                                             int64_t ld_out) {
-  using M = Tile<T, BM, BN, WM, WN>;
-  using A = RowTile<T, BM, M::THREADS, DIRECT>;
-  using B = RowTile<T, BN, M::THREADS, DIRECT>;
-  constexpr int COLS = OUT == PRODUCT ? BN : BN / 2, JN = OUT == PRODUCT ? M::FN : M::FN / 2;
+  using M = Tile<T, SIZE>;
+  using A = RowTile<T, SIZE, M::THREADS, DIRECT>;
+  using B = A;
+  constexpr int COLS = OUT == PRODUCT ? SIZE : SIZE / 2, JN = OUT == PRODUCT ? M::F : M::F / 2;
   extern __shared__ __align__(16) char shared[];
   const int64_t tile = p.first + tile_of_group(blockIdx.x);
   if (tile >= p.tiles) return;
-  const int n0 = (int)(tile % p.tiles_n) * COLS;
-  const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
+  const At at = at_of_tile(tile, (int)(p.tiles / p.tiles_n), p.tiles_n);
+  const int n0 = at.col * COLS;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, SIZE, at.row);
   if (rows.expert < -1) return;
   const int count = rows.to - rows.from, lane = threadIdx.x & 63;
 
   M m;
-  bool held[M::FM];   // whether there is a row for this lane's slots
+  bool held[M::F];   // whether there is a row for this lane's slots
 #pragma unroll
-  for (int i = 0; i < M::FM; ++i) {
+  for (int i = 0; i < M::F; ++i) {
     const int r = M::row0() + i * 32 + (lane & 31);
     held[i] = rows.expert >= 0 && r < count && row_of(p, rows.from + r) >= 0;
   }
   if (rows.expert >= 0 && p.rows > 0) {
     A a;
     B b;
-    a.open([&](int r) {
+    a.open(p.x, p.near_x, [&](int r) {
       const int64_t at = row_of(p, rows.from + min(r, count - 1));
-      return p.x + (at < 0 ? 0 : at) * p.ld;
+      return (at < 0 ? 0 : at) * p.ld;
     });
-    const int64_t first = (int64_t)rows.expert * p.n;
-    b.open([&](int r) {
-      if constexpr (OUT == PRODUCT) return p.w[0] + (first + min(n0 + r, p.n - 1)) * p.k;
-      constexpr int W = BN / WN;   // columns of a wave: half of them g's
-      const int n = n0 + r / W * (W / 2) + r % (W / 2);
-      return p.w[r % W / (W / 2)] + (first + min(n, p.n - 1)) * p.k;
+    const int64_t first = (int64_t)rows.expert * p.n * p.k;
+    // from g's matrix to u's, for chunks of u's columns (16 rows of a wave each)
+    const int64_t shift = OUT == PRODUCT ? 0 : p.w[1] - p.w[0];
+    auto of_u = [&](int i) { return (i * 64 + wave_of_group() * 16) % (SIZE / 2) >= SIZE / 4; };
+    b.open(p.w[0] + first, p.near_w, [&](int r) -> int64_t {
+      if constexpr (OUT == PRODUCT) return (int64_t)min(n0 + r, p.n - 1) * p.k;
+      constexpr int W = SIZE / 2;   // columns of a wave: half of them g's
+      return (int64_t)min(n0 + r / W * (W / 2) + r % (W / 2), p.n - 1) * p.k;
     });
     m.template run<A, B>(
         shared, (p.k + A::STEP - 1) / A::STEP,
-        [&](Place stage, int s) {
-          a.load(stage, s * A::STEP, p.k);
-          b.load(stage + BM * kStepBytes, s * A::STEP, p.k);
+        [&](int s) { return a.quick(s * A::STEP, p.k) & b.near; },
+        [&](int n, Place stage, int s, auto quick) {
+          constexpr bool QUICK = decltype(quick)::value;
+          if (n < A::N)
+            a.template load<QUICK>(n, stage, s * A::STEP, p.k);
+          else
+            b.template load<QUICK>(n - A::N, stage + M::HALF, s * A::STEP, p.k, OUT != PRODUCT && of_u(n - A::N) ? shift : 0);
         },
         [&](Place stage) {
           a.store(stage);
-          b.store(stage + BM * kStepBytes);
+          b.store(stage + M::HALF);
         });
   }
-  auto col = [&](int j) { return M::col0() / (M::FN / JN) + j * 32; };
+  auto col = [&](int j) { return M::col0() / (M::F / JN) + j * 32; };
   T* to = out + (int64_t)rows.from * ld_out + n0;
   if constexpr (OUT == PRODUCT) {
     M::template write<COLS, JN>(shared, to, ld_out, count, p.n - n0, col,
@@ -146,9 +154,9 @@ __global__ __launch_bounds__(64 * WM * WN) void rows_kernel(Products<T> p, int a
   } else {
     // the tile of dh, in whole lines through shared memory as well
     constexpr int PITCH = COLS + 8;
-    static_assert(BM * PITCH * sizeof(T) <= M::LDS, "");
+    static_assert(SIZE * PITCH * sizeof(T) <= M::LDS, "");
     T* tile_dy = reinterpret_cast<T*>(shared);
-    for (int t = threadIdx.x; t < BM * COLS / 8; t += M::THREADS) {
+    for (int t = threadIdx.x; t < SIZE * COLS / 8; t += M::THREADS) {
       const int r = t / (COLS / 8), c = t % (COLS / 8) * 8;
       *reinterpret_cast<uint4*>(tile_dy + r * PITCH + c) =
           chunk_of(dy + (int64_t)(rows.from + r) * ld_dy + n0 + c, r < count ? p.n - n0 - c : 0);
@@ -156,7 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN) void rows_kernel(Products<T> p, int a
     __syncthreads();
     with_activation(activation, [&](auto act) {
 #pragma unroll
-      for (int i = 0; i < M::FM; ++i)
+      for (int i = 0; i < M::F; ++i)
 #pragma unroll
         for (int j = 0; j < JN; ++j)
 #pragma unroll
@@ -224,18 +232,19 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Products<T> p, int act
 
 // Rows' gradients by slot: the sum over `pairs` of d W, d [slots x ld_d] of n
 // values a row.
-template <class T, class O, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void input_kernel(Products<T> p, int pairs, const T* __restrict__ d0,
+template <class T, class O, int SIZE, bool DIRECT>
+__global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void input_kernel(Products<T> p, int pairs, const T* __restrict__ d0,
                                                              const T* __restrict__ d1, int64_t ld_d,
                                                              O* __restrict__ dx) {
-  using M = Tile<T, BM, BN, WM, WN>;
-  using A = RowTile<T, BM, M::THREADS, DIRECT>;
-  using B = ColTile<T, BN, M::THREADS, DIRECT>;
+  using M = Tile<T, SIZE>;
+  using A = RowTile<T, SIZE, M::THREADS, DIRECT>;
+  using B = ColTile<T, SIZE, M::THREADS, DIRECT>;
   extern __shared__ __align__(16) char shared[];
   const int64_t tile = p.first + tile_of_group(blockIdx.x);
   if (tile >= p.tiles) return;
-  const int c0 = (int)(tile % p.tiles_n) * BN;
-  const Rows rows = find_rows(p.offsets, p.experts, p.slots, BM, (int)(tile / p.tiles_n));
+  const At at = at_of_tile(tile, (int)(p.tiles / p.tiles_n), p.tiles_n);
+  const int c0 = at.col * SIZE;
+  const Rows rows = find_rows(p.offsets, p.experts, p.slots, SIZE, at.row);
   if (rows.expert < -1) return;
   const int count = rows.to - rows.from;
 
@@ -243,25 +252,32 @@ __global__ __launch_bounds__(64 * WM * WN) void input_kernel(Products<T> p, int 
   if (rows.expert >= 0) {
     A a;
     B b;
-    a.open([&](int r) { return d0 + (int64_t)(rows.from + min(r, count - 1)) * ld_d; });
-    const T* w0 = p.w[0] + (int64_t)rows.expert * p.n * p.k;
-    b.open(w0, p.k, c0, p.k);
+    a.open(d0 + (int64_t)rows.from * ld_d, ld_d < (1 << 22), [&](int r) { return (int64_t)min(r, count - 1) * ld_d; });
+    b.open(p.w[0] + (int64_t)rows.expert * p.n * p.k, p.near_w, p.k, c0, p.k);
     const int steps = (p.n + A::STEP - 1) / A::STEP;
     m.template run<A, B>(
         shared, steps * pairs,
-        [&](Place stage, int s) {
-          const bool second = s >= steps;
+        [&](int s) { return a.quick((s >= steps ? s - steps : s) * A::STEP, p.n) & b.near & (s < steps * pairs); },
+        [&](int n, Place stage, int s, auto quick) {
+          constexpr bool QUICK = decltype(quick)::value;
+          const bool second = s >= steps && pairs == 2;
           const int k0 = (second ? s - steps : s) * A::STEP;
-          a.load(stage, k0, p.n, second ? d1 - d0 : 0);
-          b.load(stage + BM * kStepBytes, [&](int i) { return k0 + b.row(i) < p.n ? k0 + b.row(i) : -1; },
-                 second ? p.w[1] - p.w[0] : 0);
+          const int64_t shift = second ? p.w[1] - p.w[0] : 0;
+          if (n < A::N) {
+            a.template load<QUICK>(n, stage, k0, p.n, second ? d1 - d0 : 0);
+          } else if constexpr (QUICK) {
+            b.load_run(n - A::N, stage + M::HALF, k0 + B::row(n - A::N), shift);
+          } else {
+            const int k = k0 + B::row(n - A::N) + B::mine();
+            b.load(n - A::N, stage + M::HALF, k < p.n ? k : -1, shift);
+          }
         },
         [&](Place stage) {
           a.store(stage);
-          b.store(stage + BM * kStepBytes);
+          b.store(stage + M::HALF);
         });
   }
-  M::template write<BN, M::FN>(shared, dx + (int64_t)rows.from * p.k + c0, p.k, count, p.k - c0,
+  M::template write<SIZE, M::F>(shared, dx + (int64_t)rows.from * p.k + c0, p.k, count, p.k - c0,
                                [&](int j) { return M::col0() + j * 32; },
                                [&](int i, int j, int r) { return m.sum[i][j][r]; });
 }
@@ -290,17 +306,17 @@ __global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int cols, int
 // The weights' gradients: dW[e][n][c] = the sum over e's slots of d[s][n]
 // x[row(s)][c].  Both factors have the summed index as their slow one.
 // blockIdx.z: the matrix.
-template <class T, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ __launch_bounds__(64 * WM * WN) void weight_kernel(Products<T> p, Sums g, Cut cut, const Item* __restrict__ items,
+template <class T, int SIZE, bool DIRECT>
+__global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Products<T> p, Sums g, Cut cut, const Item* __restrict__ items,
                                                               const T* __restrict__ d0, const T* __restrict__ d1,
                                                               int64_t ld_d, T* __restrict__ dw0, T* __restrict__ dw1,
                                                               float* __restrict__ partials) {
-  using M = Tile<T, BM, BN, WM, WN>;
-  using A = ColTile<T, BM, M::THREADS, DIRECT>;
-  using B = ColTile<T, BN, M::THREADS, DIRECT>;
+  using M = Tile<T, SIZE>;
+  using A = ColTile<T, SIZE, M::THREADS, DIRECT>;
+  using B = A;
   extern __shared__ __align__(16) char shared[];
-  const int tiles_n = (g.n + BM - 1) / BM;
-  const int n0 = (int)(blockIdx.x % tiles_n) * BM, c0 = (int)(blockIdx.x / tiles_n) * BN;
+  const int tiles_n = (g.n + SIZE - 1) / SIZE;
+  const int n0 = (int)(blockIdx.x % tiles_n) * SIZE, c0 = (int)(blockIdx.x / tiles_n) * SIZE;
   Item it;
   if (cut.plan == Cut::WHOLE)
     it = segment(p.offsets, blockIdx.y, g.slots);
@@ -314,63 +330,86 @@ __global__ __launch_bounds__(64 * WM * WN) void weight_kernel(Products<T> p, Sum
   M m;
   A a;
   B b;
-  a.open(blockIdx.z ? d1 : d0, ld_d, n0, g.n);
-  b.open(p.x, p.ld, c0, g.cols);
-  // The slots' rows, read a step ahead: what a and b bring in of a step are the
-  // same slots.  A slot without a row takes no part, whatever its d holds.
-  static_assert(A::N == B::N && A::EACH == B::EACH, "");
-  const int64_t rows = min(p.rows, (int64_t)0x7fffffff);
-  int row[A::N];
-  auto look = [&](int first) {
+  a.open((blockIdx.z ? d1 : d0) + (int64_t)it.from * ld_d, (it.to - it.from) * ld_d < (int64_t)1 << 31, ld_d, n0, g.n);
+  b.open(p.x, p.near_x, p.ld, c0, g.cols);
+  // A slot without a row takes no part, whatever its d holds.  The numbers of
+  // the rows that a wave brings in together are the same for its lanes, so they
+  // come by scalar loads, a step before their turn.
+  const uint32_t rows = (uint32_t)min(p.rows, (int64_t)0x7fffffff);
+  const auto* map = (const __attribute__((address_space(4))) int32_t*)p.map;
+  const int slots = it.to - it.from;
+  int row[A::N][A::ROWS];
+  auto look = [&](int i, int s) {
+    const int first = it.from + s * A::STEP + A::row(i);
 #pragma unroll
-    for (int i = 0; i < A::N; ++i) {
-      const int k = first + a.row(i);
-      row[i] = p.map ? p.map[min(k, it.to - 1)] : k;
-    }
+    for (int j = 0; j < A::ROWS; ++j) row[i][j] = p.map ? map[min(first + j, it.to - 1)] : first + j;
   };
-  if (it.from < it.to) look(it.from);
-  m.template run<A, B>(
-      shared, (it.to - it.from + A::STEP - 1) / A::STEP,
-      [&](Place stage, int s) {
-        const int first = it.from + s * A::STEP;
-        bool held[A::N];
+  if (slots > 0)
 #pragma unroll
-        for (int i = 0; i < A::N; ++i) held[i] = first + a.row(i) < it.to && row[i] >= 0 && row[i] < rows;
-        a.load(stage, [&](int i) { return held[i] ? first + a.row(i) : -1; });
-        b.load(stage + BM * kStepBytes, [&](int i) { return held[i] ? row[i] : -1; });
-        look(first + A::STEP);
+    for (int i = 0; i < A::N; ++i) look(i, 0);
+  m.template run<A, B>(
+      shared, (slots + A::STEP - 1) / A::STEP,
+      [&](int s) {
+        bool all = a.near & b.near & ((s + 1) * A::STEP <= slots);
+#pragma unroll
+        for (int i = 0; i < A::N; ++i)
+#pragma unroll
+          for (int j = 0; j < A::ROWS; ++j) all &= (uint32_t)row[i][j] < rows;
+        return all;
+      },
+      [&](int n, Place stage, int s, auto quick) {
+        const int i = n % A::N, first = s * A::STEP + A::row(i);
+        if constexpr (decltype(quick)::value) {
+          if (n < A::N) {
+            a.load_run(i, stage, first);
+          } else {
+            b.load_rows(i, stage + M::HALF, row[i]);
+            look(i, s + 1);
+          }
+        } else {
+          const int slot = first + A::mine();
+          int r = row[i][0];
+#pragma unroll
+          for (int j = 1; j < A::ROWS; ++j) r = j == A::mine() ? row[i][j] : r;
+          const bool held = (slot < slots) & ((uint32_t)r < rows);
+          if (n < A::N) {
+            a.load(i, stage, held ? slot : -1);
+          } else {
+            b.load(i, stage + M::HALF, held ? r : -1);
+            look(i, s + 1);
+          }
+        }
       },
       [&](Place stage) {
         a.store(stage);
-        b.store(stage + BM * kStepBytes);
+        b.store(stage + M::HALF);
       });
   auto col = [&](int j) { return M::col0() + j * 32; };
   auto value = [&](int i, int j, int r) { return m.sum[i][j][r]; };
   const int64_t size = (int64_t)g.n * g.cols, at = (int64_t)n0 * g.cols + c0;
   if (it.partial < 0)
-    M::template write<BN, M::FN>(shared, (blockIdx.z ? dw1 : dw0) + it.expert * size + at, g.cols, g.n - n0, g.cols - c0, col, value);
+    M::template write<SIZE, M::F>(shared, (blockIdx.z ? dw1 : dw0) + it.expert * size + at, g.cols, g.n - n0, g.cols - c0, col, value);
   else
-    M::template write<BN, M::FN>(shared, partials + (blockIdx.z * cut.partials + it.partial) * size + at, g.cols, g.n - n0,
+    M::template write<SIZE, M::F>(shared, partials + (blockIdx.z * cut.partials + it.partial) * size + at, g.cols, g.n - n0,
                                  g.cols - c0, col, value);
 }
 
-// A tile's shape.
-template <class T, int BM_, int BN_, int WM_, int WN_, bool DIRECT_>
+// Calls f with the tile's shape for `size` (256 or 128).  Rows that are no
+// whole chunks pass through registers, which leaves too few for the larger tile.
+template <class T, int SIZE_, bool DIRECT_>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int SIZE = SIZE_;
   static constexpr bool DIRECT = DIRECT_;
-  using M = Tile<T, BM, BN, WM, WN>;
+  using M = Tile<T, SIZE>;
 };
-// Calls f with the shape for `size` (256 or 128).  Rows that are no whole
-// chunks pass through registers, which leaves too few for the larger tile.
 template <class T, class F>
 void with_tile(int size, bool direct, F&& f) {
   if (!direct)
-    f(Shape<T, 128, 128, 2, 2, false>{});
+    f(Shape<T, 128, false>{});
   else if (size == 256)
-    f(Shape<T, 256, 256, 2, 4, true>{});
+    f(Shape<T, 256, true>{});
   else
-    f(Shape<T, 128, 128, 2, 2, true>{});
+    f(Shape<T, 128, true>{});
 }
 template <class F>
 void with_bool(bool b, F&& f) {
@@ -402,13 +441,15 @@ struct Call {
   template <class T>
   Products<T> products() const {
     return Products<T>{experts, (int)slots, n, k, rows, ld, static_cast<const T*>(x), map, offsets,
-                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0, 0};
+                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0, 0,
+                       rows <= ((int64_t)1 << 31) / ld, (int64_t)n * k <= (int64_t)1 << 31};
   }
   // Whether x's rows, and the weights', are whole chunks of 16 bytes.
   bool x_direct() const { return ld % 8 == 0 && k % 8 == 0 && aligned(x, 16); }
   bool w_direct() const { return k % 8 == 0 && aligned(w[0], 16) && aligned(w[1], 16); }
 };
 
+constexpr int64_t kMaxPitch = 0x7fffffff;
 constexpr const char* kSizes = "experts must be 1 .. 1024, the matrices' rows and columns 1 .. 2^20, slots 0 .. 2^31-4097";
 bool sizes_ok(int32_t experts, int64_t slots, int32_t n, int32_t k) {
   return experts >= 1 && experts <= 1024 && slots >= 0 && slots <= kMaxSlots && n >= 1 && n <= kMaxCols && k >= 1 && k <= kMaxCols;
@@ -418,7 +459,7 @@ netsim_status check(const char* what, const Call& c) {
   if (c.type != NETSIM_BF16 && c.type != NETSIM_F16) return fail(NETSIM_E_INVALID, what, "the type must be of 16 bits");
   if (!sizes_ok(c.experts, c.slots, c.n, c.k)) return fail(NETSIM_E_INVALID, what, kSizes);
   if (c.rows < 0) return fail(NETSIM_E_INVALID, what, "rows is below 0");
-  if (c.ld < c.k) return fail(NETSIM_E_INVALID, what, "ld_x is below the row's length");
+  if (c.ld < c.k || c.ld > kMaxPitch) return fail(NETSIM_E_INVALID, what, "ld_x is below the row's length, or not below 2^31");
   if (!c.map && c.rows != c.slots) return fail(NETSIM_E_INVALID, what, "without a list of rows there must be one for every slot");
   if (!c.offsets && c.experts != 1) return fail(NETSIM_E_INVALID, what, "several experts need offsets");
   if ((c.rows > 0 && !c.x) || !c.w[0] || !c.w[1]) return fail(NETSIM_E_INVALID, what, "NULL array");
@@ -465,11 +506,11 @@ void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, 
     with_tile<T>(tile_of(c.slots, c.experts, c.n, c.k), c.x_direct() && c.w_direct(), [&](auto shape) {
       using S = decltype(shape);
       auto p = c.products<T>();
-      p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? S::BN : S::BN / 2);
-      p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::BM, c.offsets);
+      p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? S::SIZE : S::SIZE / 2);
+      p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::SIZE, c.offsets);
       over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
         p.first = first;
-        go(rows_kernel<T, OUT, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, activation,
+        go(rows_kernel<T, OUT, S::SIZE, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, activation,
            static_cast<const T*>(dy), ld_dy, static_cast<T*>(out), static_cast<T*>(out2), ld_out);
       });
     });
@@ -530,11 +571,11 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
           using S = decltype(shape);
           using O = std::conditional_t<decltype(mapped)::value, float, T>;
           auto p = c.products<T>();
-          p.tiles_n = (int)ceil_div(c.k, S::BN);
-          p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::BM, c.offsets);
+          p.tiles_n = (int)ceil_div(c.k, S::SIZE);
+          p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::SIZE, c.offsets);
           over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
             p.first = first;
-            go(input_kernel<T, O, S::BM, S::BN, S::WM, S::WN, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, c.matrices,
+            go(input_kernel<T, O, S::SIZE, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, c.matrices,
                static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
                static_cast<O*>(decltype(mapped)::value ? static_cast<void*>(work + space.by_slot) : dx));
           });
@@ -556,8 +597,8 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
         float* partials = reinterpret_cast<float*>(work + space.partials);
         if (cut.plan == Cut::LISTED)
           hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(c.experts, 64) * 64), 0, s, g, cut, c.offsets, items, joins);
-        go(weight_kernel<T, S::BM, S::BN, S::WM, S::WN, S::DIRECT>,
-           dim3((unsigned)(ceil_div(c.n, S::BM) * ceil_div(c.k, S::BN)), (unsigned)(cut.plan == Cut::WHOLE ? c.experts : cut.items),
+        go(weight_kernel<T, S::SIZE, S::DIRECT>,
+           dim3((unsigned)(ceil_div(c.n, S::SIZE) * ceil_div(c.k, S::SIZE)), (unsigned)(cut.plan == Cut::WHOLE ? c.experts : cut.items),
                 c.matrices),
            S::M::THREADS, S::M::LDS, s, c.products<T>(), g, cut, items, static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
            static_cast<T*>(dw0), static_cast<T*>(dw1), partials);
@@ -573,7 +614,7 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
 netsim_status check_back(const char* what, const Call& c, const void* dy, int64_t ld_dy, const int32_t* slots_of_row, int32_t each,
                          const void* dx, const void* dw0, const void* dw1, const void* work, int64_t work_bytes, const Space& space) {
   if (netsim_status bad = check(what, c)) return bad;
-  if (ld_dy < c.n) return fail(NETSIM_E_INVALID, what, "the gradient's row pitch is below n");
+  if (ld_dy < c.n || ld_dy > kMaxPitch) return fail(NETSIM_E_INVALID, what, "the gradient's row pitch is below n, or not below 2^31");
   if (c.slots > 0 && !dy) return fail(NETSIM_E_INVALID, what, "NULL array");
   if (!dw0 != !dw1) return fail(NETSIM_E_INVALID, what, "both matrices' gradients or neither");
   if (dx && c.map && (each < 1 || (c.rows > 0 && !slots_of_row)))

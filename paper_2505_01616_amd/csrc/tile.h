@@ -1,15 +1,22 @@
 // Matrix products by tiles: what the products of experts (experts.hip) and
 // those in 8 bits (eight.hip) share.
 //
-// A workgroup computes a tile of BM rows and BN columns.  A step brings 128
-// bytes of the summed index of both operands into shared memory; two stages
-// alternate, so the next step's loads are in flight while the matrix cores
-// work on this one.  An operand lies in memory with the summed index as its
-// fast one (RowTile) or as its slow one (ColTile, 16-bit values only); it goes
-// to shared memory as it lies, in chunks of 16 bytes whose place is exclusive-
-// ored with the row, so that neither the stores nor the matrix cores' reads
-// meet in a bank: a read of 16 lanes takes one chunk each of 16 rows, a
+// A workgroup of four waves computes a tile of BM rows and BN columns.  A step
+// brings 64 bytes of the summed index of both operands into shared memory, four
+// stages of which are there in turn, so loads have more than two steps until
+// their values are needed.  An operand lies in memory with the summed index as
+// its fast one (RowTile) or as its slow one (ColTile, 16-bit values only); it
+// goes to shared memory as it lies, in chunks of 16 bytes whose place is
+// exclusive-ored with the row, so that neither the stores nor the matrix cores'
+// reads meet in a bank: a read of 16 lanes takes one chunk each of 16 rows, a
 // transposing one 64 bytes each of four.
+//
+// Shared memory gives 128 bytes a cycle: a step of a 256 x 256 tile stores 32
+// KiB and, with 128 x 128 a wave, reads 64 KiB, in the 1,024 cycles of its
+// products (eight waves of 128 x 64 would read 96 KiB and be bound by that).
+// With one wave on a SIMD nothing else hides its waits: operands are read and
+// loads started between the products that come before them, and a stage is
+// handed over half a step early.
 #pragma once
 
 #include "values.h"
@@ -17,7 +24,7 @@
 namespace netsim_ops {
 namespace {
 
-constexpr int kStepBytes = 128;
+constexpr int kStepBytes = 64;   // of the summed index
 using i32x4 = __attribute__((ext_vector_type(4))) int;
 using i32x16 = __attribute__((ext_vector_type(16))) int;
 using f16x8 = __attribute__((ext_vector_type(8))) _Float16;
@@ -59,6 +66,10 @@ struct Matrix<int8_t> {
 __device__ __forceinline__ void to_shared(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
 }
+// From base + off, base the same for the wave: no 64-bit address per lane.
+__device__ __forceinline__ void to_shared(const void* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "memory");
+}
 
 __device__ __forceinline__ int wave_of_group() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
@@ -80,81 +91,127 @@ __device__ __forceinline__ uint4 chunk_of(const T* p, int left) {
   return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
 }
 
-// Rows of which a step takes 128 bytes each.  DIRECT: rows start at multiples
+using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
+using lds_u32x4 = __attribute__((address_space(3))) const u32x4;
+
+// Rows of which a step takes 64 bytes each.  DIRECT: rows start at multiples
 // of 16 bytes and have whole chunks.
-template <class T, int R, int THREADS, bool DIRECT>
+template <class T, int R, int THREADS, bool DIRECT_>
 struct RowTile {
-  static constexpr int N = R * 8 / THREADS, PER = 16 / sizeof(T), STEP = kStepBytes / sizeof(T);
-  static_assert(THREADS / 8 % 16 == 0 && N * THREADS == R * 8, "a thread's chunks have the same place in their rows");
-  const T* at[N];
+  static constexpr bool DIRECT = DIRECT_;
+  static constexpr int CHUNKS = kStepBytes / 16, N = R * CHUNKS / THREADS, PER = 16 / sizeof(T), STEP = kStepBytes / sizeof(T);
+  static_assert(THREADS / CHUNKS % 16 == 0 && N * THREADS == R * CHUNKS, "a thread's chunks have the same place in their rows");
+  const T* base;
+  int64_t at[N];      // of this thread's chunks, in elements from base on
+  uint32_t off[N];    // the same in bytes, where that fits
+  bool near;
   uint4 held[DIRECT ? 1 : N];
   int col;
 
-  // row(r): where row r of the tile starts (a row that may be read).
+  // Row r of the tile starts row(r) elements behind `from` and may be read;
+  // all_near: all rows end less than 2^32 bytes behind it.
   template <class F>
-  __device__ __forceinline__ void open(F&& row) {
-    const int r = threadIdx.x >> 3;
-    col = ((threadIdx.x & 7) ^ ((r >> 1) & 7)) * PER;
-#pragma unroll
-    for (int i = 0; i < N; ++i) at[i] = row(r + i * (THREADS / 8)) + col;
-  }
-  // Step from element k0 of rows of k elements; shift: of another array of
-  // such rows.
-  __device__ __forceinline__ void load(Place stage, int k0, int k, int64_t shift = 0) {
-    const int left = k - k0 - col, wave = wave_of_group();
+  __device__ __forceinline__ void open(const T* from, bool all_near, F&& row) {
+    const int r = threadIdx.x / CHUNKS;
+    base = from;
+    near = all_near;
+    col = (threadIdx.x % CHUNKS ^ (r >> 2) % CHUNKS) * PER;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const T* from = at[i] + shift + k0;
-      if constexpr (DIRECT)
-        to_shared(left > 0 ? static_cast<const void*>(from) : &zeros, stage.address + i * THREADS * 16 + wave * 1024);
-      else
-        held[i] = chunk_of(from, left);
+      at[i] = row(r + i * (THREADS / CHUNKS)) + col;
+      off[i] = (uint32_t)at[i] * sizeof(T);
     }
+  }
+  // Whether the step from element k0 of rows of k elements may go quickly: by
+  // 32-bit offsets, with nothing beyond the rows' ends.
+  __device__ __forceinline__ bool quick(int k0, int k) const { return near && k0 + STEP <= k; }
+  // This thread's chunk i of it, zeros beyond; shift: of another array of such
+  // rows.
+  template <bool QUICK>
+  __device__ __forceinline__ void load(int i, Place stage, int k0, int k, int64_t shift = 0) {
+    const T* step = base + shift + k0;
+    const uint32_t to = stage.address + i * THREADS * 16 + wave_of_group() * 1024;
+    const int left = k - k0 - col;
+    if constexpr (!DIRECT)
+      held[i] = chunk_of(step + at[i], left);
+    else if constexpr (QUICK)
+      to_shared(step, off[i], to);
+    else
+      to_shared(left > 0 ? static_cast<const void*>(step + at[i]) : &zeros, to);
   }
   __device__ __forceinline__ void store(Place stage) {
     if constexpr (!DIRECT)
 #pragma unroll
       for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = held[i];
   }
-  // The operand of rows first .. first + 31, bytes 32 h .. of the step.
-  static __device__ __forceinline__ uint4 operand(const char* stage, int first, int h) {
-    const int lane = threadIdx.x & 63;
-    return *reinterpret_cast<const uint4*>(stage + (first + (lane & 31)) * kStepBytes +
-                                           ((((lane >> 5) ^ (lane >> 1)) & 7) * 16 ^ 32 * h));
-  }
+  // The operand of rows 32 i .. 32 i + 31 of a wave's part, bytes 32 h .. of the
+  // step; lane_at: where a lane's part of it lies.
+  struct Lane {
+    uint32_t of[2];
+    __device__ __forceinline__ explicit Lane(int first) {
+      const int lane = threadIdx.x & 63;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        of[h] = (first + (lane & 31)) * kStepBytes + ((lane >> 5 ^ lane >> 2) % CHUNKS * 16 ^ 32 * h);
+    }
+    __device__ __forceinline__ uint4 operand(uint32_t stage, int i, int h) const {
+      return __builtin_bit_cast(uint4, *((lds_u32x4*)(stage + of[h]) + i * 32 * kStepBytes / 16));
+    }
+  };
 };
 
-// The summed index as the slow one: 64 rows of R columns each.
-template <class T, int R, int THREADS, bool DIRECT>
+// The summed index as the slow one: 32 rows of R columns each.
+template <class T, int R, int THREADS, bool DIRECT_>
 struct ColTile {
   static_assert(sizeof(T) == 2 && R >= 128, "");
-  static constexpr int CHUNKS = R / 8, N = R * 8 / THREADS, EACH = THREADS / CHUNKS, STEP = 64;
+  static constexpr bool DIRECT = DIRECT_;
+  static constexpr int STEP = kStepBytes / 2, CHUNKS = R / 8, N = STEP * CHUNKS / THREADS, EACH = THREADS / CHUNKS;
+  static constexpr int ROWS = 64 / CHUNKS;   // that a wave brings in at a time
   static_assert(EACH % 4 == 0 && EACH * N == STEP, "a thread's chunks have the same place in their rows");
-  const T* at;
-  int64_t ld;
+  const T* base;
+  uint32_t ld;       // pitches are below 2^31
+  uint32_t col, own;
+  bool near;
   uint4 held[DIRECT ? 1 : N];
   int left;
 
-  __device__ __forceinline__ int row(int i) const { return threadIdx.x / CHUNKS + i * EACH; }
-  __device__ __forceinline__ void open(const T* base, int64_t pitch, int c0, int cols) {
-    const int c = c0 + (threadIdx.x % CHUNKS ^ (4 * (row(0) & 3))) * 8;
+  // The first of the rows of a step that this wave brings in as chunk i.
+  static __device__ __forceinline__ int row(int i) { return wave_of_group() * ROWS + i * EACH; }
+  // Which of them is this lane's.
+  static __device__ __forceinline__ int mine() { return (threadIdx.x & 63) / CHUNKS; }
+
+  // Columns c0 .. of rows of `cols`; what is read of columns beyond reaches no
+  // result.  all_near: all rows end less than 2^32 bytes behind `from`.
+  __device__ __forceinline__ void open(const T* from, bool all_near, int64_t pitch, int c0, int cols) {
+    int c = c0 + (threadIdx.x % CHUNKS ^ (4 * (threadIdx.x / CHUNKS & 3))) * 8;
     left = cols - c;
-    at = base + c;
-    ld = pitch;
+    if (DIRECT && left <= 0) c = c0;
+    base = from + c0;
+    col = c - c0;
+    ld = (uint32_t)pitch;
+    near = all_near;
+    own = (mine() * ld + col) * 2;
   }
-  // Rows r(i) of the array, i: this thread's chunks; none where r is negative.
-  template <class F>
-  __device__ __forceinline__ void load(Place stage, F&& r, int64_t shift = 0) {
-    const int wave = wave_of_group();
+  __device__ __forceinline__ uint32_t place(int i, Place stage) const { return stage.address + i * THREADS * 16 + wave_of_group() * 1024; }
+  // Chunk i of a step: r, this lane's row; none: negative.
+  __device__ __forceinline__ void load(int i, Place stage, int r, int64_t shift = 0) {
+    const T* from = base + shift + (uint64_t)(uint32_t)r * ld + col;
+    if constexpr (!DIRECT)
+      held[i] = chunk_of(from, r >= 0 ? left : 0);
+    else
+      to_shared(r >= 0 ? static_cast<const void*>(from) : &zeros, place(i, stage));
+  }
+  // The same quickly, where every lane has a row and they are near: consecutive
+  // rows from `first` on,
+  __device__ __forceinline__ void load_run(int i, Place stage, int first, int64_t shift = 0) {
+    to_shared(base + shift + (uint64_t)(uint32_t)first * ld, own, place(i, stage));
+  }
+  // or the rows r, the same for the wave.
+  __device__ __forceinline__ void load_rows(int i, Place stage, const int (&r)[ROWS], int64_t shift = 0) {
+    uint32_t from = (uint32_t)r[0] * ld;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int64_t n = r(i);
-      const T* from = at + shift + n * ld;
-      if constexpr (DIRECT)
-        to_shared(left > 0 && n >= 0 ? static_cast<const void*>(from) : &zeros, stage.address + i * THREADS * 16 + wave * 1024);
-      else
-        held[i] = chunk_of(from, n >= 0 ? left : 0);
-    }
+    for (int j = 1; j < ROWS; ++j) from = mine() == j ? (uint32_t)r[j] * ld : from;
+    to_shared(base + shift, (from + col) * 2, place(i, stage));
   }
   __device__ __forceinline__ void store(Place stage) {
     if constexpr (!DIRECT)
@@ -163,98 +220,128 @@ struct ColTile {
   }
   // Lanes 0-15 give four rows of 16 columns and get a column each; lanes 16-31
   // the next 16 columns, lanes 32-63 the rows 8 further on.
-  static __device__ __forceinline__ uint4 operand(const char* stage, int first, int h) {
-    const int lane = threadIdx.x & 63, k = (lane >> 5) * 8 + ((lane >> 2) & 3);
-    const int chunk = (first / 8 ^ (4 * (k & 3))) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-    const char* from = stage + (h * 16 + k) * R * 2 + chunk * 16 + (lane & 1) * 8;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 4 * R * 2));
-    return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-  }
+  struct Lane {
+    uint32_t of[4];
+    __device__ __forceinline__ explicit Lane(int first) {
+      const int lane = threadIdx.x & 63, k = (lane >> 5) * 8 + ((lane >> 2) & 3);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        of[i] = k * R * 2 + (((first / 8 + 4 * i) ^ (4 * (k & 3))) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) * 16 + (lane & 1) * 8;
+    }
+    __device__ __forceinline__ uint4 operand(uint32_t stage, int i, int h) const {
+      const auto* from = (__attribute__((address_space(3))) char*)(stage + of[i]) + h * 16 * R * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 4 * R * 2));
+      return __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  };
 };
 
-// A tile's sums and where a wave's part of them lies: WM x WN waves, each with
-// FM x FN products of 32 x 32.
-template <class T, int BM, int BN, int WM, int WN>
+// A tile's sums and where a wave's part of them lies: 2 x 2 waves, each with
+// F x F products of 32 x 32.
+template <class T, int SIZE>
 struct Tile {
-  static constexpr int THREADS = 64 * WM * WN, FM = BM / WM / 32, FN = BN / WN / 32;
-  static constexpr int STAGE = (BM + BN) * kStepBytes, LDS = 2 * STAGE;
+  static constexpr int THREADS = 256, F = SIZE / 64, STAGES = 4;
+  static constexpr int HALF = SIZE * kStepBytes, STAGE = 2 * HALF, LDS = STAGES * STAGE;
   using M = Matrix<T>;
-  typename M::Sum sum[FM][FN];
+  typename M::Sum sum[F][F];
 
   __device__ __forceinline__ Tile() {
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < F; ++i)
 #pragma unroll
-      for (int j = 0; j < FN; ++j) sum[i][j] = typename M::Sum{};
+      for (int j = 0; j < F; ++j) sum[i][j] = typename M::Sum{};
   }
-  static __device__ __forceinline__ int row0() { return wave_of_group() / WN * (BM / WM); }
-  static __device__ __forceinline__ int col0() { return wave_of_group() % WN * (BN / WN); }
+  static __device__ __forceinline__ int row0() { return wave_of_group() / 2 * (SIZE / 2); }
+  static __device__ __forceinline__ int col0() { return wave_of_group() % 2 * (SIZE / 2); }
 
-  // `count` steps; load(stage, s) brings in step s, store(stage) what of it
-  // went to registers.  At the end no wave reads shared memory any more.
-  template <class A, class B, class Load, class Store>
-  __device__ __forceinline__ void run(char* shared, int count, Load&& load, Store&& store) {
+  // `count` steps.  load(n, stage, s, quick) brings in this thread's chunk n of
+  // step s, A's N and then B's (nothing but zeros from s = count on), quick(s)
+  // says whether it may go quickly; store(stage) what went to registers of it.  At
+  // the end no wave reads shared memory, and none writes it.
+  template <class A, class B, class Quick, class Load, class Store>
+  __device__ __forceinline__ void run(char* shared, int count, Quick&& quick, Load&& load, Store&& store) {
+    static_assert(A::N == B::N && A::DIRECT == B::DIRECT, "");
+    constexpr bool DIRECT = A::DIRECT;
+    constexpr int N = A::N, AHEAD = DIRECT ? 3 : 2;
+    const Place base = place_of(shared);
+    const typename A::Lane at_a(row0());
+    const typename B::Lane at_b(col0());
+    uint4 a[2][F], b[2][F];
+    auto stage_of = [&](int s) { return base + s % STAGES * STAGE; };
+    // Operand number n of 2 F, in the order of their first products.
+    auto operand = [&](uint32_t stage, int n, int h) {
+      if (n == 1 || n > F)
+        a[h][n == 1 ? 0 : n - F] = at_a.operand(stage, n == 1 ? 0 : n - F, h);
+      else
+        b[h][n == 0 ? 0 : n - 1] = at_b.operand(stage + HALF, n == 0 ? 0 : n - 1, h);
+    };
+    // Stage s is in shared memory for every wave, those before it are read.
+    // One and a half steps' loads may be still on their way.
+    auto hand_over = [&] {
+      if constexpr (DIRECT)
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "i"(3 * N) : "memory");
+      else
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+    };
     if (count <= 0) return;
-    const Place first = place_of(shared), second = first + STAGE;
-    const int a0 = row0(), b0 = col0();
-    load(first, 0);
-    store(first);
-    auto hand_over = [] {   // what the next step reads is in shared memory, for every wave
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-    };
-    auto step = [&](int s, Place stage, Place next) {
-      const bool more = s + 1 < count;
-      if (more) load(next, s + 1);
-      // the next operands are read while the matrix cores work on these
-      uint4 a[2][FM], b[2][FN];
-      auto operands = [&](int h) {
+    for (int s = 0; s < AHEAD; ++s) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) b[h & 1][j] = B::operand(stage.at + BM * kStepBytes, b0 + j * 32, h);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) a[h & 1][i] = A::operand(stage.at, a0 + i * 32, h);
-      };
-      operands(0);
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        if (h < 3) operands(h + 1);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-          for (int j = 0; j < FN; ++j) sum[i][j] = M::add(b[h & 1][j], a[h & 1][i], sum[i][j]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (more) store(next);
-      hand_over();
-    };
-    hand_over();
-    int s = 0;
-    for (; s + 1 < count; s += 2) {
-      step(s, first, second);
-      step(s + 1, second, first);
+      for (int i = 0; i < 2 * N; ++i) load(i, stage_of(s), s, std::false_type{});
+      if (!DIRECT && s == 0) store(stage_of(0));
     }
-    if (s < count) step(s, first, second);
+    hand_over();
+#pragma unroll
+    for (int i = 0; i < 2 * F; ++i) operand(base.address, i, 0);
+    auto step = [&](int s, auto quickly) {
+      const Place stage = stage_of(s), next = stage_of(s + 1), far = stage_of(s + 3);
+      if constexpr (!DIRECT) {
+        store(next);
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i) load(i, next, s + 2, quickly);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h == 1) hand_over();
+#pragma unroll
+        for (int t = 0; t < F * F; ++t) {
+          sum[t / F][t % F] = M::add(b[h][t % F], a[h][t / F], sum[t / F][t % F]);
+          __builtin_amdgcn_sched_barrier(0);
+          // between two products: an operand of the next half step or a load
+#pragma unroll
+          for (int n = t * 2 * F / (F * F); n < (t + 1) * 2 * F / (F * F); ++n) operand(h == 0 ? stage.address : next.address, n, 1 - h);
+          if constexpr (DIRECT)
+#pragma unroll
+            for (int n = (h * F * F + t) * N / (F * F); n < (h * F * F + t + 1) * N / (F * F); ++n) load(n, far, s + 3, quickly);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    // one loop after the other: a choice inside would cost copies of the sums
+    int s = 0;
+    if constexpr (DIRECT)
+      for (; s < count && quick(s + 3); ++s) step(s, std::true_type{});
+    for (; s < count; ++s) step(s, std::false_type{});
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
   }
 
   // Writes rows 0 .. rows-1 and columns 0 .. cols-1 of the tile to `out`,
   // through shared memory, so that rows leave as whole lines.  value(i, j, r):
   // what comes of the sums; JN fragments of 32 columns a wave, at col(j).
-  template <int COLS, int JN, class O, class C, class F>
-  static __device__ __forceinline__ void write(char* shared, O* out, int64_t ld, int rows, int cols, C&& col, F&& value) {
+  template <int COLS, int JN, class O, class C, class V_>
+  static __device__ __forceinline__ void write(char* shared, O* out, int64_t ld, int rows, int cols, C&& col, V_&& value) {
     constexpr int V = 16 / sizeof(O), PITCH = COLS + V;
     constexpr int FIT = LDS / (PITCH * (int)sizeof(O));
-    constexpr int ROWS = FIT >= BM ? BM : FIT >= BM / 2 ? BM / 2 : BM / 4;   // of a pass
+    constexpr int ROWS = FIT >= SIZE ? SIZE : FIT >= SIZE / 2 ? SIZE / 2 : SIZE / 4;   // of a pass
     static_assert(ROWS % 32 == 0 && ROWS <= FIT, "");
     const int lane = threadIdx.x & 63;
     O* tile = reinterpret_cast<O*>(shared);
     const bool wide = ld % V == 0 && cols % V == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
-    for (int first = 0; first < BM; first += ROWS) {
+    for (int first = 0; first < SIZE; first += ROWS) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
+      for (int i = 0; i < F; ++i) {
         const int m = row0() + i * 32 - first;
         if (m < 0 || m >= ROWS) continue;   // the same for a wave
 #pragma unroll
@@ -343,11 +430,21 @@ inline int64_t most_rows_tiles(int64_t experts, int64_t slots, int64_t size, boo
 }
 
 // Workgroups go to the 8 dies in turn: tiles are numbered so that 32
-// consecutive ones, which share rows and columns, meet in one die's cache.
-constexpr int kDies = 8, kNear = 32;
+// consecutive ones meet in one die's cache, and are 8 tiles of rows by 4 of
+// columns, which read the least between them.
+constexpr int kDies = 8, kNear = 32, kBand = 8;
 __device__ __forceinline__ int64_t tile_of_group(uint32_t group) {
   const uint32_t die = group % kDies, nth = group / kDies;
   return ((int64_t)(nth / kNear) * kDies + die) * kNear + nth % kNear;
+}
+// Where tile number `tile` lies among row_tiles x col_tiles.
+struct At {
+  int row, col;
+};
+__device__ __forceinline__ At at_of_tile(int64_t tile, int row_tiles, int col_tiles) {
+  const int band = (int)(tile / ((int64_t)kBand * col_tiles)) * kBand, rows = min(kBand, row_tiles - band);
+  const int in = (int)(tile - (int64_t)band * col_tiles);
+  return {band + in % rows, in / rows};
 }
 constexpr int64_t kMaxGroups = 1 << 22;   // of a launch: at most 2^31 threads, whole rounds of dies
 
