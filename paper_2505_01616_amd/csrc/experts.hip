@@ -29,7 +29,7 @@ struct Products {
   const int32_t* offsets;   // NULL: one expert has all slots
   const T* w[2];
   int64_t tiles, first;     // all tiles, and where a launch begins
-  int tiles_n;
+  int tiles_n, matrices;
   bool near_x, near_w;      // x, an expert's matrix: fewer than 2^32 bytes
 };
 
@@ -304,9 +304,12 @@ __global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int cols, int
 }
 
 // The weights' gradients: dW[e][n][c] = the sum over e's slots of d[s][n]
-// x[row(s)][c].  Both factors have the summed index as their slow one.
-// blockIdx.z: the matrix.
-template <class T, int SIZE, bool DIRECT>
+// x[row(s)][c].  Both factors have the summed index as their slow one.  Tiles are
+// numbered by matrix, part and place; MAPPED: slots have rows from a list, whose
+// places in x wait in shared memory, looked_of(SIZE) slots' at a time.
+constexpr int looked_of(int size) { return size == 256 ? 6144 : 2048; }
+constexpr uint32_t kNoRow = ~0u;
+template <class T, int SIZE, bool DIRECT, bool MAPPED>
 __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Products<T> p, Sums g, Cut cut, const Item* __restrict__ items,
                                                               const T* __restrict__ d0, const T* __restrict__ d1,
                                                               int64_t ld_d, T* __restrict__ dw0, T* __restrict__ dw1,
@@ -315,83 +318,86 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Produc
   using A = ColTile<T, SIZE, M::THREADS, DIRECT>;
   using B = A;
   extern __shared__ __align__(16) char shared[];
-  const int tiles_n = (g.n + SIZE - 1) / SIZE;
-  const int n0 = (int)(blockIdx.x % tiles_n) * SIZE, c0 = (int)(blockIdx.x / tiles_n) * SIZE;
+  constexpr int LOOKED = looked_of(SIZE);
+  uint32_t* looked = reinterpret_cast<uint32_t*>(shared + M::LDS);
+  const int64_t tile = p.first + tile_of_group(blockIdx.x);
+  if (tile >= p.tiles) return;
+  const int tiles_n = (g.n + SIZE - 1) / SIZE, tiles_c = (g.cols + SIZE - 1) / SIZE, tiles = tiles_n * tiles_c;
+  const int64_t of_matrix = p.tiles / p.matrices;
+  const bool second = tile >= of_matrix;
+  const int part = (int)((tile - (second ? of_matrix : 0)) / tiles);
+  const At at = at_of_tile((tile - (second ? of_matrix : 0)) - (int64_t)part * tiles, tiles_n, tiles_c);
+  const int n0 = at.row * SIZE, c0 = at.col * SIZE;
   Item it;
   if (cut.plan == Cut::WHOLE)
-    it = segment(p.offsets, blockIdx.y, g.slots);
+    it = segment(p.offsets, part, g.slots);
   else if (cut.plan == Cut::LISTED)
-    it = items[blockIdx.y];
+    it = items[part];
   else
-    find_part<false>(g, cut, p.offsets, blockIdx.y, &it, nullptr);
+    find_part<false>(g, cut, p.offsets, part, &it, nullptr);
   if (it.expert < 0) return;
   if (p.rows == 0) it.to = it.from;
 
   M m;
   A a;
   B b;
-  a.open((blockIdx.z ? d1 : d0) + (int64_t)it.from * ld_d, (it.to - it.from) * ld_d < (int64_t)1 << 31, ld_d, n0, g.n);
-  b.open(p.x, p.near_x, p.ld, c0, g.cols);
-  // A slot without a row takes no part, whatever its d holds.  The numbers of
-  // the rows that a wave brings in together are the same for its lanes, so they
-  // come by scalar loads, a step before their turn.
-  const uint32_t rows = (uint32_t)min(p.rows, (int64_t)0x7fffffff);
-  const auto* map = (const __attribute__((address_space(4))) int32_t*)p.map;
-  const int slots = it.to - it.from;
-  int row[A::N][A::ROWS];
-  auto look = [&](int i, int s) {
-    const int first = it.from + s * A::STEP + A::row(i);
-#pragma unroll
-    for (int j = 0; j < A::ROWS; ++j) row[i][j] = p.map ? map[min(first + j, it.to - 1)] : first + j;
-  };
-  if (slots > 0)
-#pragma unroll
-    for (int i = 0; i < A::N; ++i) look(i, 0);
-  m.template run<A, B>(
-      shared, (slots + A::STEP - 1) / A::STEP,
-      [&](int s) {
-        bool all = a.near & b.near & ((s + 1) * A::STEP <= slots);
-#pragma unroll
-        for (int i = 0; i < A::N; ++i)
-#pragma unroll
-          for (int j = 0; j < A::ROWS; ++j) all &= (uint32_t)row[i][j] < rows;
-        return all;
-      },
-      [&](int n, Place stage, int s, auto quick) {
-        const int i = n % A::N, first = s * A::STEP + A::row(i);
-        if constexpr (decltype(quick)::value) {
-          if (n < A::N) {
-            a.load_run(i, stage, first);
+  const T* d = second ? d1 : d0;
+  for (int from = it.from; from < it.to; from += LOOKED) {
+    const int slots = min(it.to - from, LOOKED);
+    // A slot without a row takes no part, whatever its d holds.
+    bool none = false;
+    if constexpr (MAPPED) {
+      __syncthreads();
+      for (int t = threadIdx.x; t < slots; t += M::THREADS) {
+        const int64_t r = row_of(p, from + t);
+        none |= r < 0;
+        looked[t] = r < 0 ? kNoRow : (uint32_t)(p.near_x ? r * p.ld * 2 : r);
+      }
+      none = __syncthreads_or(none);
+    }
+    a.open(d + (int64_t)from * ld_d, slots * ld_d < (int64_t)1 << 31, ld_d, n0, g.n);
+    b.open(MAPPED ? p.x : p.x + (int64_t)from * p.ld, MAPPED ? p.near_x : slots * p.ld < (int64_t)1 << 31, p.ld, c0, g.cols);
+    const bool all_near = a.near & b.near & !none;
+    uint32_t place[A::N];
+    m.template run<A, B>(
+        shared, (slots + A::STEP - 1) / A::STEP, [&](int s) { return all_near & ((s + 1) * A::STEP <= slots); },
+        [&](int n, Place stage, int s, auto quick) {
+          const int i = n % A::N, first = s * A::STEP + A::row(i), slot = first + A::mine();
+          if constexpr (decltype(quick)::value) {
+            if (n < A::N) {
+              a.load_run(i, stage, first);
+              if constexpr (MAPPED) place[i] = looked[slot];   // for the second half of the step
+            } else if constexpr (MAPPED) {
+              b.load_at(i, stage + M::HALF, place[i]);
+            } else {
+              b.load_run(i, stage + M::HALF, first);
+            }
           } else {
-            b.load_rows(i, stage + M::HALF, row[i]);
-            look(i, s + 1);
+            int r = slot < slots ? slot : -1;
+            if constexpr (MAPPED)
+              if (r >= 0) {
+                const uint32_t at = looked[slot];
+                r = at == kNoRow ? -1 : n < A::N ? slot : p.near_x ? (int)(at / (uint32_t)(p.ld * 2)) : (int)at;
+              }
+            if (n < A::N)
+              a.load(i, stage, r);
+            else
+              b.load(i, stage + M::HALF, r);
           }
-        } else {
-          const int slot = first + A::mine();
-          int r = row[i][0];
-#pragma unroll
-          for (int j = 1; j < A::ROWS; ++j) r = j == A::mine() ? row[i][j] : r;
-          const bool held = (slot < slots) & ((uint32_t)r < rows);
-          if (n < A::N) {
-            a.load(i, stage, held ? slot : -1);
-          } else {
-            b.load(i, stage + M::HALF, held ? r : -1);
-            look(i, s + 1);
-          }
-        }
-      },
-      [&](Place stage) {
-        a.store(stage);
-        b.store(stage + M::HALF);
-      });
+        },
+        [&](Place stage) {
+          a.store(stage);
+          b.store(stage + M::HALF);
+        });
+  }
   auto col = [&](int j) { return M::col0() + j * 32; };
   auto value = [&](int i, int j, int r) { return m.sum[i][j][r]; };
-  const int64_t size = (int64_t)g.n * g.cols, at = (int64_t)n0 * g.cols + c0;
+  const int64_t size = (int64_t)g.n * g.cols, to = (int64_t)n0 * g.cols + c0;
   if (it.partial < 0)
-    M::template write<SIZE, M::F>(shared, (blockIdx.z ? dw1 : dw0) + it.expert * size + at, g.cols, g.n - n0, g.cols - c0, col, value);
+    M::template write<SIZE, M::F>(shared, (second ? dw1 : dw0) + it.expert * size + to, g.cols, g.n - n0, g.cols - c0, col, value);
   else
-    M::template write<SIZE, M::F>(shared, partials + (blockIdx.z * cut.partials + it.partial) * size + at, g.cols, g.n - n0,
-                                 g.cols - c0, col, value);
+    M::template write<SIZE, M::F>(shared, partials + ((second ? cut.partials : 0) + it.partial) * size + to, g.cols, g.n - n0,
+                                  g.cols - c0, col, value);
 }
 
 // Calls f with the tile's shape for `size` (256 or 128).  Rows that are no
@@ -441,7 +447,7 @@ struct Call {
   template <class T>
   Products<T> products() const {
     return Products<T>{experts, (int)slots, n, k, rows, ld, static_cast<const T*>(x), map, offsets,
-                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0, 0,
+                       {static_cast<const T*>(w[0]), static_cast<const T*>(w[1])}, 0, 0, 0, matrices,
                        rows <= ((int64_t)1 << 31) / ld, (int64_t)n * k <= (int64_t)1 << 31};
   }
   // Whether x's rows, and the weights', are whole chunks of 16 bytes.
@@ -529,14 +535,15 @@ struct Space {
   }
 };
 
-// How the weights' sums are cut (parts.h): into parts as long as each of the
-// 256 compute units would have slots of one tile if all were busy to the end.
+// How the weights' sums are cut (parts.h): a die's 32 compute units work on 32
+// tiles of a part together, and the dies get their parts in turn, so parts are a
+// quarter as long as what each would have if all were busy to the end.
 Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t k, int matrices) {
   Cut c{};
   c.tile = tile_of(slots, experts, n, k);
   c.step = 64;
   const int64_t tiles = matrices * ceil_div(n, c.tile) * ceil_div(k, c.tile);
-  c.longest = ceil_div(slots * tiles, 256);
+  c.longest = ceil_div(slots * tiles, 256 * 4);
   if (c.longest < 256) c.longest = 256;
   if (c.longest > kMaxSlots) c.longest = kMaxSlots;
   c.plan = slots <= 512 ? Cut::WHOLE : experts * tiles <= 64 && experts <= 16 ? Cut::BY_WAVE : Cut::LISTED;
@@ -597,11 +604,16 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
         float* partials = reinterpret_cast<float*>(work + space.partials);
         if (cut.plan == Cut::LISTED)
           hipLaunchKernelGGL(plan_kernel, dim3(1), dim3((unsigned)ceil_div(c.experts, 64) * 64), 0, s, g, cut, c.offsets, items, joins);
-        go(weight_kernel<T, S::SIZE, S::DIRECT>,
-           dim3((unsigned)(ceil_div(c.n, S::SIZE) * ceil_div(c.k, S::SIZE)), (unsigned)(cut.plan == Cut::WHOLE ? c.experts : cut.items),
-                c.matrices),
-           S::M::THREADS, S::M::LDS, s, c.products<T>(), g, cut, items, static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
-           static_cast<T*>(dw0), static_cast<T*>(dw1), partials);
+        auto p = c.products<T>();
+        p.tiles = c.matrices * (cut.plan == Cut::WHOLE ? c.experts : cut.items) * ceil_div(c.n, S::SIZE) * ceil_div(c.k, S::SIZE);
+        with_bool(c.map != nullptr, [&](auto mapped) {
+          over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
+            p.first = first;
+            go(weight_kernel<T, S::SIZE, S::DIRECT, decltype(mapped)::value>, dim3(groups), S::M::THREADS,
+               S::M::LDS + (decltype(mapped)::value ? 4 * looked_of(S::SIZE) : 0), s, p, g, cut, items, static_cast<const T*>(d0),
+               static_cast<const T*>(d1), ld_d, static_cast<T*>(dw0), static_cast<T*>(dw1), partials);
+          });
+        });
         if (cut.joins > 0)
           for (int i = 0; i < c.matrices; ++i)
             hipLaunchKernelGGL(join_kernel<T>, dim3(256, (unsigned)cut.joins), dim3(256), 0, s, g, cut, c.offsets, joins,

@@ -206,12 +206,9 @@ struct ColTile {
   __device__ __forceinline__ void load_run(int i, Place stage, int first, int64_t shift = 0) {
     to_shared(base + shift + (uint64_t)(uint32_t)first * ld, own, place(i, stage));
   }
-  // or the rows r, the same for the wave.
-  __device__ __forceinline__ void load_rows(int i, Place stage, const int (&r)[ROWS], int64_t shift = 0) {
-    uint32_t from = (uint32_t)r[0] * ld;
-#pragma unroll
-    for (int j = 1; j < ROWS; ++j) from = mine() == j ? (uint32_t)r[j] * ld : from;
-    to_shared(base + shift, (from + col) * 2, place(i, stage));
+  // or a row of each lane's that starts `from` bytes behind the array.
+  __device__ __forceinline__ void load_at(int i, Place stage, uint32_t from, int64_t shift = 0) {
+    to_shared(base + shift, from + col * 2, place(i, stage));
   }
   __device__ __forceinline__ void store(Place stage) {
     if constexpr (!DIRECT)
@@ -242,7 +239,9 @@ struct ColTile {
 template <class T, int SIZE>
 struct Tile {
   static constexpr int THREADS = 256, F = SIZE / 64, STAGES = 4;
-  static constexpr int HALF = SIZE * kStepBytes, STAGE = 2 * HALF, LDS = STAGES * STAGE;
+  static constexpr int HALF = SIZE * kStepBytes, STAGE = 2 * HALF;
+  // the stages, or a tile of 16-bit values with rows of 16 bytes more
+  static constexpr int RING = STAGES * STAGE, ROOM = SIZE * (SIZE + 8) * 2 > RING ? SIZE * (SIZE + 8) * 2 : RING, LDS = ROOM;
   using M = Matrix<T>;
   typename M::Sum sum[F][F];
 
@@ -327,23 +326,22 @@ struct Tile {
 
   // Writes rows 0 .. rows-1 and columns 0 .. cols-1 of the tile to `out`,
   // through shared memory, so that rows leave as whole lines.  value(i, j, r):
-  // what comes of the sums; JN fragments of 32 columns a wave, at col(j).
+  // what comes of the sums; JN fragments of 32 columns a wave, at col(j).  A pass
+  // takes as many fragments of every wave as fit.
   template <int COLS, int JN, class O, class C, class V_>
   static __device__ __forceinline__ void write(char* shared, O* out, int64_t ld, int rows, int cols, C&& col, V_&& value) {
     constexpr int V = 16 / sizeof(O), PITCH = COLS + V;
-    constexpr int FIT = LDS / (PITCH * (int)sizeof(O));
-    constexpr int ROWS = FIT >= SIZE ? SIZE : FIT >= SIZE / 2 ? SIZE / 2 : SIZE / 4;   // of a pass
-    static_assert(ROWS % 32 == 0 && ROWS <= FIT, "");
-    const int lane = threadIdx.x & 63;
+    constexpr int FIT = ROOM / (PITCH * (int)sizeof(O)) / 64;
+    constexpr int EACH = FIT >= F ? F : FIT >= F / 2 ? F / 2 : 1;   // fragments of rows of a pass
+    static_assert(EACH <= FIT && F % EACH == 0, "");
+    const int lane = threadIdx.x & 63, half = wave_of_group() / 2;
     O* tile = reinterpret_cast<O*>(shared);
     const bool wide = ld % V == 0 && cols % V == 0 && reinterpret_cast<uintptr_t>(out) % 16 == 0;
 #pragma unroll
-    for (int first = 0; first < SIZE; first += ROWS) {
+    for (int first = 0; first < F; first += EACH) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < F; ++i) {
-        const int m = row0() + i * 32 - first;
-        if (m < 0 || m >= ROWS) continue;   // the same for a wave
+      for (int i = first; i < first + EACH; ++i)
 #pragma unroll
         for (int j = 0; j < JN; ++j)
 #pragma unroll
@@ -353,22 +351,23 @@ struct Tile {
             } four;
 #pragma unroll
             for (int h = 0; h < 4; ++h) four.v[h] = (O)value(i, j, r + h);
-            *reinterpret_cast<Four*>(tile + (m + (lane & 31)) * PITCH + col(j) + r * 2 + (lane >> 5) * 4) = four;
+            *reinterpret_cast<Four*>(tile + ((half * EACH + i - first) * 32 + (lane & 31)) * PITCH + col(j) + r * 2 + (lane >> 5) * 4) = four;
           }
-      }
       __syncthreads();
+      // row m of the pass is row place(m) of the tile
+      auto place = [&](int m) { return m / (EACH * 32) * (SIZE / 2) + first * 32 + m % (EACH * 32); };
       if (wide) {
 #pragma unroll 4
-        for (int t = threadIdx.x; t < ROWS * COLS / V; t += THREADS) {
-          const int m = t / (COLS / V), c = t % (COLS / V) * V;
-          if (first + m < rows && c < cols)
-            *reinterpret_cast<uint4*>(out + (first + m) * ld + c) = *reinterpret_cast<const uint4*>(tile + m * PITCH + c);
+        for (int t = threadIdx.x; t < EACH * 64 * COLS / V; t += THREADS) {
+          const int m = t / (COLS / V), c = t % (COLS / V) * V, at = place(m);
+          if (at < rows && c < cols)
+            *reinterpret_cast<uint4*>(out + at * ld + c) = *reinterpret_cast<const uint4*>(tile + m * PITCH + c);
         }
       } else {
 #pragma unroll 4
-        for (int t = threadIdx.x; t < ROWS * COLS; t += THREADS) {
-          const int m = t / COLS, c = t % COLS;
-          if (first + m < rows && c < cols) out[(first + m) * ld + c] = tile[m * PITCH + c];
+        for (int t = threadIdx.x; t < EACH * 64 * COLS; t += THREADS) {
+          const int m = t / COLS, c = t % COLS, at = place(m);
+          if (at < rows && c < cols) out[at * ld + c] = tile[m * PITCH + c];
         }
       }
     }
