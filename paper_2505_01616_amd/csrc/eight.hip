@@ -116,14 +116,14 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void eight_kernel(Eights 
     m.template run<A, B>(
         shared, (p.pitch + A::STEP - 1) / A::STEP,
         [&](int s) { return a.quick(s * A::STEP, p.pitch) & b.near; },
-        [&](int n, Place stage, int s, auto quick) {
+        [&](int n, auto to, int s, auto quick) {
           constexpr bool QUICK = decltype(quick)::value;
           if (n < A::N)
-            a.template load<QUICK>(n, stage, s * A::STEP, p.pitch);
+            a.template load<QUICK>(n, to.stage, 0, s * A::STEP, p.pitch);
           else
-            b.template load<QUICK>(n - A::N, stage + M::HALF, s * A::STEP, p.pitch);
+            b.template load<QUICK>(n - A::N, to.stage + M::HALF, 0, s * A::STEP, p.pitch);
         },
-        [](Place) {});
+        [](auto) {});
   }
   float x_scale[M::F], w_scale[M::F][16];
   bool held[M::F];
@@ -233,15 +233,16 @@ extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts
                    rows * padded(cols) <= (int64_t)1 << 32, n * padded(cols) <= (int64_t)1 << 32};
           p.tiles_n = (int)ceil_div(n, bn);
           p.tiles = p.tiles_n * most_rows_tiles(experts, slots, bm, d_offsets);
-          (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+          allow_shared((const void*)kernel, lds);
           over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
             p.first = first;
             hipLaunchKernelGGL(kernel, dim3(groups), dim3(threads), lds, static_cast<hipStream_t>(hip_stream), p, static_cast<O*>(d_y), ld_y);
           });
         };
-        if (slots <= 24 * (int64_t)experts)
+        const Kernel which = kernel_for(slots, experts, n, 2 * kFewCols, 128);
+        if (which == FEW)
           run(few_eight_kernel<O>, kFewRows, 2 * kFewCols, kFewThreads, kFewShared);
-        else if (slots / experts >= 256)
+        else if (which == TILE_256)
           run(eight_kernel<O, 256>, 256, 256, 256, Tile<int8_t, 256>::LDS);
         else
           run(eight_kernel<O, 128>, 128, 128, 256, Tile<int8_t, 128>::LDS);

@@ -128,16 +128,16 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products
     m.template run<A, B>(
         shared, (p.k + A::STEP - 1) / A::STEP,
         [&](int s) { return a.quick(s * A::STEP, p.k) & b.near; },
-        [&](int n, Place stage, int s, auto quick) {
+        [&](int n, auto to, int s, auto quick) {
           constexpr bool QUICK = decltype(quick)::value;
           if (n < A::N)
-            a.template load<QUICK>(n, stage, s * A::STEP, p.k);
+            a.template load<QUICK>(n, to.stage, to.set, s * A::STEP, p.k);
           else
-            b.template load<QUICK>(n - A::N, stage + M::HALF, s * A::STEP, p.k, OUT != PRODUCT && of_u(n - A::N) ? shift : 0);
+            b.template load<QUICK>(n - A::N, to.stage + M::HALF, to.set, s * A::STEP, p.k, OUT != PRODUCT && of_u(n - A::N) ? shift : 0);
         },
-        [&](Place stage) {
-          a.store(stage);
-          b.store(stage + M::HALF);
+        [&](auto to) {
+          a.store(to.stage, to.set);
+          b.store(to.stage + M::HALF, to.set);
         });
   }
   auto col = [&](int j) { return M::col0() / (M::F / JN) + j * 32; };
@@ -258,23 +258,23 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void input_kernel(Product
     m.template run<A, B>(
         shared, steps * pairs,
         [&](int s) { return a.quick((s >= steps ? s - steps : s) * A::STEP, p.n) & b.near & (s < steps * pairs); },
-        [&](int n, Place stage, int s, auto quick) {
+        [&](int n, auto to, int s, auto quick) {
           constexpr bool QUICK = decltype(quick)::value;
           const bool second = s >= steps && pairs == 2;
           const int k0 = (second ? s - steps : s) * A::STEP;
           const int64_t shift = second ? p.w[1] - p.w[0] : 0;
           if (n < A::N) {
-            a.template load<QUICK>(n, stage, k0, p.n, second ? d1 - d0 : 0);
+            a.template load<QUICK>(n, to.stage, to.set, k0, p.n, second ? d1 - d0 : 0);
           } else if constexpr (QUICK) {
-            b.load_run(n - A::N, stage + M::HALF, k0 + B::row(n - A::N), shift);
+            b.load_run(n - A::N, to.stage + M::HALF, to.set, k0 + B::row(n - A::N), shift);
           } else {
             const int k = k0 + B::row(n - A::N) + B::mine();
-            b.load(n - A::N, stage + M::HALF, k < p.n ? k : -1, shift);
+            b.load(n - A::N, to.stage + M::HALF, to.set, k < p.n ? k : -1, shift);
           }
         },
-        [&](Place stage) {
-          a.store(stage);
-          b.store(stage + M::HALF);
+        [&](auto to) {
+          a.store(to.stage, to.set);
+          b.store(to.stage + M::HALF, to.set);
         });
   }
   M::template write<SIZE, M::F>(shared, dx + (int64_t)rows.from * p.k + c0, p.k, count, p.k - c0,
@@ -348,10 +348,17 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Produc
     bool none = false;
     if constexpr (MAPPED) {
       __syncthreads();
-      for (int t = threadIdx.x; t < slots; t += M::THREADS) {
-        const int64_t r = row_of(p, from + t);
-        none |= r < 0;
-        looked[t] = r < 0 ? kNoRow : (uint32_t)(p.near_x ? r * p.ld * 2 : r);
+      const uint32_t rows = (uint32_t)min(p.rows, (int64_t)0x7fffffff), pitch = p.near_x ? (uint32_t)p.ld * 2 : 1;
+      for (int t0 = threadIdx.x; t0 < slots; t0 += 8 * M::THREADS) {
+        int r[8];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) r[h] = p.map[from + min(t0 + h * (int)M::THREADS, slots - 1)];
+#pragma unroll
+        for (int h = 0; h < 8; ++h) {
+          const bool has = (uint32_t)r[h] < rows;
+          none |= !has;
+          if (t0 + h * (int)M::THREADS < slots) looked[t0 + h * M::THREADS] = has ? (uint32_t)r[h] * pitch : kNoRow;
+        }
       }
       none = __syncthreads_or(none);
     }
@@ -361,16 +368,16 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Produc
     uint32_t place[A::N];
     m.template run<A, B>(
         shared, (slots + A::STEP - 1) / A::STEP, [&](int s) { return all_near & ((s + 1) * A::STEP <= slots); },
-        [&](int n, Place stage, int s, auto quick) {
+        [&](int n, auto to, int s, auto quick) {
           const int i = n % A::N, first = s * A::STEP + A::row(i), slot = first + A::mine();
           if constexpr (decltype(quick)::value) {
             if (n < A::N) {
-              a.load_run(i, stage, first);
+              a.load_run(i, to.stage, to.set, first);
               if constexpr (MAPPED) place[i] = looked[slot];   // for the second half of the step
             } else if constexpr (MAPPED) {
-              b.load_at(i, stage + M::HALF, place[i]);
+              b.load_at(i, to.stage + M::HALF, to.set, place[i]);
             } else {
-              b.load_run(i, stage + M::HALF, first);
+              b.load_run(i, to.stage + M::HALF, to.set, first);
             }
           } else {
             int r = slot < slots ? slot : -1;
@@ -380,14 +387,14 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Produc
                 r = at == kNoRow ? -1 : n < A::N ? slot : p.near_x ? (int)(at / (uint32_t)(p.ld * 2)) : (int)at;
               }
             if (n < A::N)
-              a.load(i, stage, r);
+              a.load(i, to.stage, to.set, r);
             else
-              b.load(i, stage + M::HALF, r);
+              b.load(i, to.stage + M::HALF, to.set, r);
           }
         },
-        [&](Place stage) {
-          a.store(stage);
-          b.store(stage + M::HALF);
+        [&](auto to) {
+          a.store(to.stage, to.set);
+          b.store(to.stage + M::HALF, to.set);
         });
   }
   auto col = [&](int j) { return M::col0() + j * 32; };
@@ -474,29 +481,20 @@ netsim_status check(const char* what, const Call& c) {
   return NETSIM_OK;
 }
 
-int tile_of(int64_t slots, int64_t experts, int64_t n, int64_t k) {
-  (void)n;
-  (void)k;
-  return slots / experts >= 256 ? 256 : 128;
-}
-
 template <class K, class... Args>
 void go(K kernel, dim3 grid, int threads, int lds, hipStream_t s, Args... args) {
-  (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  allow_shared((const void*)kernel, lds);
   hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, s, args...);
 }
-
-// Whether an expert has few rows: few_kernel reads the weights faster, tiles
-// read the rows less often.
-bool few(int64_t slots, int64_t experts) { return slots <= 24 * experts; }
 
 // Rows by slot (rows_kernel, few_kernel).
 template <int OUT>
 void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, void* out, void* out2, int64_t ld_out, hipStream_t s) {
   with_16_bits(c.type, [&](auto t) {
     using T = decltype(t);
+    const Kernel kernel = kernel_for(c.slots, c.experts, c.n, OUT == PRODUCT ? 2 * kFewCols : kFewCols, OUT == PRODUCT ? 128 : 64);
     if constexpr (OUT != GATED_BACK)
-      if (few(c.slots, c.experts)) {
+      if (kernel == FEW) {
         auto p = c.products<T>();
         p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? 2 * kFewCols : kFewCols);
         p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, kFewRows, c.offsets);
@@ -509,7 +507,7 @@ void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, 
         });
         return;
       }
-    with_tile<T>(tile_of(c.slots, c.experts, c.n, c.k), c.x_direct() && c.w_direct(), [&](auto shape) {
+    with_tile<T>(kernel == TILE_256 ? 256 : 128, c.x_direct() && c.w_direct(), [&](auto shape) {
       using S = decltype(shape);
       auto p = c.products<T>();
       p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? S::SIZE : S::SIZE / 2);
@@ -540,7 +538,9 @@ struct Space {
 // quarter as long as what each would have if all were busy to the end.
 Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t k, int matrices) {
   Cut c{};
-  c.tile = tile_of(slots, experts, n, k);
+  // as for the sums of saved rows: tiles of 256 from 3,000 slots for each
+  // compute unit on
+  c.tile = slots * matrices * ceil_div(n, 256) * ceil_div(k, 256) / 256 >= 3000 ? 256 : 128;
   c.step = 64;
   const int64_t tiles = matrices * ceil_div(n, c.tile) * ceil_div(k, c.tile);
   c.longest = ceil_div(slots * tiles, 256 * 4);
@@ -573,7 +573,7 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
   with_16_bits(c.type, [&](auto t) {
     using T = decltype(t);
     if (dx && c.slots > 0)
-      with_tile<T>(tile_of(c.slots, c.experts, c.n, c.k), d_direct && c.w_direct(), [&](auto shape) {
+      with_tile<T>(kernel_for(c.slots, c.experts, c.k, 2 * kFewCols, 128) == TILE_256 ? 256 : 128, d_direct && c.w_direct(), [&](auto shape) {
         with_bool(c.map != nullptr, [&](auto mapped) {
           using S = decltype(shape);
           using O = std::conditional_t<decltype(mapped)::value, float, T>;

@@ -73,6 +73,12 @@ netsim_status launch(const char* what, int32_t device, F&& go) {
   return e == hipSuccess ? NETSIM_OK : fail(NETSIM_E_DEVICE, what, hipGetErrorString(e));
 }
 
+// Lets a kernel have `bytes` of shared memory on the current device: up to 64
+// KiB it has them anyway.
+inline void allow_shared(const void* kernel, int bytes) {
+  if (bytes > 65536) (void)hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
 // A grid of 2^32 threads or more is cut short by the runtime, without an error:
 // work over `count` items goes in launches of at most `most`.
 template <class F>

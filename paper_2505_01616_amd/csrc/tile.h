@@ -84,6 +84,12 @@ __device__ __forceinline__ Place place_of(char* shared) {
   return {shared, (uint32_t)__builtin_amdgcn_readfirstlane(address)};
 }
 
+// 16 bytes at base + off, at any alignment of the elements.
+template <class T>
+__device__ __forceinline__ uint4 chunk_at(const T* base, uint32_t off) {
+  const Eight<T> v = load_eight(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + off));
+  return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+}
 // A chunk of 16 bytes of which `left` elements are there, zeros beyond.
 template <class T>
 __device__ __forceinline__ uint4 chunk_of(const T* p, int left) {
@@ -93,6 +99,7 @@ __device__ __forceinline__ uint4 chunk_of(const T* p, int left) {
 
 using u32x4 = __attribute__((ext_vector_type(4))) uint32_t;
 using lds_u32x4 = __attribute__((address_space(3))) const u32x4;
+constexpr int HELD = 3;   // steps' chunks that wait in registers where they pass through them
 
 // Rows of which a step takes 64 bytes each.  DIRECT: rows start at multiples
 // of 16 bytes and have whole chunks.
@@ -105,7 +112,7 @@ struct RowTile {
   int64_t at[N];      // of this thread's chunks, in elements from base on
   uint32_t off[N];    // the same in bytes, where that fits
   bool near;
-  uint4 held[DIRECT ? 1 : N];
+  uint4 held[DIRECT ? 1 : HELD][DIRECT ? 1 : N];
   int col;
 
   // Row r of the tile starts row(r) elements behind `from` and may be read;
@@ -128,21 +135,23 @@ struct RowTile {
   // This thread's chunk i of it, zeros beyond; shift: of another array of such
   // rows.
   template <bool QUICK>
-  __device__ __forceinline__ void load(int i, Place stage, int k0, int k, int64_t shift = 0) {
+  __device__ __forceinline__ void load(int i, Place stage, int set, int k0, int k, int64_t shift = 0) {
     const T* step = base + shift + k0;
     const uint32_t to = stage.address + i * THREADS * 16 + wave_of_group() * 1024;
     const int left = k - k0 - col;
-    if constexpr (!DIRECT)
-      held[i] = chunk_of(step + at[i], left);
+    if constexpr (!DIRECT && QUICK)
+      held[set][i] = chunk_at(step, off[i]);
+    else if constexpr (!DIRECT)
+      held[set][i] = chunk_of(step + at[i], left);
     else if constexpr (QUICK)
       to_shared(step, off[i], to);
     else
       to_shared(left > 0 ? static_cast<const void*>(step + at[i]) : &zeros, to);
   }
-  __device__ __forceinline__ void store(Place stage) {
+  __device__ __forceinline__ void store(Place stage, int set) {
     if constexpr (!DIRECT)
 #pragma unroll
-      for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = held[i];
+      for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = held[set][i];
   }
   // The operand of rows 32 i .. 32 i + 31 of a wave's part, bytes 32 h .. of the
   // step; lane_at: where a lane's part of it lies.
@@ -172,7 +181,7 @@ struct ColTile {
   uint32_t ld;       // pitches are below 2^31
   uint32_t col, own;
   bool near;
-  uint4 held[DIRECT ? 1 : N];
+  uint4 held[DIRECT ? 1 : HELD][DIRECT ? 1 : N];
   int left;
 
   // The first of the rows of a step that this wave brings in as chunk i.
@@ -189,31 +198,38 @@ struct ColTile {
     base = from + c0;
     col = c - c0;
     ld = (uint32_t)pitch;
-    near = all_near;
+    near = all_near && (DIRECT || c0 + R <= cols);
     own = (mine() * ld + col) * 2;
   }
   __device__ __forceinline__ uint32_t place(int i, Place stage) const { return stage.address + i * THREADS * 16 + wave_of_group() * 1024; }
   // Chunk i of a step: r, this lane's row; none: negative.
-  __device__ __forceinline__ void load(int i, Place stage, int r, int64_t shift = 0) {
+  __device__ __forceinline__ void load(int i, Place stage, int set, int r, int64_t shift = 0) {
     const T* from = base + shift + (uint64_t)(uint32_t)r * ld + col;
     if constexpr (!DIRECT)
-      held[i] = chunk_of(from, r >= 0 ? left : 0);
+      held[set][i] = chunk_of(from, r >= 0 ? left : 0);
     else
       to_shared(r >= 0 ? static_cast<const void*>(from) : &zeros, place(i, stage));
   }
   // The same quickly, where every lane has a row and they are near: consecutive
   // rows from `first` on,
-  __device__ __forceinline__ void load_run(int i, Place stage, int first, int64_t shift = 0) {
-    to_shared(base + shift + (uint64_t)(uint32_t)first * ld, own, place(i, stage));
+  __device__ __forceinline__ void load_run(int i, Place stage, int set, int first, int64_t shift = 0) {
+    const T* from = base + shift + (uint64_t)(uint32_t)first * ld;
+    if constexpr (DIRECT)
+      to_shared(from, own, place(i, stage));
+    else
+      held[set][i] = chunk_at(from, own);
   }
   // or a row of each lane's that starts `from` bytes behind the array.
-  __device__ __forceinline__ void load_at(int i, Place stage, uint32_t from, int64_t shift = 0) {
-    to_shared(base + shift, from + col * 2, place(i, stage));
+  __device__ __forceinline__ void load_at(int i, Place stage, int set, uint32_t from, int64_t shift = 0) {
+    if constexpr (DIRECT)
+      to_shared(base + shift, from + col * 2, place(i, stage));
+    else
+      held[set][i] = chunk_at(base + shift, from + col * 2);
   }
-  __device__ __forceinline__ void store(Place stage) {
+  __device__ __forceinline__ void store(Place stage, int set) {
     if constexpr (!DIRECT)
 #pragma unroll
-      for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = held[i];
+      for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = held[set][i];
   }
   // Lanes 0-15 give four rows of 16 columns and get a column each; lanes 16-31
   // the next 16 columns, lanes 32-63 the rows 8 further on.
@@ -254,15 +270,19 @@ struct Tile {
   static __device__ __forceinline__ int row0() { return wave_of_group() / 2 * (SIZE / 2); }
   static __device__ __forceinline__ int col0() { return wave_of_group() % 2 * (SIZE / 2); }
 
-  // `count` steps.  load(n, stage, s, quick) brings in this thread's chunk n of
+  // `count` steps.  load(n, to, s, quick) brings in this thread's chunk n of
   // step s, A's N and then B's (nothing but zeros from s = count on), quick(s)
-  // says whether it may go quickly; store(stage) what went to registers of it.  At
-  // the end no wave reads shared memory, and none writes it.
+  // says whether it may go quickly; store(to) what went to registers.  At the end
+  // no wave reads shared memory, and none writes it.
+  struct To {
+    Place stage;
+    int set;   // of the registers
+  };
   template <class A, class B, class Quick, class Load, class Store>
   __device__ __forceinline__ void run(char* shared, int count, Quick&& quick, Load&& load, Store&& store) {
     static_assert(A::N == B::N && A::DIRECT == B::DIRECT, "");
     constexpr bool DIRECT = A::DIRECT;
-    constexpr int N = A::N, AHEAD = DIRECT ? 3 : 2;
+    constexpr int N = A::N;
     const Place base = place_of(shared);
     const typename A::Lane at_a(row0());
     const typename B::Lane at_b(col0());
@@ -284,20 +304,26 @@ struct Tile {
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
     };
     if (count <= 0) return;
-    for (int s = 0; s < AHEAD; ++s) {
 #pragma unroll
-      for (int i = 0; i < 2 * N; ++i) load(i, stage_of(s), s, std::false_type{});
-      if (!DIRECT && s == 0) store(stage_of(0));
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+      for (int i = 0; i < 2 * N; ++i) load(i, To{stage_of(s), s}, s, std::false_type{});
+    if constexpr (!DIRECT) {
+      store(To{base, 0});
+#pragma unroll
+      for (int i = 0; i < 2 * N; ++i) load(i, To{base, 0}, 3, std::false_type{});
     }
     hand_over();
 #pragma unroll
     for (int i = 0; i < 2 * F; ++i) operand(base.address, i, 0);
-    auto step = [&](int s, auto quickly) {
+    // set: s % HELD.  What waits in registers: steps s + 1 to s + 3.
+    auto step = [&](int s, int set, auto quickly) {
       const Place stage = stage_of(s), next = stage_of(s + 1), far = stage_of(s + 3);
       if constexpr (!DIRECT) {
-        store(next);
+        const int one = (set + 1) % HELD;
+        store(To{next, one});
 #pragma unroll
-        for (int i = 0; i < 2 * N; ++i) load(i, next, s + 2, quickly);
+        for (int i = 0; i < 2 * N; ++i) load(i, To{next, one}, s + 4, quickly);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -311,16 +337,26 @@ struct Tile {
           for (int n = t * 2 * F / (F * F); n < (t + 1) * 2 * F / (F * F); ++n) operand(h == 0 ? stage.address : next.address, n, 1 - h);
           if constexpr (DIRECT)
 #pragma unroll
-            for (int n = (h * F * F + t) * N / (F * F); n < (h * F * F + t + 1) * N / (F * F); ++n) load(n, far, s + 3, quickly);
+            for (int n = (h * F * F + t) * N / (F * F); n < (h * F * F + t + 1) * N / (F * F); ++n) load(n, To{far, 0}, s + 3, quickly);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
     };
     // one loop after the other: a choice inside would cost copies of the sums
     int s = 0;
-    if constexpr (DIRECT)
-      for (; s < count && quick(s + 3); ++s) step(s, std::true_type{});
-    for (; s < count; ++s) step(s, std::false_type{});
+    if constexpr (DIRECT) {
+      for (; s < count && quick(s + 3); ++s) step(s, 0, std::true_type{});
+      for (; s < count; ++s) step(s, 0, std::false_type{});
+    } else {
+      for (; s + HELD <= count && quick(s + 4) && quick(s + 5) && quick(s + 6); s += HELD) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) step(s + i, i, std::true_type{});
+      }
+      for (; s < count; s += HELD) {   // steps from count on add nothing
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) step(s + i, i, std::false_type{});
+      }
+    }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
   }
 
@@ -364,10 +400,18 @@ struct Tile {
             *reinterpret_cast<uint4*>(out + at * ld + c) = *reinterpret_cast<const uint4*>(tile + m * PITCH + c);
         }
       } else {
+        // 16 bytes at any alignment of the elements
+        using Words = std::conditional_t<sizeof(O) == 2, words_at_2, words_at_4>;
 #pragma unroll 4
-        for (int t = threadIdx.x; t < EACH * 64 * COLS; t += THREADS) {
-          const int m = t / COLS, c = t % COLS, at = place(m);
-          if (at < rows && c < cols) out[at * ld + c] = tile[m * PITCH + c];
+        for (int t = threadIdx.x; t < EACH * 64 * COLS / V; t += THREADS) {
+          const int m = t / (COLS / V), c = t % (COLS / V) * V, at = place(m);
+          if (at >= rows || c >= cols) continue;
+          O* to = out + at * ld + c;
+          const O* from = tile + m * PITCH + c;
+          if (c + V <= cols)
+            *reinterpret_cast<Words*>(to) = *reinterpret_cast<const Words*>(from);
+          else
+            for (int h = 0; h < cols - c; ++h) to[h] = from[h];
         }
       }
     }
@@ -426,6 +470,30 @@ __device__ __forceinline__ Rows find_rows(const int32_t* offsets, int experts, i
 inline int64_t most_rows_tiles(int64_t experts, int64_t slots, int64_t size, bool offsets) {
   if (!offsets) return ceil_div(slots, size);
   return slots / size + (experts + 2 < slots ? experts + 2 : slots);
+}
+
+// Which kernel multiplies `slots` rows, spread over `experts`, by matrices of n
+// rows; cols: columns of the result that a workgroup for few rows and a tile of
+// 128 compute (one of 256: twice the latter).
+//
+// FEW (few.h): where its workgroups, weighed by what they read (weights count
+// twice, each 16 rows once), are few enough to run together.  Columns 2,048,
+// bfloat16, us, few rows' kernel and tiles of 128: one matrix of 2,048 rows, 16
+// rows of x 8.1 and 18.2, 256 15.9 and 20.8, 512 28 and 22; 8 matrices of 1,024 x
+// 4,096, 16 rows each 18.5 and 35, 64 34 and 36, 128 50 and 40; 64 matrices of
+// 1,024, a row each 46 and 42, 16 rows each 56 and 47.
+// Tiles of 256 instead of 128: where they keep most compute units busy and their
+// unused rows cost less than their better use of shared memory gains.  2,048
+// columns, a matrix of 2,048: 4,096 rows (128 tiles) 62 and 52, 8,192 rows 66
+// and 89, 16,384 rows 123 and 166.
+enum Kernel { FEW, TILE_128, TILE_256 };
+inline Kernel kernel_for(int64_t slots, int64_t experts, int64_t n, int few_cols, int tile_cols) {
+  const int64_t used = experts < slots ? experts : slots, each = ceil_div(slots, experts);   // rows of an expert, if all have as many
+  const int64_t sixteens = each >= 64 ? 4 : ceil_div(each, 16);
+  const int64_t groups = used * ceil_div(each, 64) * ceil_div(n, few_cols);
+  if (groups * (2 + sixteens) <= 300 * 6) return FEW;
+  const int64_t small = (2 * slots / 128 + used) * ceil_div(n, tile_cols), large = (2 * slots / 256 + used) * ceil_div(n, 2 * tile_cols);
+  return large >= 2 * 150 && 3 * large <= small ? TILE_256 : TILE_128;   // both counts are doubled
 }
 
 // Workgroups go to the 8 dies in turn: tiles are numbered so that 32

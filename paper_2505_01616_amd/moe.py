@@ -92,7 +92,7 @@ def _rows(name: str, t: torch.Tensor, types) -> int:
 
 
 def _flat(name: str, t: torch.Tensor, dtype, shape, device):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {device} is wanted")
 
 
