@@ -145,8 +145,8 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void eight_kernel(Eights 
 }
 
 // For few rows of each expert.
-template <class O>
-__global__ __launch_bounds__(kFewThreads) void few_eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
+template <class O, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
   constexpr int COLS = 2 * kFewCols;
   extern __shared__ __align__(16) char shared[];
   auto* sums = reinterpret_cast<i32x4*>(shared);
@@ -161,16 +161,16 @@ __global__ __launch_bounds__(kFewThreads) void few_eight_kernel(Eights p, O* __r
     constexpr int MT = decltype(tiles)::value;
     const bool any = rows.expert >= 0 && p.rows > 0;
     if (any)
-      few_sums<int8_t, MT, true>(sums, [&](int m) {
+      few_sums<int8_t, MT, WAVES, true>(sums, [&](int m) {
         const int64_t at = row_of(p, rows.from + min(m, count - 1));
         return p.x + (at < 0 ? 0 : at) * p.pitch;
       }, p.w + (first + min(n0 + (lane & 15), p.n - 1)) * p.pitch, p.w + (first + min(n0 + 16 + (lane & 15), p.n - 1)) * p.pitch, p.pitch);
     __syncthreads();
-    for (int t = threadIdx.x; t < MT * 16 * COLS; t += kFewThreads) {
+    for (int t = threadIdx.x; t < MT * 16 * COLS; t += 64 * WAVES) {
       const int m = t / COLS, n = t % COLS;
       if (m >= count || n0 + n >= p.n) continue;
       const int64_t at = any ? row_of(p, rows.from + m) : -1;
-      const float v = at >= 0 ? (float)few_sum<int8_t, MT>(sums, n / 16, m, n % 16) * p.x_scales[at] * p.w_scales[first + n0 + n] : 0.0f;
+      const float v = at >= 0 ? (float)few_sum<int8_t, MT, WAVES>(sums, n / 16, m, n % 16) * p.x_scales[at] * p.w_scales[first + n0 + n] : 0.0f;
       out[(int64_t)(rows.from + m) * ld_out + n0 + n] = (O)v;
     }
   });
@@ -241,7 +241,10 @@ extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts
         };
         const Kernel which = kernel_for(slots, experts, n, 2 * kFewCols, 128);
         if (which == FEW)
-          run(few_eight_kernel<O>, kFewRows, 2 * kFewCols, kFewThreads, kFewShared);
+          with_few_waves(padded(cols), [&](auto waves) {
+            constexpr int WAVES = decltype(waves)::value;
+            run(few_eight_kernel<O, WAVES>, kFewRows, 2 * kFewCols, 64 * WAVES, few_shared(WAVES));
+          });
         else if (which == TILE_256)
           run(eight_kernel<O, 256>, 256, 256, 256, Tile<int8_t, 256>::LDS);
         else

@@ -188,8 +188,8 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products
 }
 
 // PRODUCT and GATED for few rows of each expert.
-template <class T, int OUT, bool DIRECT>
-__global__ __launch_bounds__(kFewThreads) void few_kernel(Products<T> p, int activation, T* __restrict__ out, int64_t ld_out) {
+template <class T, int OUT, int WAVES, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(Products<T> p, int activation, T* __restrict__ out, int64_t ld_out) {
   constexpr int COLS = OUT == PRODUCT ? 2 * kFewCols : kFewCols;
   extern __shared__ __align__(16) char shared[];
   auto* sums = reinterpret_cast<f32x4*>(shared);
@@ -207,21 +207,21 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(Products<T> p, int act
       const T* w0 = p.w[0] + (first + min(n0 + (lane & 15), p.n - 1)) * p.k;
       const T* w1 = OUT == PRODUCT ? p.w[0] + (first + min(n0 + 16 + (lane & 15), p.n - 1)) * p.k
                                    : p.w[1] + (first + min(n0 + (lane & 15), p.n - 1)) * p.k;
-      few_sums<T, MT, DIRECT>(sums, [&](int m) {
+      few_sums<T, MT, WAVES, DIRECT>(sums, [&](int m) {
         const int64_t at = row_of(p, rows.from + min(m, count - 1));
         return p.x + (at < 0 ? 0 : at) * p.ld;
       }, w0, w1, p.k);
     }
     __syncthreads();
-    for (int t = threadIdx.x; t < MT * 16 * COLS; t += kFewThreads) {
+    for (int t = threadIdx.x; t < MT * 16 * COLS; t += 64 * WAVES) {
       const int m = t / COLS, n = t % COLS;
       if (m >= count || n0 + n >= p.n) continue;
       float v = 0.0f;
       if (any && row_of(p, rows.from + m) >= 0) {
         if constexpr (OUT == PRODUCT) {
-          v = few_sum<T, MT>(sums, n / 16, m, n % 16);
+          v = few_sum<T, MT, WAVES>(sums, n / 16, m, n % 16);
         } else {
-          const float g = few_sum<T, MT>(sums, 0, m, n), u = few_sum<T, MT>(sums, 1, m, n);
+          const float g = few_sum<T, MT, WAVES>(sums, 0, m, n), u = few_sum<T, MT, WAVES>(sums, 1, m, n);
           with_activation(activation, [&](auto act) { v = act.at(g).act * u; });
         }
       }
@@ -499,10 +499,13 @@ void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, 
         p.tiles_n = (int)ceil_div(c.n, OUT == PRODUCT ? 2 * kFewCols : kFewCols);
         p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, kFewRows, c.offsets);
         with_bool(c.x_direct() && c.w_direct(), [&](auto direct) {
-          over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
-            p.first = first;
-            go(few_kernel<T, OUT, decltype(direct)::value>, dim3(groups), kFewThreads, kFewShared, s, p, activation,
-               static_cast<T*>(out), ld_out);
+          with_few_waves(c.k * (int64_t)sizeof(T), [&](auto waves) {
+            constexpr int WAVES = decltype(waves)::value;
+            over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
+              p.first = first;
+              go(few_kernel<T, OUT, WAVES, decltype(direct)::value>, dim3(groups), 64 * WAVES, few_shared(WAVES), s, p, activation,
+                 static_cast<T*>(out), ld_out);
+            });
           });
         });
         return;

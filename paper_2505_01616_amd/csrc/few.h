@@ -39,13 +39,15 @@ struct Small<int8_t> {
   }
 };
 
-constexpr int kFewRows = 64, kFewCols = 16, kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+constexpr int kFewRows = 64, kFewCols = 16;
 
-// 16 bytes of a row of which `left` elements are there.
-template <class T, bool DIRECT>
+// 16 bytes of a row of which `left` elements are there (WHOLE: all).
+template <class T, bool DIRECT, bool WHOLE>
 __device__ __forceinline__ uint4 few_chunk(const T* p, int left) {
   if constexpr (DIRECT)
-    return *(left > 0 ? reinterpret_cast<const uint4*>(p) : &zeros);
+    return *(WHOLE || left > 0 ? reinterpret_cast<const uint4*>(p) : &zeros);
+  else if constexpr (WHOLE)
+    return chunk_at(p, 0);
   else
     return chunk_of(p, left);
 }
@@ -53,33 +55,36 @@ __device__ __forceinline__ uint4 few_chunk(const T* p, int left) {
 // The sums of up to 16 MT rows, rows k elements long: x(m): row m, w[0], w[1]:
 // this lane's rows of the matrices.  Every wave takes its part of the summed
 // index and leaves its sums in `shared`.
-template <class T, int MT, bool DIRECT, class X>
+template <class T, int MT, int WAVES, bool DIRECT, class X>
 __device__ __forceinline__ void few_sums(typename Small<T>::Sum* shared, X&& x, const T* w0, const T* w1, int k) {
   constexpr int PER = 16 / sizeof(T), STEP = 4 * PER, U = MT == 1 ? 8 : MT == 2 ? 6 : 4;
   const int lane = threadIdx.x & 63, wave = wave_of_group(), at = (lane >> 4) * PER;
   const int steps = (k + STEP - 1) / STEP;
-  const int from = steps * wave / kFewWaves, to = steps * (wave + 1) / kFewWaves;
+  const int from = steps * wave / WAVES, to = steps * (wave + 1) / WAVES;
   typename Small<T>::Sum sum[2][MT] = {};
   const T* rows[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) rows[m] = x(m * 16 + (lane & 15)) + at;
   w0 += at;
   w1 += at;
-  auto some = [&](int s0, auto number) {
-    constexpr int N = decltype(number)::value;
-    uint4 a[N][2], b[N][MT];
+  // U steps; what lies behind `to` or the rows' ends counts as zeros
+  auto some = [&](int s0, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
+    uint4 a[U][2], b[U][MT];
+    int left[U];
 #pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const int c = (s0 + u) * STEP, left = k - c - at;
-      a[u][0] = few_chunk<T, DIRECT>(w0 + c, left);
-      a[u][1] = few_chunk<T, DIRECT>(w1 + c, left);
+    for (int u = 0; u < U; ++u) {
+      const int c = (s0 + u) * STEP;
+      left[u] = s0 + u < to ? k - c - at : 0;
+      a[u][0] = few_chunk<T, DIRECT, WHOLE>(w0 + c, left[u]);
+      a[u][1] = few_chunk<T, DIRECT, WHOLE>(w1 + c, left[u]);
     }
 #pragma unroll
-    for (int u = 0; u < N; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) b[u][m] = few_chunk<T, DIRECT>(rows[m] + (s0 + u) * STEP, k - (s0 + u) * STEP - at);
+      for (int m = 0; m < MT; ++m) b[u][m] = few_chunk<T, DIRECT, WHOLE>(rows[m] + (s0 + u) * STEP, left[u]);
 #pragma unroll
-    for (int u = 0; u < N; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         sum[0][m] = Small<T>::add(a[u][0], b[u][m], sum[0][m]);
@@ -87,8 +92,8 @@ __device__ __forceinline__ void few_sums(typename Small<T>::Sum* shared, X&& x, 
       }
   };
   int s = from;
-  for (; s + U <= to; s += U) some(s, std::integral_constant<int, U>{});
-  for (; s < to; ++s) some(s, std::integral_constant<int, 1>{});
+  for (; s + U <= to && (s + U) * STEP <= k; s += U) some(s, std::true_type{});
+  for (; s < to; s += U) some(s, std::false_type{});
 #pragma unroll
   for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -96,13 +101,13 @@ __device__ __forceinline__ void few_sums(typename Small<T>::Sum* shared, X&& x, 
 }
 
 // The workgroup's sum over its waves: matrix p, row m, column n.
-template <class T, int MT>
+template <class T, int MT, int WAVES>
 __device__ __forceinline__ auto few_sum(const typename Small<T>::Sum* shared, int p, int m, int n) {
   using V = std::conditional_t<sizeof(T) == 1, int, float>;
   const V* at = reinterpret_cast<const V*>(shared) + ((p * MT + m / 16) * 64 + m % 16 + 16 * (n / 4)) * 4 + n % 4;
   V sum = 0;
 #pragma unroll
-  for (int w = 0; w < kFewWaves; ++w) sum += at[w * 2 * MT * 256];
+  for (int w = 0; w < WAVES; ++w) sum += at[w * 2 * MT * 256];
   return sum;
 }
 
@@ -113,10 +118,25 @@ __device__ __forceinline__ void with_few(int count, F&& f) {
     f(std::integral_constant<int, 1>{});
   else if (count <= 32)
     f(std::integral_constant<int, 2>{});
+  else if (count <= 48)
+    f(std::integral_constant<int, 3>{});
   else
     f(std::integral_constant<int, 4>{});
 }
-constexpr int kFewShared = kFewWaves * 2 * 4 * 64 * 16;
+constexpr int few_shared(int waves) { return waves * 2 * 4 * 64 * 16; }
+
+// Calls f with the waves of a workgroup: as many as have 16 steps each, so that
+// all have a second batch of loads behind the first, from four to eight.  A row
+// on 4 of 64 experts, two matrices of 2,048 x 2,048 bfloat16 each (64 steps): 13.9
+// us by four waves, 15.5 by eight; 96 rows on 8 experts of two 1,024 x 4,096
+// (128 steps): 44.9 and 40.8.
+template <class F>
+void with_few_waves(int64_t row_bytes, F&& f) {
+  if (row_bytes > 64 * 64)
+    f(std::integral_constant<int, 8>{});
+  else
+    f(std::integral_constant<int, 4>{});
+}
 
 }  // namespace
 }  // namespace netsim_ops
