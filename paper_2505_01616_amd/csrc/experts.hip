@@ -84,7 +84,8 @@ __device__ __forceinline__ Eight<T> quad(const T* p) {
 
 // Rows by slot.  PRODUCT: out = y.  GATED: out = h; a tile's columns are 32 of
 // g and 32 of u in turn, so that a lane holds both of an element.  GATED_BACK:
-// out = dg, out2 = du, both [slots x ld_out].
+// out = dg, out2 = du, both [slots x ld_out],
+// zeros beyond n.
 template <class T, int OUT, int SIZE, bool DIRECT>
 __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products<T> p, int activation, const T* __restrict__ dy,
                                                             int64_t ld_dy, T* __restrict__ out, T* __restrict__ out2,
@@ -162,27 +163,39 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products
           chunk_of(dy + (int64_t)(rows.from + r) * ld_dy + n0 + c, r < count ? p.n - n0 - c : 0);
     }
     __syncthreads();
-    with_activation(activation, [&](auto act) {
 #pragma unroll
-      for (int i = 0; i < M::F; ++i)
+    for (int i = 0; i < M::F; ++i)
 #pragma unroll
-        for (int j = 0; j < JN; ++j)
+      for (int j = 0; j < JN; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; r += 4) {
-            const Eight<T> d = quad(tile_dy + (M::row0() + i * 32 + (lane & 31)) * PITCH + col(j) + 2 * r + 4 * (lane >> 5));
+        for (int r = 0; r < 16; r += 4) {
+          const Eight<T> d = quad(tile_dy + (M::row0() + i * 32 + (lane & 31)) * PITCH + col(j) + 2 * r + 4 * (lane >> 5));
+          Slope s[4];
+          with_activation(activation, [&](auto act) {
 #pragma unroll
-            for (int h = r; h < r + 4; ++h) {
-              const float v = value_of(d, h - r), u = m.sum[i][j + JN][h];
-              const Slope s = act.at(m.sum[i][j][h]);
-              m.sum[i][j][h] = held[i] ? v * u * s.slope : 0.0f;
-              m.sum[i][j + JN][h] = held[i] ? v * s.act : 0.0f;
-            }
-            // one after the other: together they need more registers than there are
-            __builtin_amdgcn_sched_barrier(0);
+            for (int h = 0; h < 4; ++h) s[h] = act.at(m.sum[i][j][r + h]);
+          });
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            const float v = value_of(d, h), u = m.sum[i][j + JN][r + h];
+            m.sum[i][j][r + h] = held[i] ? v * u * s[h].slope : 0.0f;
+            m.sum[i][j + JN][r + h] = held[i] ? v * s[h].act : 0.0f;
           }
-    });
-    M::template write<COLS, JN>(shared, to, ld_out, count, p.n - n0, col, [&](int i, int j, int r) { return m.sum[i][j][r]; });
-    M::template write<COLS, JN>(shared, out2 + (int64_t)rows.from * ld_out + n0, ld_out, count, p.n - n0, col,
+          // one after the other: together they need more registers than there are
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    const int cols = (int)ld_out - n0;   // up to the rows' whole chunks, with zeros
+    if (n0 + COLS > p.n) {
+#pragma unroll
+      for (int j = 0; j < JN; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (n0 + col(j) + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3) >= p.n)
+#pragma unroll
+            for (int i = 0; i < M::F; ++i) m.sum[i][j][r] = m.sum[i][j + JN][r] = 0.0f;
+    }
+    M::template write<COLS, JN>(shared, to, ld_out, count, cols, col, [&](int i, int j, int r) { return m.sum[i][j][r]; });
+    M::template write<COLS, JN>(shared, out2 + (int64_t)rows.from * ld_out + n0, ld_out, count, cols, col,
                                 [&](int i, int j, int r) { return m.sum[i][j + JN][r]; });
   }
 }
@@ -230,10 +243,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Products<T> p, int acti
   });
 }
 
-// Rows' gradients by slot: the sum over `pairs` of d W, d [slots x ld_d] of n
-// values a row.
+// Rows' gradients by slot: the sum over `pairs` of d W, d [slots x ld_d] of
+// `length` values a row, n and zeros.
 template <class T, class O, int SIZE, bool DIRECT>
-__global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void input_kernel(Products<T> p, int pairs, const T* __restrict__ d0,
+__global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void input_kernel(Products<T> p, int pairs, int length, const T* __restrict__ d0,
                                                              const T* __restrict__ d1, int64_t ld_d,
                                                              O* __restrict__ dx) {
   using M = Tile<T, SIZE>;
@@ -264,7 +277,7 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void input_kernel(Product
           const int k0 = (second ? s - steps : s) * A::STEP;
           const int64_t shift = second ? p.w[1] - p.w[0] : 0;
           if (n < A::N) {
-            a.template load<QUICK>(n, to.stage, to.set, k0, p.n, second ? d1 - d0 : 0);
+            a.template load<QUICK>(n, to.stage, to.set, k0, length, second ? d1 - d0 : 0);
           } else if constexpr (QUICK) {
             b.load_run(n - A::N, to.stage + M::HALF, to.set, k0 + B::row(n - A::N), shift);
           } else {
@@ -572,7 +585,9 @@ Space space_of(const Cut& cut, int matrices, int64_t slots, int64_t n, int64_t k
 // rows are the slots'.
 void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work, const void* d0, const void* d1, int64_t ld_d,
                    const int32_t* slots_of_row, int32_t each, void* dx, void* dw0, void* dw1, hipStream_t s) {
-  const bool d_direct = ld_d % 8 == 0 && c.n % 8 == 0 && aligned(d0, 16) && aligned(d1, 16);
+  // rows of the workspace are filled up with zeros to whole chunks
+  const bool filled = c.matrices == 2, d_direct = filled || (ld_d % 8 == 0 && c.n % 8 == 0 && aligned(d0, 16));
+  const int length = filled ? (int)ld_d : c.n;
   with_16_bits(c.type, [&](auto t) {
     using T = decltype(t);
     if (dx && c.slots > 0)
@@ -585,7 +600,7 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
           p.tiles = p.tiles_n * most_rows_tiles(c.experts, c.slots, S::SIZE, c.offsets);
           over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
             p.first = first;
-            go(input_kernel<T, O, S::SIZE, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, c.matrices,
+            go(input_kernel<T, O, S::SIZE, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, c.matrices, length,
                static_cast<const T*>(d0), static_cast<const T*>(d1), ld_d,
                static_cast<O*>(decltype(mapped)::value ? static_cast<void*>(work + space.by_slot) : dx));
           });
