@@ -767,7 +767,8 @@ netsim_status netsim_act_weight_grad(int32_t device, int32_t experts, int64_t sl
  * distribution's function of g (NETSIM_GELU).  x, the weights and the result
  * [slots x ld_y] have one type of 16 bits; sums and act are computed in 32 and
  * rounded once.  A slot of no expert or without a row (its number out of
- * range) has a result of zeros.
+ * range) has a result of zeros.  d_g, d_u: g and u, [slots x n] in 32 bits, kept
+ * for the backward pass (NULL: not).
  * experts: 1 .. 1024; n, cols: 1 .. 2^20; slots < 2^31-4096.
  */
 enum { NETSIM_SILU = 0, NETSIM_GELU = 1 };
@@ -780,7 +781,8 @@ netsim_status netsim_experts_gated(int32_t device, int32_t experts, int64_t slot
                                    int32_t cols, int32_t type, int32_t activation, int64_t rows,
                                    const void* d_x, int64_t ld_x, const int32_t* d_row_of_slot,
                                    const int32_t* d_offsets, const void* d_w_gate,
-                                   const void* d_w_up, void* d_h, int64_t ld_h, void* hip_stream);
+                                   const void* d_w_up, void* d_h, int64_t ld_h, float* d_g,
+                                   float* d_u, void* hip_stream);
 
 /*
  * Their backward passes.  From the result's gradient d_dy (d_dh)
@@ -792,8 +794,9 @@ netsim_status netsim_experts_gated(int32_t device, int32_t experts, int64_t slot
  *     gives the row, -1 for none) in the list's order;
  *   d_dw, or d_dw_gate and d_dw_up: the weights' [experts x n x cols], zero
  *     for an expert without slots (NULL: none).
- * gated's g and u are computed again; their gradients are rounded to the
- * inputs' type before they enter the products.  Sums in 32 bits, rounded once.
+ * gated's g and u are those that were kept (d_g and d_u NULL: computed again);
+ * their gradients are rounded to the inputs' type before
+ * they enter the products.  Sums in 32 bits, rounded once.
  * A slot of no expert or without a row is left out, whatever its gradient
  * holds.  d_work: netsim_experts_backward_work_bytes(...) bytes (-1 for
  * refused sizes), aligned to 16; matrices: 1 for product, 2 for gated;
@@ -810,8 +813,8 @@ netsim_status netsim_experts_product_backward(
 netsim_status netsim_experts_gated_backward(
     int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols, int32_t type,
     int32_t activation, int64_t rows, const void* d_x, int64_t ld_x, const int32_t* d_row_of_slot,
-    const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up, const void* d_dh,
-    int64_t ld_dh, const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx, void* d_dw_gate,
+    const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up, const float* d_g,
+    const float* d_u, const void* d_dh, int64_t ld_dh, const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx, void* d_dw_gate,
     void* d_dw_up, void* d_work, int64_t work_bytes, void* hip_stream);
 
 /*

@@ -3,7 +3,8 @@
 //   product:  y_s = x W_e^T                    (x: the row of slot s, e its expert)
 //   gated:    h_s = act(g) u, g = x Wg_e^T, u = x Wu_e^T
 //
-// gated's backward pass computes g and u again, from which
+// gated's backward pass takes g and u as the forward pass kept them, in 32 bits, or
+// computes them again, and from them
 //   dg = dh u act'(g), du = dh act(g)          (rounded to the inputs' type)
 // and then, as product's does from dy, the rows' gradient dg Wg + du Wu and
 // the weights', the sums of dg x and du x over an expert's slots.  All of it
@@ -89,7 +90,7 @@ __device__ __forceinline__ Eight<T> quad(const T* p) {
 template <class T, int OUT, int SIZE, bool DIRECT>
 __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products<T> p, int activation, const T* __restrict__ dy,
                                                             int64_t ld_dy, T* __restrict__ out, T* __restrict__ out2,
-                                                            int64_t ld_out) {
+                                                            int64_t ld_out, float* __restrict__ g_out, float* __restrict__ u_out) {
   using M = Tile<T, SIZE>;
   using A = RowTile<T, SIZE, M::THREADS, DIRECT>;
   using B = A;
@@ -152,6 +153,11 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products
         return held[i] ? act.at(m.sum[i][j][r]).act * m.sum[i][j + JN][r] : 0.0f;
       });
     });
+    if (g_out) {
+      const int64_t at = (int64_t)rows.from * p.n + n0;
+      M::template write<COLS, JN>(shared, g_out + at, p.n, count, p.n - n0, col, [&](int i, int j, int r) { return held[i] ? m.sum[i][j][r] : 0.0f; });
+      M::template write<COLS, JN>(shared, u_out + at, p.n, count, p.n - n0, col, [&](int i, int j, int r) { return held[i] ? m.sum[i][j + JN][r] : 0.0f; });
+    }
   } else {
     // the tile of dh, in whole lines through shared memory as well
     constexpr int PITCH = COLS + 8;
@@ -202,7 +208,8 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products
 
 // PRODUCT and GATED for few rows of each expert.
 template <class T, int OUT, int WAVES, bool DIRECT>
-__global__ __launch_bounds__(64 * WAVES) void few_kernel(Products<T> p, int activation, T* __restrict__ out, int64_t ld_out) {
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(Products<T> p, int activation, T* __restrict__ out, int64_t ld_out,
+                                                         float* __restrict__ g_out, float* __restrict__ u_out) {
   constexpr int COLS = OUT == PRODUCT ? 2 * kFewCols : kFewCols;
   extern __shared__ __align__(16) char shared[];
   auto* sums = reinterpret_cast<f32x4*>(shared);
@@ -230,17 +237,47 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Products<T> p, int acti
       const int m = t / COLS, n = t % COLS;
       if (m >= count || n0 + n >= p.n) continue;
       float v = 0.0f;
-      if (any && row_of(p, rows.from + m) >= 0) {
-        if constexpr (OUT == PRODUCT) {
-          v = few_sum<T, MT, WAVES>(sums, n / 16, m, n % 16);
-        } else {
-          const float g = few_sum<T, MT, WAVES>(sums, 0, m, n), u = few_sum<T, MT, WAVES>(sums, 1, m, n);
-          with_activation(activation, [&](auto act) { v = act.at(g).act * u; });
+      const bool held = any && row_of(p, rows.from + m) >= 0;
+      if constexpr (OUT == PRODUCT) {
+        if (held) v = few_sum<T, MT, WAVES>(sums, n / 16, m, n % 16);
+      } else {
+        const float g = held ? few_sum<T, MT, WAVES>(sums, 0, m, n) : 0.0f, u = held ? few_sum<T, MT, WAVES>(sums, 1, m, n) : 0.0f;
+        with_activation(activation, [&](auto act) { v = act.at(g).act * u; });
+        if (g_out) {
+          const int64_t at = (int64_t)(rows.from + m) * p.n + n0 + n;
+          g_out[at] = g;
+          u_out[at] = u;
         }
       }
       out[(int64_t)(rows.from + m) * ld_out + n0 + n] = (T)v;
     }
   });
+}
+
+// dg and du from g and u that were kept, as GATED_BACK leaves them: one pass, bound
+// by memory.  A lane takes eight columns.
+template <class T>
+__global__ __launch_bounds__(256) void slope_kernel(Products<T> p, int64_t first, int units, int activation, const float* __restrict__ g,
+                                                    const float* __restrict__ u, const T* __restrict__ dy, int64_t ld_dy,
+                                                    T* __restrict__ dg, T* __restrict__ du, int64_t ld_d) {
+  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x, slot = first + unit / units;
+  const int c = (int)(unit % units) * 8, left = p.n - c;
+  if (slot >= p.slots) return;
+  const bool held = row_of(p, (int)slot) >= 0;
+  const Eight<float> gs = load_some(g + slot * p.n + c, left), us = load_some(u + slot * p.n + c, left);
+  const Eight<T> d = load_some(dy + slot * ld_dy + c, held ? left : 0);
+  float a[8], b[8];
+  with_activation(activation, [&](auto act) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const Slope s = act.at(value_of(gs, j));
+      const bool in = held & (j < left);
+      a[j] = in ? value_of(d, j) * value_of(us, j) * s.slope : 0.0f;
+      b[j] = in ? value_of(d, j) * s.act : 0.0f;
+    }
+  });
+  store_some(dg + slot * ld_d + c, a, 8);
+  store_some(du + slot * ld_d + c, b, 8);
 }
 
 // Rows' gradients by slot: the sum over `pairs` of d W, d [slots x ld_d] of
@@ -502,7 +539,8 @@ void go(K kernel, dim3 grid, int threads, int lds, hipStream_t s, Args... args) 
 
 // Rows by slot (rows_kernel, few_kernel).
 template <int OUT>
-void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, void* out, void* out2, int64_t ld_out, hipStream_t s) {
+void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, void* out, void* out2, int64_t ld_out, float* g, float* u,
+                  hipStream_t s) {
   with_16_bits(c.type, [&](auto t) {
     using T = decltype(t);
     const Kernel kernel = kernel_for(c.slots, c.experts, c.n, OUT == PRODUCT ? 2 * kFewCols : kFewCols, OUT == PRODUCT ? 128 : 64);
@@ -517,7 +555,7 @@ void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, 
             over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
               p.first = first;
               go(few_kernel<T, OUT, WAVES, decltype(direct)::value>, dim3(groups), 64 * WAVES, few_shared(WAVES), s, p, activation,
-                 static_cast<T*>(out), ld_out);
+                 static_cast<T*>(out), ld_out, g, u);
             });
           });
         });
@@ -531,7 +569,7 @@ void enqueue_rows(const Call& c, int activation, const void* dy, int64_t ld_dy, 
       over_tiles(p.tiles, [&](int64_t first, unsigned groups) {
         p.first = first;
         go(rows_kernel<T, OUT, S::SIZE, S::DIRECT>, dim3(groups), S::M::THREADS, S::M::LDS, s, p, activation,
-           static_cast<const T*>(dy), ld_dy, static_cast<T*>(out), static_cast<T*>(out2), ld_out);
+           static_cast<const T*>(dy), ld_dy, static_cast<T*>(out), static_cast<T*>(out2), ld_out, g, u);
       });
     });
   });
@@ -672,24 +710,26 @@ extern "C" netsim_status netsim_experts_product(int32_t device, int32_t experts,
     if (slots == 0) return (netsim_status)NETSIM_OK;
     if (!d_y) return fail(NETSIM_E_INVALID, what, "NULL array");
     if (!aligned(d_y, 2)) return fail(NETSIM_E_INVALID, what, "d_y is not aligned to its type");
-    return launch(what, device, [&] { enqueue_rows<PRODUCT>(c, 0, nullptr, 0, d_y, nullptr, ld_y, static_cast<hipStream_t>(hip_stream)); });
+    return launch(what, device, [&] { enqueue_rows<PRODUCT>(c, 0, nullptr, 0, d_y, nullptr, ld_y, nullptr, nullptr, static_cast<hipStream_t>(hip_stream)); });
   });
 }
 
 extern "C" netsim_status netsim_experts_gated(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
                                               int32_t type, int32_t activation, int64_t rows, const void* d_x, int64_t ld_x,
                                               const int32_t* d_row_of_slot, const int32_t* d_offsets, const void* d_w_gate,
-                                              const void* d_w_up, void* d_h, int64_t ld_h, void* hip_stream) {
+                                              const void* d_w_up, void* d_h, int64_t ld_h, float* d_g, float* d_u,
+                                              void* hip_stream) {
   const char* what = "experts_gated";
   return entry(what, device, [&] {
     const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w_gate, d_w_up}, 2};
     if (netsim_status bad = check(what, c)) return bad;
     if (activation != NETSIM_SILU && activation != NETSIM_GELU) return fail(NETSIM_E_INVALID, what, "bad activation");
     if (ld_h < n) return fail(NETSIM_E_INVALID, what, "ld_h is below n");
+    if (!d_g != !d_u) return fail(NETSIM_E_INVALID, what, "both of g and u or neither");
     if (slots == 0) return (netsim_status)NETSIM_OK;
     if (!d_h) return fail(NETSIM_E_INVALID, what, "NULL array");
-    if (!aligned(d_h, 2)) return fail(NETSIM_E_INVALID, what, "d_h is not aligned to its type");
-    return launch(what, device, [&] { enqueue_rows<GATED>(c, activation, nullptr, 0, d_h, nullptr, ld_h, static_cast<hipStream_t>(hip_stream)); });
+    if (!aligned(d_h, 2) || !aligned(d_g, 4) || !aligned(d_u, 4)) return fail(NETSIM_E_INVALID, what, "d_h, d_g or d_u is not aligned to its type");
+    return launch(what, device, [&] { enqueue_rows<GATED>(c, activation, nullptr, 0, d_h, nullptr, ld_h, d_g, d_u, static_cast<hipStream_t>(hip_stream)); });
   });
 }
 
@@ -723,7 +763,8 @@ extern "C" netsim_status netsim_experts_product_backward(int32_t device, int32_t
 extern "C" netsim_status netsim_experts_gated_backward(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
                                                        int32_t type, int32_t activation, int64_t rows, const void* d_x,
                                                        int64_t ld_x, const int32_t* d_row_of_slot, const int32_t* d_offsets,
-                                                       const void* d_w_gate, const void* d_w_up, const void* d_dh, int64_t ld_dh,
+                                                       const void* d_w_gate, const void* d_w_up, const float* d_g,
+                                                       const float* d_u, const void* d_dh, int64_t ld_dh,
                                                        const int32_t* d_slots_of_row, int32_t slots_each, void* d_dx,
                                                        void* d_dw_gate, void* d_dw_up, void* d_work, int64_t work_bytes,
                                                        void* hip_stream) {
@@ -732,6 +773,7 @@ extern "C" netsim_status netsim_experts_gated_backward(int32_t device, int32_t e
     const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w_gate, d_w_up}, 2};
     if (!sizes_ok(experts, slots, n, cols)) return fail(NETSIM_E_INVALID, what, kSizes);
     if (activation != NETSIM_SILU && activation != NETSIM_GELU) return fail(NETSIM_E_INVALID, what, "bad activation");
+    if (!d_g != !d_u || !aligned(d_g, 4) || !aligned(d_u, 4)) return fail(NETSIM_E_INVALID, what, "both of g and u, aligned, or neither");
     const Cut cut = make_cut(experts, slots, n, cols, 2);
     const Space space = space_of(cut, 2, slots, n, cols, d_row_of_slot);
     if (netsim_status bad =
@@ -740,7 +782,18 @@ extern "C" netsim_status netsim_experts_gated_backward(int32_t device, int32_t e
     return launch(what, device, [&] {
       hipStream_t s = static_cast<hipStream_t>(hip_stream);
       char* work = static_cast<char*>(d_work);
-      if (slots > 0) enqueue_rows<GATED_BACK>(c, activation, d_dh, ld_dh, work + space.d[0], work + space.d[1], space.ld_d, s);
+      if (slots > 0 && !d_g)
+        enqueue_rows<GATED_BACK>(c, activation, d_dh, ld_dh, work + space.d[0], work + space.d[1], space.ld_d, nullptr, nullptr, s);
+      else if (slots > 0)
+        with_16_bits(type, [&](auto t) {
+          using T = decltype(t);
+          const int units = (int)(space.ld_d / 8);
+          in_launches(slots, (kMaxGroups << 8) / units, [&](int64_t first, int64_t count) {
+            hipLaunchKernelGGL(slope_kernel<T>, dim3((unsigned)ceil_div(count * units, 256)), dim3(256), 0, s, c.products<T>(), first, units,
+                               activation, d_g, d_u, static_cast<const T*>(d_dh), ld_dh, reinterpret_cast<T*>(work + space.d[0]),
+                               reinterpret_cast<T*>(work + space.d[1]), space.ld_d);
+          });
+        });
       enqueue_grads(c, cut, space, work, work + space.d[0], work + space.d[1], space.ld_d, d_slots_of_row, slots_each, d_dx, d_dw_gate,
                     d_dw_up, s);
     });

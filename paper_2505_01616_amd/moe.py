@@ -302,15 +302,19 @@ def _matrices(weights):
     return [w.unsqueeze(0) if w.dim() == 2 else w for w in weights]
 
 
-def _products(x, weights, offsets, row_of_slot, slots_of_row, activation):
+def _products(x, weights, offsets, row_of_slot, slots_of_row, activation, kept=None):
+    """kept: a list that g and u are put into."""
     p = _Products(x, weights, offsets, row_of_slot, slots_of_row)
     y = p.result(x)
     head, tail = (p.index, p.experts, p.slots, p.n, p.cols, p.type), (p.rows, x.data_ptr(), p.ld, p.map, p.offsets)
     if activation is None:
         ns.netsim_experts_product(*head, *tail, weights[0].data_ptr(), y.data_ptr(), p.n, p.stream)
-    else:
-        ns.netsim_experts_gated(*head, activation, *tail, weights[0].data_ptr(), weights[1].data_ptr(), y.data_ptr(), p.n,
-                                p.stream)
+        return y
+    g = u = None
+    if kept is not None and p.slots:
+        kept += [torch.empty((p.slots, p.n), dtype=torch.float32, device=x.device) for _ in range(2)]
+        g, u = (t.data_ptr() for t in kept)
+    ns.netsim_experts_gated(*head, activation, *tail, weights[0].data_ptr(), weights[1].data_ptr(), y.data_ptr(), p.n, g, u, p.stream)
     return y
 
 
@@ -319,45 +323,48 @@ class _Multiplied(torch.autograd.Function):
     and the weights."""
 
     @staticmethod
-    def forward(ctx, x, offsets, row_of_slot, slots_of_row, activation, *weights):
+    def forward(ctx, x, offsets, row_of_slot, slots_of_row, activation, recompute, *weights):
         if ctx.needs_input_grad[0] and row_of_slot is not None and slots_of_row is None:
             raise ValueError("slots_of_row: the gradient of rows in a list needs the slots of every row")
-        ctx.activation = activation
-        ctx.save_for_backward(x, offsets, row_of_slot, slots_of_row, *weights)
-        return _products(x, weights, offsets, row_of_slot, slots_of_row, activation)
+        kept = [] if activation is not None and not recompute else None
+        y = _products(x, weights, offsets, row_of_slot, slots_of_row, activation, kept)
+        ctx.activation, ctx.matrices = activation, len(weights)
+        ctx.save_for_backward(x, offsets, row_of_slot, slots_of_row, *weights, *(kept or ()))
+        return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        x, offsets, row_of_slot, slots_of_row, *weights = ctx.saved_tensors
+        x, offsets, row_of_slot, slots_of_row, *rest = ctx.saved_tensors
+        weights, kept = rest[:ctx.matrices], rest[ctx.matrices:]
         if dy.stride(1) != 1 or dy.shape[0] > 1 and dy.stride(0) < dy.shape[1]:
             dy = dy.contiguous()
         p = _Products(x, weights, offsets, row_of_slot, slots_of_row)
         dx = torch.empty((p.rows, p.cols), dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
-        wanted = any(ctx.needs_input_grad[5:])
+        wanted = any(ctx.needs_input_grad[6:])
         dw = [torch.empty_like(w) if wanted else None for w in weights]
         space, size = p.workspace(len(weights), x.device)
         address = [None if t is None else t.data_ptr() for t in (dx, *dw, space)]
         head, tail = (p.index, p.experts, p.slots, p.n, p.cols, p.type), (p.rows, x.data_ptr(), p.ld, p.map, p.offsets)
-        tail += (*(w.data_ptr() for w in weights), dy.data_ptr(), dy.stride(0) if dy.shape[0] > 1 else p.n, p.list, p.each,
-                 *address, size, p.stream)
+        given = (dy.data_ptr(), dy.stride(0) if dy.shape[0] > 1 else p.n, p.list, p.each, *address, size, p.stream)
         if ctx.activation is None:
-            ns.netsim_experts_product_backward(*head, *tail)
+            ns.netsim_experts_product_backward(*head, *tail, weights[0].data_ptr(), *given)
         else:
-            ns.netsim_experts_gated_backward(*head, ctx.activation, *tail)
-        return dx, None, None, None, None, *dw
+            g, u = (t.data_ptr() for t in kept) if kept else (None, None)
+            ns.netsim_experts_gated_backward(*head, ctx.activation, *tail, weights[0].data_ptr(), weights[1].data_ptr(), g, u, *given)
+        return dx, None, None, None, None, None, *dw
 
 
-def _multiply(x, weights, offsets, row_of_slot, slots_of_row, activation):
+def _multiply(x, weights, offsets, row_of_slot, slots_of_row, activation, recompute=False):
     weights = _matrices(weights)
     if torch.is_grad_enabled() and (x.requires_grad or any(w.requires_grad for w in weights)):
-        return _Multiplied.apply(x, offsets, row_of_slot, slots_of_row, activation, *weights)
+        return _Multiplied.apply(x, offsets, row_of_slot, slots_of_row, activation, recompute, *weights)
     return _products(x, weights, offsets, row_of_slot, slots_of_row, activation)
 
 
 def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, offsets: Optional[torch.Tensor] = None,
           row_of_slot: Optional[torch.Tensor] = None, slots_of_row: Optional[torch.Tensor] = None,
-          activation: str = "silu") -> torch.Tensor:
+          activation: str = "silu", recompute: bool = False) -> torch.Tensor:
     """act(x w_gate^T) * (x w_up^T) by slot, [slots, n], in one kernel.
     activation: 'silu' or 'gelu'.
 
@@ -368,10 +375,14 @@ def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, offsets: Op
     other way round (-1 for none), is what the gradient of rows in such a list
     needs.  With a Dispatch: plan.offsets, plan.token_of_slot and
     plan.slot_of_choice.  Slots of no expert or without a row are zeros, and
-    left out of the gradients."""
+    left out of the gradients.
+
+    With gradients wanted, g = x w_gate^T and u = x w_up^T are kept for the
+    backward pass, 8 bytes an element of the result; recompute: they are computed
+    again there instead."""
     if activation not in _ACTIVATIONS:
         raise ValueError("activation: 'silu' or 'gelu'")
-    return _multiply(x, (w_gate, w_up), offsets, row_of_slot, slots_of_row, _ACTIVATIONS[activation])
+    return _multiply(x, (w_gate, w_up), offsets, row_of_slot, slots_of_row, _ACTIVATIONS[activation], recompute)
 
 
 def product(x: torch.Tensor, w: torch.Tensor, offsets: Optional[torch.Tensor] = None,

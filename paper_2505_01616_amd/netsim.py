@@ -154,11 +154,12 @@ _SIGS = {
     "netsim_act_weight_grad": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _P, _I64, _I64, _P, _P, _P, _P,
                                       _I32, _P, _P, _I64, _P]),
     "netsim_experts_product": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P]),
-    "netsim_experts_gated": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64, _P]),
+    "netsim_experts_gated": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64, _P, _P,
+                                    _P]),
     "netsim_experts_backward_work_bytes": (_I64, [_I32, _I64, _I32, _I32, _I32, _I32, _I32]),
     "netsim_experts_product_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P,
                                                _I32, _P, _P, _P, _I64, _P]),
-    "netsim_experts_gated_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64,
+    "netsim_experts_gated_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _I64,
                                              _P, _I32, _P, _P, _P, _P, _I64, _P]),
     "netsim_rows_quantise": (_I32, [_I32, _I64, _I32, _I32, _P, _I64, _P, _P, _P]),
     "netsim_experts_product8": (_I32, [_I32, _I32, _I64, _I32, _I32, _I64, _P, _P, _P, _P, _P, _P, _I32, _P, _I64, _P]),
@@ -556,9 +557,9 @@ def netsim_experts_product(device, experts, slots, n, cols, type, rows, d_x, ld_
 
 
 def netsim_experts_gated(device, experts, slots, n, cols, type, activation, rows, d_x, ld_x, d_row_of_slot, d_offsets,
-                         d_w_gate, d_w_up, d_h, ld_h, stream=None):
+                         d_w_gate, d_w_up, d_h, ld_h, d_g, d_u, stream=None):
     _check(None, load_library().netsim_experts_gated(device, experts, slots, n, cols, type, activation, rows, d_x, ld_x,
-                                                     d_row_of_slot, d_offsets, d_w_gate, d_w_up, d_h, ld_h,
+                                                     d_row_of_slot, d_offsets, d_w_gate, d_w_up, d_h, ld_h, d_g, d_u,
                                                      _stream(stream)))
 
 
@@ -575,10 +576,10 @@ def netsim_experts_product_backward(device, experts, slots, n, cols, type, rows,
 
 
 def netsim_experts_gated_backward(device, experts, slots, n, cols, type, activation, rows, d_x, ld_x, d_row_of_slot,
-                                  d_offsets, d_w_gate, d_w_up, d_dh, ld_dh, d_slots_of_row, slots_each, d_dx, d_dw_gate,
+                                  d_offsets, d_w_gate, d_w_up, d_g, d_u, d_dh, ld_dh, d_slots_of_row, slots_each, d_dx, d_dw_gate,
                                   d_dw_up, d_work, work_bytes, stream=None):
     _check(None, load_library().netsim_experts_gated_backward(device, experts, slots, n, cols, type, activation, rows, d_x,
-                                                              ld_x, d_row_of_slot, d_offsets, d_w_gate, d_w_up, d_dh, ld_dh,
+                                                              ld_x, d_row_of_slot, d_offsets, d_w_gate, d_w_up, d_g, d_u, d_dh, ld_dh,
                                                               d_slots_of_row, slots_each, d_dx, d_dw_gate, d_dw_up, d_work,
                                                               work_bytes, _stream(stream)))
 

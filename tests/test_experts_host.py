@@ -42,8 +42,8 @@ def test_products():
     for bad in BAD + [dict(w=None), dict(w=P + 1), dict(y=None), dict(y=P + 1), dict(ld_y=15)]:
         refused(ns.netsim_experts_product, *{**base, **bad}.values())
     ns.netsim_experts_product(*{**base, "slots": 0, "rows": 0, "x": None, "map": None, "y": None}.values())
-    base = {**put(BASE, "type", act=ns.SILU), "w": P, "w2": P, "y": P, "ld_y": 16}
-    for bad in BAD + [dict(act=2), dict(act=-1), dict(w=None), dict(w2=None), dict(w2=P + 1), dict(y=None), dict(ld_y=15)]:
+    base = {**put(BASE, "type", act=ns.SILU), "w": P, "w2": P, "y": P, "ld_y": 16, "g": None, "u": None}
+    for bad in BAD + [dict(g=P), dict(u=P), dict(g=P + 2, u=P),dict(act=2), dict(act=-1), dict(w=None), dict(w2=None), dict(w2=P + 1), dict(y=None), dict(ld_y=15)]:
         refused(ns.netsim_experts_gated, *{**base, **bad}.values())
     assert "offsets" in refused(ns.netsim_experts_gated, *{**base, "offsets": None}.values())
     assert "list" in refused(ns.netsim_experts_gated, *{**base, "map": None}.values())
@@ -57,8 +57,8 @@ def test_products_backward():
     for bad in bads + [dict(size=-1)]:
         refused(ns.netsim_experts_product_backward, *{**base, **bad}.values())
     assert "workspace" in refused(ns.netsim_experts_product_backward, *{**base, "size": 0}.values())
-    base = {**put(BASE, "type", act=ns.GELU), "w": P, "w2": P, **put(more, "dw", dw2=P)}
-    for bad in bads + [dict(act=2), dict(dw2=None), dict(dw=None), dict(dw2=P + 1), dict(size=0), dict(work=None)]:
+    base = {**put(BASE, "type", act=ns.GELU), "w": P, "w2": P, "g": P, "u": P, **put(more, "dw", dw2=P)}
+    for bad in bads + [dict(g=None), dict(u=None), dict(u=P + 2),dict(act=2), dict(dw2=None), dict(dw=None), dict(dw2=P + 1), dict(size=0), dict(work=None)]:
         refused(ns.netsim_experts_gated_backward, *{**base, **bad}.values())
     size = ns.netsim_experts_backward_work_bytes
     assert size(0, 8, 16, 16, 1, 1, 1) == -1 and size(4, 8, 16, 16, 3, 1, 1) == -1 and size(4, 8, 16, 1 << 21, 1, 1, 1) == -1

@@ -118,6 +118,11 @@ def check(gpu, kind, act, x, weights, lists, dy=None, pad=0, skew=0, scale=1.0, 
     gdy = wide(torch, dy, t, pad, skew)
     wanted = ([gx] if grads[0] else []) + (gw if grads[1] else [])
     back = torch.autograd.grad(got, wanted, gdy)
+    backs = [back]
+    if act:      # g and u computed again, by another kernel where rows are few
+        again = moe.gated(gx, *gw, activation=act, recompute=True, **more)
+        assert torch.equal(again, got)
+        backs.append(torch.autograd.grad(again, wanted, gdy))
     live = plain.used(lists[0], len(weights[0]), lists[1], len(dy), len(x))[:, None]
     dy = np.where(live, dy, 0)
     if act:
@@ -132,12 +137,13 @@ def check(gpu, kind, act, x, weights, lists, dy=None, pad=0, skew=0, scale=1.0, 
     tx, tw = plain.gradients(absx, absw, [np.abs(v) for v in d], *lists)
     ex, ew = plain.gradients(absx, absw, ed, *lists)
     each = 1 if lists[2] is None else lists[2].shape[1]
-    if grads[0]:
-        bound = ex + off(len(weights) * weights[0].shape[1] + each, tx + ex)
-        near(host(back[0]), dx, bound * (1 + s) + s * np.abs(dx) + least, "dx")
-    if grads[1]:
-        for g, w, t_, e_ in zip(back[-len(weights):], dw, tw, ew):
-            near(host(g), w, (e_ + off(len(dy), t_ + e_)) * (1 + s) + s * np.abs(w) + least, "dW")
+    for back in backs:
+        if grads[0]:
+            bound = ex + off(len(weights) * weights[0].shape[1] + each, tx + ex)
+            near(host(back[0]), dx, bound * (1 + s) + s * np.abs(dx) + least, "dx")
+        if grads[1]:
+            for g, w, t_, e_ in zip(back[-len(weights):], dw, tw, ew):
+                near(host(g), w, (e_ + off(len(dy), t_ + e_)) * (1 + s) + s * np.abs(w) + least, "dW")
     return got, back
 
 
