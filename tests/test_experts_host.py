@@ -89,7 +89,7 @@ def test_adamw():
 
     nan, inf = float("nan"), float("inf")
     for bad in (dict(tensors=-1), dict(tensor=0), dict(bits=16), dict(step=0), dict(counter=P + 4), dict(lr=-1.0), dict(lr=nan),
-                dict(lr=inf), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=nan), dict(eps=0.0), dict(eps=inf), dict(eps=nan),
+                dict(lr=inf), dict(b1=1.0), dict(b1=-0.1), dict(b2=1.0), dict(b2=nan), dict(eps=0.0), dict(eps=1e-31), dict(eps=inf), dict(eps=nan),
                 dict(decay=-1.0), dict(decay=nan), dict(scale=nan), dict(scale=inf), dict(size=-1), dict(pt=3), dict(gt=-1),
                 dict(p=None), dict(g=None), dict(m=None), dict(v=None), dict(p=P + 2), dict(g=P + 2), dict(m=P + 2), dict(master=P),
                 dict(pt=ns.BF16, p=P + 1), dict(pt=ns.BF16, master=P + 2), dict(bits=8, ms=None), dict(bits=8, vs=None),

@@ -2,8 +2,9 @@
 
 Bounds, u = 2^-24.  m and v are two products and a sum of values of one sign
 (v) or two (m): 4 u of |b1 m| + |c1 g|; the factors' own rounding is in it.
-d = m / (r root + eps): r off by half of v's 4 u and its own u, the sum,
-product and quotient 4 u: d off by Em / (r root + eps) + 8 u |d|.  p: 3 u of
+d = m / (r root + eps): r off by half of v's 4 u and its own u (2 u with moments
+in 8 bits, whose root may be a unit in the last place off, as the reciprocal),
+the sum, product and quotient 4 u: d off by Em / (r root + eps) + 8 u |d|.  p: 3 u of
 |p| + |rate d| and rate times d's error.  16-bit results add half a step.
 Moments in 8 bits are half a step of a 4-bit number (2^-4 of themselves, or
 2^-10 units below the smallest normal one) from the 64-bit value, with what
@@ -69,7 +70,7 @@ def check_step(torch, moe, opt, grads, scale, kind):
         ev = 4 * U * v + 2.0 ** -148
         root = (1 - b2 ** t) ** -0.5
         r = np.sqrt(v)
-        er = np.minimum(ev / np.maximum(r, 1e-300), np.sqrt(ev)) + U * r
+        er = np.minimum(ev / np.maximum(r, 1e-300), np.sqrt(ev)) + (U if opt.bits == 32 else 2 * U) * r
         denominator = r * root + opt.eps
         d = m / denominator
         ed = em / denominator + np.abs(d) * (er * root / denominator + 8 * U)
