@@ -230,7 +230,7 @@ extern "C" netsim_status netsim_experts_product8(int32_t device, int32_t experts
         using O = decltype(o);
         auto run = [&](auto kernel, int bm, int bn, int threads, int lds) {
           Eights p{experts, (int)slots, n, (int)padded(cols), rows, d_q, d_scales, d_row_of_slot, d_offsets, d_wq, d_w_scales, 0, 0, 0,
-                   rows * padded(cols) <= (int64_t)1 << 32, n * padded(cols) <= (int64_t)1 << 32};
+                   rows <= ((int64_t)1 << 32) / padded(cols), n * padded(cols) <= (int64_t)1 << 32};
           p.tiles_n = (int)ceil_div(n, bn);
           p.tiles = p.tiles_n * most_rows_tiles(experts, slots, bm, d_offsets);
           allow_shared((const void*)kernel, lds);

@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256) void gather_kernel(int64_t rows, int cols, int
 // x[row(s)][c].  Both factors have the summed index as their slow one.  Tiles are
 // numbered by matrix, part and place; MAPPED: slots have rows from a list, whose
 // places in x wait in shared memory, looked_of(SIZE) slots' at a time.
-constexpr int looked_of(int size) { return size == 256 ? 6144 : 2048; }
+constexpr int looked_of(int size) { return size == 256 ? 4096 : 2048; }   // at most 2^31 - kMaxSlots
 constexpr uint32_t kNoRow = ~0u;
 template <class T, int SIZE, bool DIRECT, bool MAPPED>
 __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void weight_kernel(Products<T> p, Sums g, Cut cut, const Item* __restrict__ items,
@@ -589,16 +589,23 @@ struct Space {
 
 // How the weights' sums are cut (parts.h): a die's 32 compute units work on 32
 // tiles of a part together, and the dies get their parts in turn, so parts are a
-// quarter as long as what each would have if all were busy to the end.
+// quarter as long as what each would have of one matrix if all were busy to the
+// end.  131,072 slots on 64 experts of 2,048 x 2,048, forward and backward, parts
+// of 4,096, 8,192 and 16,384 slots: one matrix 3.41, 3.36 and 3.44 ms, two
+// (the latter two) 8.34 and 8.60 ms.
 Cut make_cut(int64_t experts, int64_t slots, int64_t n, int64_t k, int matrices) {
   Cut c{};
   // as for the sums of saved rows: tiles of 256 from 3,000 slots for each
   // compute unit on
   c.tile = slots * matrices * ceil_div(n, 256) * ceil_div(k, 256) / 256 >= 3000 ? 256 : 128;
   c.step = 64;
-  const int64_t tiles = matrices * ceil_div(n, c.tile) * ceil_div(k, c.tile);
+  const int64_t tiles = ceil_div(n, c.tile) * ceil_div(k, c.tile);
   c.longest = ceil_div(slots * tiles, 256 * 4);
-  if (c.longest < 256) c.longest = 256;
+  // shorter ones cost more in joining than they save, unless there are too few
+  // tiles: 9,003 slots on 16 experts, two of 705 x 1,000, parts of 422 and 1,024
+  // slots: 338 and 296 us forward and backward
+  const int64_t least = experts * tiles * matrices >= 512 ? 1024 : 256;
+  if (c.longest < least) c.longest = least;
   if (c.longest > kMaxSlots) c.longest = kMaxSlots;
   c.plan = slots <= 512 ? Cut::WHOLE : experts * tiles <= 64 && experts <= 16 ? Cut::BY_WAVE : Cut::LISTED;
   if (c.plan == Cut::WHOLE) return c;
@@ -670,9 +677,10 @@ void enqueue_grads(const Call& c, const Cut& cut, const Space& space, char* work
                static_cast<const T*>(d1), ld_d, static_cast<T*>(dw0), static_cast<T*>(dw1), partials);
           });
         });
+        const int64_t groups = ceil_div((int64_t)c.n * c.k, 256), most = cut.joins < 16 ? 4096 / (cut.joins + 1) : 256;
         if (cut.joins > 0)
           for (int i = 0; i < c.matrices; ++i)
-            hipLaunchKernelGGL(join_kernel<T>, dim3(256, (unsigned)cut.joins), dim3(256), 0, s, g, cut, c.offsets, joins,
+            hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(groups < most ? groups : most), (unsigned)cut.joins), dim3(256), 0, s, g, cut, c.offsets, joins,
                                partials + i * cut.partials * (int64_t)c.n * c.k, static_cast<T*>(i ? dw1 : dw0));
       });
   });

@@ -441,7 +441,7 @@ __device__ __forceinline__ int lanes_up(int v) {
 __device__ __forceinline__ Rows find_rows(const int32_t* offsets, int experts, int slots, int size, int want) {
   auto part = [&](int expert, int from, int to, int nth) {
     const int64_t start = from + (int64_t)nth * size;
-    return start < to ? Rows{expert, (int)start, (int)min(start + size, (int64_t)to)} : Rows{-2, 0, 0};
+    return nth >= 0 && start < to ? Rows{expert, (int)start, (int)min(start + size, (int64_t)to)} : Rows{-2, 0, 0};
   };
   if (!offsets) return part(0, 0, slots, want);
   const int lane = threadIdx.x & 63;
