@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void rows_kernel(Products
     for (int t = threadIdx.x; t < SIZE * COLS / 8; t += M::THREADS) {
       const int r = t / (COLS / 8), c = t % (COLS / 8) * 8;
       *reinterpret_cast<uint4*>(tile_dy + r * PITCH + c) =
-          chunk_of(dy + (int64_t)(rows.from + r) * ld_dy + n0 + c, r < count ? p.n - n0 - c : 0);
+          chunk_of(dy + (int64_t)(rows.from + r) * ld_dy + n0 + c, r < count ? p.n - n0 - c : 0, p.n >= 8);
     }
     __syncthreads();
 #pragma unroll

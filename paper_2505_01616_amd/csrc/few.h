@@ -43,13 +43,13 @@ constexpr int kFewRows = 64, kFewCols = 16;
 
 // 16 bytes of a row of which `left` elements are there (WHOLE: all).
 template <class T, bool DIRECT, bool WHOLE>
-__device__ __forceinline__ uint4 few_chunk(const T* p, int left) {
+__device__ __forceinline__ uint4 few_chunk(const T* p, int left, bool wide) {
   if constexpr (DIRECT)
     return *(WHOLE || left > 0 ? reinterpret_cast<const uint4*>(p) : &zeros);
   else if constexpr (WHOLE)
     return chunk_at(p, 0);
   else
-    return chunk_of(p, left);
+    return chunk_of(p, left, wide);
 }
 
 // The sums of up to 16 MT rows, rows k elements long: x(m): row m, w[0], w[1]:
@@ -76,13 +76,13 @@ __device__ __forceinline__ void few_sums(typename Small<T>::Sum* shared, X&& x, 
     for (int u = 0; u < U; ++u) {
       const int c = (s0 + u) * STEP;
       left[u] = s0 + u < to ? k - c - at : 0;
-      a[u][0] = few_chunk<T, DIRECT, WHOLE>(w0 + c, left[u]);
-      a[u][1] = few_chunk<T, DIRECT, WHOLE>(w1 + c, left[u]);
+      a[u][0] = few_chunk<T, DIRECT, WHOLE>(w0 + c, left[u], k >= 8);
+      a[u][1] = few_chunk<T, DIRECT, WHOLE>(w1 + c, left[u], k >= 8);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) b[u][m] = few_chunk<T, DIRECT, WHOLE>(rows[m] + (s0 + u) * STEP, left[u]);
+      for (int m = 0; m < MT; ++m) b[u][m] = few_chunk<T, DIRECT, WHOLE>(rows[m] + (s0 + u) * STEP, left[u], k >= 8);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll

@@ -90,9 +90,29 @@ __device__ __forceinline__ uint4 chunk_at(const T* base, uint32_t off) {
   const Eight<T> v = load_eight(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + off));
   return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
 }
-// A chunk of 16 bytes of which `left` elements are there, zeros beyond.
+// Eight 16-bit values without the first `miss` (0 .. 7), zeros behind.
+__device__ __forceinline__ uint4 without_first(uint4 v, int miss) {
+  const bool by4 = miss & 4, by2 = miss & 2, by1 = miss & 1;
+  v = by4 ? make_uint4(v.z, v.w, 0, 0) : v;
+  v = by2 ? make_uint4(v.y, v.z, v.w, 0) : v;
+  return by1 ? make_uint4(__builtin_amdgcn_alignbit(v.y, v.x, 16), __builtin_amdgcn_alignbit(v.z, v.y, 16),
+                          __builtin_amdgcn_alignbit(v.w, v.z, 16), v.w >> 16)
+             : v;
+}
+// A chunk of 16 bytes of which `left` elements are there, zeros beyond.  In a row
+// of at least eight values (wide) the last chunk is read so that it ends with the
+// row: one by one its values would be loaded one after the other.
 template <class T>
-__device__ __forceinline__ uint4 chunk_of(const T* p, int left) {
+__device__ __forceinline__ uint4 chunk_of(const T* p, int left, bool wide) {
+  if constexpr (sizeof(T) == 2)
+    if (wide) {
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (left >= 8)
+        v = chunk_at(p, 0);
+      else if (left > 0)
+        v = without_first(chunk_at(p - (8 - left), 0), 8 - left);
+      return v;
+    }
   const Eight<T> v = load_some(p, left);
   return make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
 }
@@ -142,7 +162,7 @@ struct RowTile {
     if constexpr (!DIRECT && QUICK)
       held[set][i] = chunk_at(step, off[i]);
     else if constexpr (!DIRECT)
-      held[set][i] = chunk_of(step + at[i], left);
+      held[set][i] = chunk_of(step + at[i], left, k >= 8);
     else if constexpr (QUICK)
       to_shared(step, off[i], to);
     else
@@ -180,7 +200,8 @@ struct ColTile {
   const T* base;
   uint32_t ld;       // pitches are below 2^31
   uint32_t col, own;
-  bool near;
+  bool near, wide;
+  int back;          // !DIRECT: how far before its place the row's last chunk is read
   uint4 held[DIRECT ? 1 : HELD][DIRECT ? 1 : N];
   int left;
 
@@ -194,11 +215,13 @@ struct ColTile {
   __device__ __forceinline__ void open(const T* from, bool all_near, int64_t pitch, int c0, int cols) {
     int c = c0 + (threadIdx.x % CHUNKS ^ (4 * (threadIdx.x / CHUNKS & 3))) * 8;
     left = cols - c;
-    if (DIRECT && left <= 0) c = c0;
-    base = from + c0;
-    col = c - c0;
+    wide = cols >= 8;
+    back = !DIRECT && wide && left > 0 && left < 8 ? 8 - left : 0;
+    if ((DIRECT || wide) && left <= 0) c = DIRECT ? c0 : 0;
+    base = DIRECT ? from + c0 : from;
+    col = (DIRECT ? c - c0 : c) - back;
     ld = (uint32_t)pitch;
-    near = all_near && (DIRECT || c0 + R <= cols);
+    near = all_near && (DIRECT || wide);
     own = (mine() * ld + col) * 2;
   }
   __device__ __forceinline__ uint32_t place(int i, Place stage) const { return stage.address + i * THREADS * 16 + wave_of_group() * 1024; }
@@ -206,7 +229,7 @@ struct ColTile {
   __device__ __forceinline__ void load(int i, Place stage, int set, int r, int64_t shift = 0) {
     const T* from = base + shift + (uint64_t)(uint32_t)r * ld + col;
     if constexpr (!DIRECT)
-      held[set][i] = chunk_of(from, r >= 0 ? left : 0);
+      held[set][i] = wide ? chunk_of(from, r >= 0 ? 8 : 0, true) : chunk_of(from, r >= 0 ? left : 0, false);
     else
       to_shared(r >= 0 ? static_cast<const void*>(from) : &zeros, place(i, stage));
   }
@@ -229,7 +252,7 @@ struct ColTile {
   __device__ __forceinline__ void store(Place stage, int set) {
     if constexpr (!DIRECT)
 #pragma unroll
-      for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = held[set][i];
+      for (int i = 0; i < N; ++i) *reinterpret_cast<uint4*>(stage.at + (i * THREADS + threadIdx.x) * 16) = without_first(held[set][i], back);
   }
   // Lanes 0-15 give four rows of 16 columns and get a column each; lanes 16-31
   // the next 16 columns, lanes 32-63 the rows 8 further on.
