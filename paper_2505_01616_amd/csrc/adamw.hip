@@ -142,7 +142,10 @@ __device__ __forceinline__ int tensor_of(const Many& many, int64_t c) {
 }
 
 // A lane takes eight elements in a row, so 32 lanes hold a block of 8-bit
-// moments.
+// moments.  96 million bfloat16 elements with copies (2.7 GB) 536 us, 5.0 TB/s; 74
+// million with moments in 8 bits (0.75 GB) 155 us, 4.8 TB/s (a copy: 5.2).  The
+// tensors' addresses are the kernel's arguments, 40 tensors a launch: no table is
+// copied to the GPU.
 template <bool EIGHT>
 __global__ __launch_bounds__(256) void adamw_kernel(Many many, Factors f, const Counter* __restrict__ counter) {
   if (counter) {
@@ -185,8 +188,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Many many, Factors f, const 
         g[j] *= f.grad_scale;
         m[j] = m[j] * f.b1 + g[j] * f.c1;
         v[j] = v[j] * f.b2 + g[j] * g[j] * f.c2;
-        // what 8 bits hold needs no last bit: 104 million elements take 180 us with
-        // the exact root and quotient, which are 25 instructions an element
+        // what 8 bits hold needs no last bit: 74 million elements take 180 us
+        // instead of 155 with the exact root and quotient and tests for infinities
         r[j] = EIGHT ? root_of(v[j]) : sqrtf(v[j]);
         const float denominator = r[j] * f.root + f.eps;
         p[j] = p[j] * f.keep - (EIGHT ? m[j] * __builtin_amdgcn_rcpf(denominator) : m[j] / denominator) * f.rate;

@@ -19,7 +19,8 @@ constexpr int kMaxEight = 1 << 17;                // 127 127 2^17 < 2^31
 
 inline int64_t padded(int64_t cols) { return ceil_div(cols, 16) * 16; }
 
-// A workgroup per row.
+// A workgroup per row, up to 8,192 of whose values stay in registers between the
+// two looks at them.  Bound by memory: 8,192 rows of 2,048 bfloat16 (50 MB) 19 us.
 template <class T>
 __global__ __launch_bounds__(256) void quantise_kernel(int cols, int pitch, const T* __restrict__ x, int64_t ld,
                                                        int8_t* __restrict__ q, float* __restrict__ scales) {
@@ -89,6 +90,9 @@ __device__ __forceinline__ int64_t row_of(const Eights& p, int slot) {
   return r >= 0 && r < p.rows ? r : -1;
 }
 
+// Bound by a tile's beginning and end at short rows, by the matrix cores at long
+// ones: 32,768 slots on 64 uneven experts of 4,096 x 2,048 0.42 ms (1.3 POP/s),
+// 16,384 rows by 4,096 x 8,192 484 us (2.3 POP/s).
 template <class O, int SIZE>
 __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
   using M = Tile<int8_t, SIZE>;
@@ -144,7 +148,9 @@ __global__ __launch_bounds__(256, SIZE == 256 ? 1 : 2) void eight_kernel(Eights 
                                [&](int i, int j, int r) { return held[i] ? (float)m.sum[i][j][r] * x_scale[i] * w_scale[j][r] : 0.0f; });
 }
 
-// For few rows of each expert.
+// For few rows of each expert.  One row on 2 of 8 experts of 4,096 x 4,096 (34 MB):
+// 9.4 us under the profiler, of which a launch and the way to the first load are
+// about 4.
 template <class O, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void few_eight_kernel(Eights p, O* __restrict__ out, int64_t ld_out) {
   constexpr int COLS = 2 * kFewCols;
