@@ -800,10 +800,10 @@ netsim_status netsim_experts_gated(int32_t device, int32_t experts, int64_t slot
  * A slot of no expert or without a row is left out, whatever its gradient
  * holds.  d_work: netsim_experts_backward_work_bytes(...) bytes (-1 for
  * refused sizes), aligned to 16; matrices: 1 for product, 2 for gated;
- * has_offsets, has_rows: whether d_offsets and d_row_of_slot are given.
+ * by_row: whether d_row_of_slot and d_dx are given.
  */
 int64_t netsim_experts_backward_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
-                                           int32_t matrices, int32_t has_offsets, int32_t has_rows);
+                                           int32_t matrices, int32_t by_row);
 netsim_status netsim_experts_product_backward(
     int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols, int32_t type,
     int64_t rows, const void* d_x, int64_t ld_x, const int32_t* d_row_of_slot,

@@ -756,9 +756,9 @@ extern "C" netsim_status netsim_experts_gated(int32_t device, int32_t experts, i
 }
 
 extern "C" int64_t netsim_experts_backward_work_bytes(int32_t experts, int64_t slots, int32_t n, int32_t cols,
-                                                      int32_t matrices, int32_t has_offsets, int32_t has_rows) {
+                                                      int32_t matrices, int32_t by_row) {
   if (!sizes_ok(experts, slots, n, cols) || matrices < 1 || matrices > 2) return -1;
-  return space_of(make_cut(experts, slots, n, cols, matrices), matrices, slots, n, cols, has_rows).bytes;
+  return space_of(make_cut(experts, slots, n, cols, matrices), matrices, slots, n, cols, by_row).bytes;
 }
 
 extern "C" netsim_status netsim_experts_product_backward(int32_t device, int32_t experts, int64_t slots, int32_t n, int32_t cols,
@@ -772,7 +772,7 @@ extern "C" netsim_status netsim_experts_product_backward(int32_t device, int32_t
     const Call c{device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, {d_w, d_w}, 1};
     if (!sizes_ok(experts, slots, n, cols)) return fail(NETSIM_E_INVALID, what, kSizes);
     const Cut cut = make_cut(experts, slots, n, cols, 1);
-    const Space space = space_of(cut, 1, slots, n, cols, d_row_of_slot);
+    const Space space = space_of(cut, 1, slots, n, cols, d_row_of_slot && d_dx);
     if (netsim_status bad = check_back(what, c, d_dy, ld_dy, d_slots_of_row, slots_each, d_dx, d_dw, d_dw, d_work, work_bytes, space))
       return bad;
     return launch(what, device, [&] {
@@ -797,7 +797,7 @@ extern "C" netsim_status netsim_experts_gated_backward(int32_t device, int32_t e
     if (activation != NETSIM_SILU && activation != NETSIM_GELU) return fail(NETSIM_E_INVALID, what, "bad activation");
     if (!d_g != !d_u || !aligned(d_g, 4) || !aligned(d_u, 4)) return fail(NETSIM_E_INVALID, what, "both of g and u, aligned, or neither");
     const Cut cut = make_cut(experts, slots, n, cols, 2);
-    const Space space = space_of(cut, 2, slots, n, cols, d_row_of_slot);
+    const Space space = space_of(cut, 2, slots, n, cols, d_row_of_slot && d_dx);
     if (netsim_status bad =
             check_back(what, c, d_dh, ld_dh, d_slots_of_row, slots_each, d_dx, d_dw_gate, d_dw_up, d_work, work_bytes, space))
       return bad;

@@ -291,9 +291,9 @@ class _Products:
     def result(self, x):
         return torch.empty((self.slots, self.n), dtype=x.dtype, device=x.device)
 
-    def workspace(self, matrices: int, device):
+    def workspace(self, matrices: int, device, dx: bool):
         size = max(0, ns.netsim_experts_backward_work_bytes(self.experts, self.slots, self.n, self.cols, matrices,
-                                                            self.offsets is not None, self.map is not None))
+                                                            int(dx and self.map is not None)))
         return torch.empty(size, dtype=torch.uint8, device=device) if size else None, size
 
 
@@ -343,7 +343,7 @@ class _Multiplied(torch.autograd.Function):
         dx = torch.empty((p.rows, p.cols), dtype=x.dtype, device=x.device) if ctx.needs_input_grad[0] else None
         wanted = any(ctx.needs_input_grad[6:])
         dw = [torch.empty_like(w) if wanted else None for w in weights]
-        space, size = p.workspace(len(weights), x.device)
+        space, size = p.workspace(len(weights), x.device, dx is not None)
         address = [None if t is None else t.data_ptr() for t in (dx, *dw, space)]
         head, tail = (p.index, p.experts, p.slots, p.n, p.cols, p.type), (p.rows, x.data_ptr(), p.ld, p.map, p.offsets)
         given = (dy.data_ptr(), dy.stride(0) if dy.shape[0] > 1 else p.n, p.list, p.each, *address, size, p.stream)
@@ -548,6 +548,9 @@ class AdamW:
                 or not all(map(_contiguous, params))):
             raise ValueError("params: shapes, types and GPU must stay as they were, and tensors contiguous")
         if params:
+            places = [a for a in map(_address, params) if a]
+            if len(set(places)) != len(places):
+                raise ValueError("params: a tensor is there twice")
             entries["p"] = list(map(_address, params))
             entries["g"] = list(map(_address, grads))
             entries["g_type"] = [_TYPES[k] for k in kinds]

@@ -156,7 +156,7 @@ _SIGS = {
     "netsim_experts_product": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P]),
     "netsim_experts_gated": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _I64, _P, _P,
                                     _P]),
-    "netsim_experts_backward_work_bytes": (_I64, [_I32, _I64, _I32, _I32, _I32, _I32, _I32]),
+    "netsim_experts_backward_work_bytes": (_I64, [_I32, _I64, _I32, _I32, _I32, _I32]),
     "netsim_experts_product_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P,
                                                _I32, _P, _P, _P, _I64, _P]),
     "netsim_experts_gated_backward": (_I32, [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _I64, _P, _I64, _P, _P, _P, _P, _P, _P, _P, _I64,
@@ -563,8 +563,8 @@ def netsim_experts_gated(device, experts, slots, n, cols, type, activation, rows
                                                      _stream(stream)))
 
 
-def netsim_experts_backward_work_bytes(experts, slots, n, cols, matrices, has_offsets, has_rows) -> int:
-    return load_library().netsim_experts_backward_work_bytes(experts, slots, n, cols, matrices, has_offsets, has_rows)
+def netsim_experts_backward_work_bytes(experts, slots, n, cols, matrices, by_row) -> int:
+    return load_library().netsim_experts_backward_work_bytes(experts, slots, n, cols, matrices, by_row)
 
 
 def netsim_experts_product_backward(device, experts, slots, n, cols, type, rows, d_x, ld_x, d_row_of_slot, d_offsets, d_w,

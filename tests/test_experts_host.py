@@ -61,8 +61,8 @@ def test_products_backward():
     for bad in bads + [dict(g=None), dict(u=None), dict(u=P + 2),dict(act=2), dict(dw2=None), dict(dw=None), dict(dw2=P + 1), dict(size=0), dict(work=None)]:
         refused(ns.netsim_experts_gated_backward, *{**base, **bad}.values())
     size = ns.netsim_experts_backward_work_bytes
-    assert size(0, 8, 16, 16, 1, 1, 1) == -1 and size(4, 8, 16, 16, 3, 1, 1) == -1 and size(4, 8, 16, 1 << 21, 1, 1, 1) == -1
-    assert size(4, 8, 16, 16, 2, 1, 1) > size(4, 8, 16, 16, 1, 1, 1) > 0 and size(4, 0, 16, 16, 2, 1, 1) >= 0
+    assert size(0, 8, 16, 16, 1, 1) == -1 and size(4, 8, 16, 16, 3, 1) == -1 and size(4, 8, 16, 1 << 21, 1, 1) == -1
+    assert size(4, 8, 16, 16, 2, 1) > size(4, 8, 16, 16, 1, 1) > size(4, 8, 16, 16, 1, 0) >= 0 and size(4, 0, 16, 16, 2, 1) >= 0
 
 
 def test_eight():

@@ -156,6 +156,31 @@ def test_nothing_and_none(gpu):
         y.backward()
 
 
+def test_refusals(gpu):
+    torch, moe = gpu
+    p = torch.ones(8, device="cuda")
+    opt = moe.AdamW([p, p])
+    with pytest.raises(ValueError, match="twice"):
+        opt.step([p.clone(), p.clone()])
+    opt = moe.AdamW([p])
+    for bad in ([torch.ones(9, device="cuda")], [torch.ones(2, 4, device="cuda")], [torch.ones(8)], [torch.ones(8, device="cuda").double()],
+                [torch.ones(16, device="cuda")[::2]], []):
+        with pytest.raises(ValueError):
+            opt.step(bad)
+    q = torch.ones(8, device="cuda", requires_grad=True)
+    opt = moe.AdamW([q])
+    q.data = torch.ones(4, device="cuda")
+    with pytest.raises(ValueError, match="params"):
+        opt.step([torch.ones(8, device="cuda")])
+    assert opt.steps == 0 and torch.equal(p, torch.ones_like(p))
+    with pytest.raises(ValueError):
+        moe.AdamW([p], masters=[p.clone()])
+    with pytest.raises(ValueError):
+        moe.AdamW([p], moments=[moe.Moments(torch.zeros(9, device="cuda"), torch.zeros(8, device="cuda"))])
+    with pytest.raises(ValueError):
+        moe.AdamW([p], bits=8, moments=[moe.Moments(torch.zeros(8, device="cuda"), torch.zeros(8, device="cuda"))])
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_undefined_gradients_stay_with_their_block(gpu, bits):
     torch, moe = gpu
