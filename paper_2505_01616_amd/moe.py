@@ -548,10 +548,10 @@ class AdamW:
                 or not all(map(_contiguous, params))):
             raise ValueError("params: shapes, types and GPU must stay as they were, and tensors contiguous")
         if params:
-            places = [a for a in map(_address, params) if a]
-            if len(set(places)) != len(places):
+            places = list(map(_address, params))
+            if len(set(places)) != len(places) and len(set(filter(None, places))) != len(list(filter(None, places))):
                 raise ValueError("params: a tensor is there twice")
-            entries["p"] = list(map(_address, params))
+            entries["p"] = places
             entries["g"] = list(map(_address, grads))
             entries["g_type"] = [_TYPES[k] for k in kinds]
             index, stream = _at(params[0].device)
