@@ -415,3 +415,97 @@ def test_same_bits(gpu):
         out = (y, *torch.autograd.grad(y, [x, wg, wu], dy.detach()))
         assert first is None or all(torch.equal(a, b) for a, b in zip(out, first))
         first = out
+
+
+@pytest.mark.parametrize("cols", [64, 50])
+@pytest.mark.parametrize("slots", [50, 700])
+def test_outputs_inside_wider_arrays(gpu, cols, slots):
+    """The C calls on parts of wider arrays; offsets that decrease or leave the
+    array (which callers must not give) write nothing outside the result."""
+    torch, moe = gpu
+    from paper_2505_01616_amd import netsim as ns
+    rng = np.random.default_rng(10)
+    experts, n, pad = 4, 72, 5
+    make = lambda *s: torch.from_numpy(rng.normal(0, 1, s)).bfloat16().cuda()      # noqa: E731
+    x, w, w2 = make(slots, cols), make(experts, n, cols), make(experts, n, cols)
+    x8, w8 = moe.quantise(x), moe.quantise(w)
+    stream = torch.cuda.current_stream().cuda_stream
+    for k, bounds in enumerate(([0, slots // 3, slots // 3, slots - 4, slots - 1], [5, 2, 9 * slots, -3, slots // 2])):
+        offsets = torch.tensor(bounds, dtype=torch.int32, device="cuda")
+        for op in range(3):
+            wide = torch.full((3 * slots, n + pad), 7.0, dtype=torch.bfloat16, device="cuda")
+            y = wide[slots:2 * slots, :n]
+            tail = (slots, x.data_ptr(), cols, None, offsets.data_ptr())
+            if op == 0:
+                ns.netsim_experts_product(0, experts, slots, n, cols, ns.BF16, *tail, w.data_ptr(), y.data_ptr(), n + pad, stream)
+                want = moe.product(x, w, offsets) if k == 0 else None
+            elif op == 1:
+                ns.netsim_experts_gated(0, experts, slots, n, cols, ns.BF16, ns.SILU, *tail, w.data_ptr(), w2.data_ptr(), y.data_ptr(),
+                                        n + pad, None, None, stream)
+                want = moe.gated(x, w, w2, offsets) if k == 0 else None
+            else:
+                ns.netsim_experts_product8(0, experts, slots, n, cols, slots, x8.q.data_ptr(), x8.scales.data_ptr(), None,
+                                           offsets.data_ptr(), w8.q.data_ptr(), w8.scales.data_ptr(), ns.BF16, y.data_ptr(), n + pad, stream)
+                want = moe.product8(x8, w8, offsets) if k == 0 else None
+            assert want is None or torch.equal(y, want)
+            y.fill_(7.0)
+            assert bool((wide == 7.0).all()), (k, op)
+        if k:
+            leaves = [t.detach().requires_grad_() for t in (x, w, w2)]
+            torch.autograd.grad(moe.gated(*leaves, offsets), leaves, torch.ones((slots, n), dtype=torch.bfloat16, device="cuda"))
+            torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("act", [None, "gelu"])
+def test_large_tiles(gpu, kind, act):
+    """Sizes that take tiles of 256 (but one matrix's gradients), rows from a list with some
+    missing, last tiles and steps of every kind cut short."""
+    torch, moe = gpu
+    g = torch.Generator(device="cuda").manual_seed(11)
+    t = types(torch)[kind]
+    experts, slots, rows, n, cols = 3, 14000, 5000, 1288, 1096
+    w = [(torch.randn((experts, n, cols), generator=g, device="cuda") * cols ** -0.5).to(t) for _ in range(2 if act else 1)]
+    x = torch.randn((rows, cols + 8), generator=g, device="cuda").to(t)[:, :cols]
+    dy = torch.randn((slots, n), generator=g, device="cuda").to(t)
+    offsets = torch.tensor([3, 9001, 9001, 13990], dtype=torch.int32, device="cuda")
+    row = (torch.arange(slots, device="cuda") * 7 % rows).int()
+    row[[4000, 9500]] = -1
+    at = row.long().clamp(min=0)
+    order = torch.argsort(torch.where(row < 0, rows, at), stable=True)[: slots - 2]
+    first = torch.searchsorted(at[order], torch.arange(rows, device="cuda"))
+    place = torch.arange(slots - 2, device="cuda") - first[at[order]]
+    lists = torch.full((rows, 3), -1, dtype=torch.int32, device="cuda")
+    lists[at[order], place] = order.int()
+    leaves = [v.detach().requires_grad_() for v in (x, *w)]
+    more = dict(offsets=offsets, row_of_slot=row, slots_of_row=lists)
+    y = moe.gated(*leaves, activation=act, **more) if act else moe.product(*leaves, **more)
+    got = (y.detach(), *torch.autograd.grad(y, leaves, dy))
+    # the same in 64 bits, expert by expert
+    X, W, D = x.double(), [v.double() for v in w], dy.double()
+    want = [torch.zeros((slots, n), dtype=torch.float64, device="cuda"), torch.zeros_like(X), *(torch.zeros_like(v) for v in W)]
+    bounds = offsets.tolist()
+    for e in range(experts):
+        s = torch.arange(bounds[e], bounds[e + 1], device="cuda")
+        s = s[row[s] >= 0]
+        if not len(s):
+            continue
+        v = [X[at[s]].requires_grad_(), *(u[e].clone().requires_grad_() for u in W)]
+        z = v[0] @ v[1].t()
+        if act:
+            z = torch.nn.functional.gelu(z) * (v[0] @ v[2].t())
+        grads = torch.autograd.grad(z, v, D[s])
+        want[0][s] = z.detach()
+        want[1].index_add_(0, at[s], grads[0])
+        for i, d in enumerate(grads[1:]):
+            want[2 + i][e] = d
+    # a rounding of the result, and of dg and du before it: each at most a half
+    # step of every value, so together 2.1 of them in the 2-norm; element by
+    # element against the largest, as sums of cancelling terms are off by theirs
+    for a, b in zip(got, want):
+        a = a.double()
+        assert float((a - b).norm() / b.norm()) <= 2.1 * HALF[kind]
+        assert float((a - b).abs().max()) <= 2.1 * HALF[kind] * float(b.abs().max())
+    zero = torch.zeros_like(row, dtype=torch.bool)
+    zero[:3] = zero[13990:] = zero[4000] = zero[9500] = True
+    assert not got[0][zero].any() and not got[2][1].any()
