@@ -5,6 +5,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -15,7 +17,7 @@ SOURCES = ["netsim.cpp", "fabric.cpp", "kernels.hip", "wave.hip", "xwave.hip", "
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
-    "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
+    "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
     # no implicit a*b+c contraction: every product and sum rounds on its own
     "-ffp-contract=off",
     # packed fp32 instructions are kept out of the device code
@@ -24,13 +26,23 @@ FLAGS = [
 ]
 
 
+JOBS = 8    # sources compiled at a time
+
+
 def build(verbose: bool = False) -> str:
-    srcs = [os.path.join(CSRC, s) for s in SOURCES]
+    def run(*args):
+        if verbose:
+            print(" ".join(args), flush=True)
+        subprocess.run(args, check=True)
+
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [HIPCC, *FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp, *srcs]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(JOBS) as pool:
+        def compiled(source):
+            out = os.path.join(objects, source + ".o")
+            run(HIPCC, *FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c", "-o", out, os.path.join(CSRC, source))
+            return out
+
+        run(HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", tmp, *pool.map(compiled, SOURCES))
     os.replace(tmp, LIB)
     return LIB
 
